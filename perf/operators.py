@@ -123,7 +123,8 @@ def _quantise(x):
     x = x.float().unflatten(-1, (ng, -1))
     lo, hi = x.amin(-1, keepdim=True), x.amax(-1, keepdim=True)
     mn = lo.bfloat16().float()
-    sc = ((hi - lo) / 15.0).bfloat16().float()
+    # a quotient of tensors: division by a number may multiply by its rounded inverse
+    sc = ((hi - lo) / torch.full_like(hi, 15.0)).bfloat16().float()
     # in 64 bits: a quotient next to a border must fall on its own side of it
     q = (x.double() - mn.double()) / torch.where(sc > 0, sc, 1.0).double()
     codes = torch.where(sc > 0, q.round().clamp(0, 15), 0.0).to(torch.uint8)
