@@ -13,6 +13,7 @@ import threading
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libmg.so")
 HEADER_PATH = os.path.join(os.path.dirname(HERE), "include", "mg_attn.h")
+KV4_HEADER_PATH = os.path.join(os.path.dirname(HERE), "include", "mg_kv4.h")
 CONV_HEADER_PATH = os.path.join(os.path.dirname(HERE), "include", "mg_conv.h")
 
 STRICT_F32 = 0
@@ -76,6 +77,22 @@ def _declare(lib):
     lib.mg_conv2d_bwd_workspace_bytes.restype = c_size
     lib.mg_conv2d_bwd.argtypes = [vp, vp, vp, vp, vp, shp, c_int, vp, c_size, vp]
     lib.mg_conv2d_bwd.restype = c_int
+    lib.mg_kv4_cache_bytes.argtypes = [c_int, c_int, c_int, c_int]
+    lib.mg_kv4_cache_bytes.restype = c_size
+    lib.mg_kv4_append.argtypes = [vp, vp, vp, vp, vp, vp, c_int, c_int, c_int, c_int, c_int,
+                                  c_int, vp]
+    lib.mg_kv4_append.restype = c_int
+    lib.mg_kv4_read.argtypes = [vp, vp, vp, vp, vp, c_int, c_int, c_int, c_int, c_int, c_int, vp]
+    lib.mg_kv4_read.restype = c_int
+    lib.mg_attn_fwd_kv4_workspace_bytes.argtypes = [c_int, c_int, c_int, c_int, c_int, c_int,
+                                                    c_int, c_int]
+    lib.mg_attn_fwd_kv4_workspace_bytes.restype = c_size
+    lib.mg_attn_fwd_kv4.argtypes = [vp, vp, vp, vp, vp, vp, vp, c_int, c_int, c_int, c_int, c_int,
+                                    c_int, c_int, c_float, c_int, vp, c_size, vp]
+    lib.mg_attn_fwd_kv4.restype = c_int
+    lib.mg_kv4_evict.argtypes = [vp, vp, vp, vp, vp, vp, vp, c_int, c_int, c_int, c_int, c_int,
+                                 c_int, vp]
+    lib.mg_kv4_evict.restype = c_int
     lib.mg_status_string.argtypes = [c_int]
     lib.mg_status_string.restype = ctypes.c_char_p
     lib.mg_last_error_detail.argtypes = []

@@ -1,5 +1,5 @@
-"""Build libmg.so (the C-ABI attention and convolution-derivative library)
-in-tree for gfx950.
+"""Build libmg.so (the C-ABI attention, convolution-derivative and 4-bit cache
+library) in-tree for gfx950.
 
     python -m paper_2608_01563_amd.build [-v]
 
@@ -18,6 +18,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
+PARTS = ("conv", "kv4")   # folders of csrc/ with sources of their own
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libmg.so")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
@@ -55,12 +56,12 @@ def _compile(src, verbose):
 
 
 def build(verbose=False):
-    """Compile every source under csrc/ and csrc/conv/ and link libmg.so; returns
+    """Compile every source under csrc/ and its folders and link libmg.so; returns
     its path."""
     os.makedirs(BUILD_DIR, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "*.cpp")) +
-                  glob.glob(os.path.join(CSRC, "conv", "*.hip")) +
-                  glob.glob(os.path.join(CSRC, "conv", "*.cpp")))
+                  [f for part in PARTS for ext in ("*.hip", "*.cpp")
+                   for f in glob.glob(os.path.join(CSRC, part, ext))])
     with cf.ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
         objs = list(ex.map(lambda s: _compile(s, verbose), srcs))
     tmp = LIB_PATH + ".tmp%d" % os.getpid()

@@ -1,0 +1,523 @@
+// kv4_rows.hip -- attention over the 4-bit cache: a workgroup takes 16 of the
+// query rows that share a cache head and one share of the tokens; its four
+// waves take 32-token blocks in turn, each with its own online softmax, and
+// join through LDS; shares join in kv4_join.
+//
+// Scores: kv4_tile.h.  The second product is O^T = V^T P^T on V's codes:
+//   O = sum_j (p_j scale_j) code_j + sum_j p_j min_j
+// with p scale rounded to f16 (within 2^-12; strict: two parts, 2^-23) and the
+// second sum in f32 from the unrounded p.  f16 holds p scale because both
+// factors are taken relative to a running bound: p to 2^kSlack above 1, and the
+// scales to a power of two of the row's own, moved up (and the sums rescaled,
+// as for a new maximum) when a block has a larger one.  kRaise lifts the
+// products to the top of f16's range, so that values 2^-25 below the largest
+// keep all their bits.
+#include "cdiv.h"
+#include "kv4_launch.h"
+#include "kv4_tile.h"
+
+namespace mg {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kRows = 16;
+constexpr float kRowSlack = 4.f;
+constexpr int kRaise = 11;    // 2^(slack + 11) = 2^15 at most
+constexpr int kExpMax = 100;  // bound on the scales' exponent (|V| about 2^104)
+
+struct RowsArgs {
+    const void *Q;
+    const uint32_t *kw, *vw, *kp, *vp;
+    void *O;
+    float *LSE, *part, *stat, *score;
+    const int32_t *key_len, *q_len;
+    int H, G, Lq, L, Lp, causal;
+    float scale_log2;
+    int splits, row_tiles;
+};
+
+// Where row r = i * G + g of a cache head lies among the query rows.
+struct RowAt {
+    int i;
+    size_t at;   // row of [B][Hq][Lq]
+};
+__device__ __forceinline__ RowAt row_at(int r, int bh, int G, int Lq) {
+    const int i = r / G;
+    return {i, ((size_t)bh * G + (r - i * G)) * Lq + i};
+}
+
+template <int D>
+struct Kv4Values {
+    static constexpr int NG = Kv4Dim<D>::kGroups, NB = Kv4Dim<D>::kBlocks, W = Kv4Dim<D>::kWide;
+    uint32_t w[NB], group[8 * NG];   // word of channel 16b + c of the lane's octet
+
+    __device__ __forceinline__ void load(const uint32_t *words, const uint32_t *groups, int block,
+                                         int c, int g) {
+        typedef uint32_t wv __attribute__((ext_vector_type(W)));
+        const uint32_t *p = words + (size_t)(4 * block + g) * D + W * c;
+#pragma unroll
+        for (int h = 0; h < NB / W; ++h) {
+            const wv v = *reinterpret_cast<const wv *>(p + 16 * W * h);
+#pragma unroll
+            for (int i = 0; i < W; ++i) w[W * h + i] = v[i];
+        }
+        const uint32_t *q = groups + (size_t)(32 * block + 8 * g) * NG;
+#pragma unroll
+        for (int i = 0; i < 2 * NG; ++i) {
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(q + 4 * i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) group[4 * i + k] = v[k];
+        }
+    }
+};
+
+template <typename T, int D, int NP>
+__global__ __launch_bounds__(kThreads)
+void kv4_rows(RowsArgs a) {
+    constexpr int NG = Kv4Dim<D>::kGroups, NB = Kv4Dim<D>::kBlocks;
+    constexpr int LD = D + 4;
+    __shared__ __attribute__((aligned(16))) float Os[kWaves][kRows][LD];
+    __shared__ float Ms[kWaves][kRows], Ls[kWaves][kRows];
+
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tile = blockIdx.x % a.row_tiles, share = blockIdx.x / a.row_tiles;
+    const int bh = share / a.splits, split = share - bh * a.splits;
+    const int b = bh / a.H;
+    const int rows = a.G * a.Lq;
+    const Kv4Mask mask = sequence_mask(a.key_len, a.q_len, b, a.L, a.Lq, a.causal);
+
+    // the tile's rows, and the tokens that its last and its first row see
+    const int r = kRows * tile + c;
+    const bool in = r < rows;
+    const RowAt at = row_at(in ? r : rows - 1, bh, a.G, a.Lq);
+    const int first_i = kRows * tile / a.G;
+    const int last_i = min((min(rows, kRows * (tile + 1)) - 1) / a.G, mask.rows - 1);
+    const int end = first_i < mask.rows ? max(mask.limit(last_i), 0) : 0;
+    const int all = mask.limit(first_i);   // below: every row sees the token
+    const int limit = mask.limit(at.i);
+
+    const int blocks = (end + 31) / 32, each = (blocks + a.splits - 1) / a.splits;
+    const int begin = split * each, stop = min(blocks, begin + each);
+
+    const size_t head = (size_t)bh * a.Lp;
+    const uint32_t *kw = a.kw + head * (D / 8), *vw = a.vw + head / 8 * D;
+    const uint32_t *kp = a.kp + head * NG, *vp = a.vp + head * NG;
+
+    Kv4Query<D, NP> q;
+    q.load(static_cast<const T *>(a.Q) + at.at * D, in, g);
+    const float factor = row_factor(a.scale_log2, q.exponent);
+
+    float m = -INFINITY;               // running maximum (base 2) rounded up, of the row
+    int e = -kExpMax;                  // V's scales are below 2^e
+    uint32_t most = 0;                 // ... as a bound on their group words
+    float l = 0.f;                     // sum of p 2^(kRaise - e)
+    float low[NG];                     // sums of p min in the same units
+    f32x4 o[NB];                       // O^T[16 b + 4g + r][row c], over kCodeUnit
+#pragma unroll
+    for (int i = 0; i < NG; ++i) low[i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) o[i] = zero4();
+
+    auto step = [&](int block, const Kv4Keys<D> &key, Kv4Values<D> &val) {
+        f32x4 s[2];
+        key.scores(s, q);
+        s[0] *= factor;
+        s[1] *= factor;
+        if (32 * (block + 1) > all) {
+            // tokens out of sight: no score, and group words (which may hold
+            // anything behind the sequence) that add nothing
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (32 * block + 8 * g + k >= limit) {
+                    s[k >> 2][k & 3] = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < NG; ++i) val.group[k * NG + i] = 0;
+                }
+        }
+        if (a.score != nullptr && in) {
+            float *to = a.score + ((size_t)bh * rows + r) * a.Lp + 32 * block + 8 * g;
+            *reinterpret_cast<f32x4 *>(to) = s[0];
+            *reinterpret_cast<f32x4 *>(to + 4) = s[1];
+        }
+        float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                         fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        mx = max_over_groups(mx);
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < 8 * NG; ++k) top = max(top, val.group[k]);
+        if (__any(mx > m + kRowSlack || top > most)) {
+            // NaN scales (a token that is not finite) move nothing
+            top = 0;
+#pragma unroll
+            for (int k = 0; k < 8 * NG; ++k)
+                top = max(top, val.group[k] < 0x7f800000u ? val.group[k] : 0u);
+            top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+            top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+            const float m_new = fmaxf(m, ceilf(mx));
+            const int e_new = max(e, min(kExpMax, (int)(top >> 23) - 126));
+            const float alpha =
+                m_new == -INFINITY ? 1.f : ldexpf(exp2_fast(m - m_new), e - e_new);
+            l *= alpha;
+#pragma unroll
+            for (int i = 0; i < NG; ++i) low[i] *= alpha;
+#pragma unroll
+            for (int i = 0; i < NB; ++i) o[i] *= alpha;
+            m = m_new;
+            e = e_new;
+            most = e == kExpMax ? 0xffffffffu : ((uint32_t)(e + 127) << 23) - 1;
+        }
+        const float off = (m == -INFINITY ? 0.f : m) + (float)(e - kRaise);
+        float p[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            p[k] = exp2_fast(s[k >> 2][k & 3] - off);
+            l += p[k];
+        }
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+            float x[8];
+            f16x8 part[NP];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t gw = val.group[k * NG + i];
+                x[k] = p[k] * group_scale(gw);
+                low[i] = fmaf(p[k], group_min(gw), low[i]);
+            }
+            split_operand<NP>(part, x);
+#pragma unroll
+            for (int cb = i * (NB / NG); cb < (i + 1) * (NB / NG); ++cb) {
+                const f16x8 v = code_operand(val.w[cb]);
+#pragma unroll
+                for (int n = 0; n < NP; ++n) o[cb] = mfma16x16x32f16(v, part[n], o[cb]);
+            }
+        }
+    };
+
+    // blocks begin + w, + kWaves, ...; the next one's words load while one is
+    // worked on (past the end the last block again)
+    const int mine = begin + w;
+    if (mine < stop) {
+        Kv4Keys<D> k0, k1;
+        Kv4Values<D> v0, v1;
+        k0.load(kw, kp, mine, c, g);
+        v0.load(vw, vp, mine, c, g);
+        for (int block = mine; block < stop; block += 2 * kWaves) {
+            const int b1 = min(block + kWaves, stop - 1), b2 = min(block + 2 * kWaves, stop - 1);
+            k1.load(kw, kp, b1, c, g);
+            v1.load(vw, vp, b1, c, g);
+            step(block, k0, v0);
+            if (block + kWaves >= stop) break;
+            k0.load(kw, kp, b2, c, g);
+            v0.load(vw, vp, b2, c, g);
+            step(block + kWaves, k1, v1);
+        }
+    }
+
+    // out of the running units, then the waves' shares through LDS
+    l = ldexpf(sum_over_groups(l), e - kRaise);
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+        const float base = sum_over_groups(low[i]);
+#pragma unroll
+        for (int cb = i * (NB / NG); cb < (i + 1) * (NB / NG); ++cb) {
+            f32x4 x;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = ldexpf(fmaf(o[cb][k], kCodeUnit, base), e - kRaise);
+            *reinterpret_cast<f32x4 *>(&Os[w][c][16 * cb + 4 * g]) = x;
+        }
+    }
+    if (g == 0) {
+        Ms[w][c] = m;
+        Ls[w][c] = l;
+    }
+    __syncthreads();
+
+    constexpr int N = D / 16;   // channels a thread writes
+    const int row = tid >> 4, d0 = N * (tid & 15);
+    const int rr = kRows * tile + row;
+    if (rr >= rows) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) top = fmaxf(top, Ms[k][row]);
+    float sum = 0.f, x[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+        const float f = top == -INFINITY ? 1.f : exp2_fast(Ms[k][row] - top);
+        sum = fmaf(f, Ls[k][row], sum);
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = fmaf(f, Os[k][row][d0 + i], x[i]);
+    }
+    const RowAt to = row_at(rr, bh, a.G, a.Lq);
+    const bool valid = to.i < mask.rows;
+    if (a.splits > 1) {
+        const size_t slot = ((size_t)bh * a.splits + split) * rows + rr;
+        float *p = a.part + slot * D + d0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = valid ? x[i] : 0.f;
+        if (d0 == 0) {
+            a.stat[2 * slot] = valid ? top : -INFINITY;
+            a.stat[2 * slot + 1] = valid ? sum : 0.f;
+        }
+        return;
+    }
+    if (!valid) sum = 0.f;
+    const float inv = 1.f / sum;
+    T *out = static_cast<T *>(a.O) + to.at * D + d0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float y = sum == 0.f ? 0.f : x[i] * inv;
+        if constexpr (sizeof(T) == 2) out[i] = f32_to_bf16_rne(y);
+        else out[i] = y;
+    }
+    if (d0 == 0) a.LSE[to.at] = sum != sum ? sum : row_lse(top, sum);
+}
+
+// ------------------------------------------------------------------- joining --
+struct JoinArgs {
+    void *O;
+    float *LSE, *weight;
+    const float *part, *stat, *score;
+    const int32_t *key_len, *q_len;
+    int H, G, Lq, L, Lp, causal, splits, heads, out_groups;
+};
+constexpr int kJoinKeys = 4 * kThreads;   // tokens of a weights workgroup
+
+// Row's maximum and sum over the splits.
+__device__ __forceinline__ void joined_stat(const float *stat, size_t first, int stride,
+                                            int splits, float *top, float *sum) {
+    float m = -INFINITY, l = 0.f;
+    for (int k = 0; k < splits; ++k) m = fmaxf(m, stat[2 * (first + (size_t)k * stride)]);
+    if (m > -INFINITY)
+        for (int k = 0; k < splits; ++k) {
+            const float *st = stat + 2 * (first + (size_t)k * stride);
+            l = fmaf(exp2_fast(st[0] - m), st[1], l);
+        }
+    else   // no score above -inf: the sums are 0, or NaN where a score is
+        for (int k = 0; k < splits; ++k) l += stat[2 * (first + (size_t)k * stride) + 1];
+    *top = m;
+    *sum = l;
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads)
+void kv4_join(JoinArgs a) {
+    const int rows = a.G * a.Lq;
+    if ((int)blockIdx.x < a.out_groups) {
+        // a wave joins a row
+        const int id = blockIdx.x * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+        const int bh = id / rows, r = id - bh * rows;
+        if (bh >= a.heads) return;
+        const size_t first = (size_t)bh * a.splits * rows + r;
+        float top, sum;
+        joined_stat(a.stat, first, rows, a.splits, &top, &sum);
+        constexpr int N = D < 64 ? 1 : D / 64;
+        const bool mine = D >= 64 || lane < D;
+        const int d0 = mine ? N * lane : 0;
+        float x[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = 0.f;
+        for (int k = 0; k < a.splits; ++k) {
+            const size_t slot = first + (size_t)k * rows;
+            const float f = top > -INFINITY ? exp2_fast(a.stat[2 * slot] - top) : 1.f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = fmaf(f, a.part[slot * D + d0 + i], x[i]);
+        }
+        const RowAt to = row_at(r, bh, a.G, a.Lq);
+        if (mine) {
+            T *out = static_cast<T *>(a.O) + to.at * D + d0;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float y = sum == 0.f ? 0.f : x[i] / sum;
+                if constexpr (sizeof(T) == 2) out[i] = f32_to_bf16_rne(y);
+                else out[i] = y;
+            }
+        }
+        if (lane == 0) a.LSE[to.at] = sum != sum ? sum : row_lse(top, sum);
+        return;
+    }
+    // weights: a thread adds the rows' probabilities of four tokens
+    __shared__ float lse2[kRows];
+    const int per = (a.Lp + kJoinKeys - 1) / kJoinKeys;
+    const int id = blockIdx.x - a.out_groups, bh = id / per;
+    const int j0 = (id - bh * per) * kJoinKeys + 4 * threadIdx.x;
+    const int b = bh / a.H;
+    const Kv4Mask mask = sequence_mask(a.key_len, a.q_len, b, a.L, a.Lq, a.causal);
+    if ((id - bh * per) * kJoinKeys >= mask.n) return;
+    if ((int)threadIdx.x < rows) {
+        const int r = threadIdx.x;
+        const RowAt at = row_at(r, bh, a.G, a.Lq);
+        float v;
+        if (a.splits > 1) {
+            float top, sum;
+            joined_stat(a.stat, (size_t)bh * a.splits * rows + r, rows, a.splits, &top, &sum);
+            v = sum == 0.f ? INFINITY : top + log2f(sum);
+        } else {
+            v = a.LSE[at.at] * kLog2e;
+            if (v == -INFINITY) v = INFINITY;
+        }
+        lse2[r] = at.i < mask.rows ? v : INFINITY;   // a row without sight adds nothing
+    }
+    __syncthreads();
+    if (j0 >= mask.n) return;
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < rows; ++r) {
+        const float z = lse2[r];
+        if (z == INFINITY) continue;
+        const RowAt at = row_at(r, bh, a.G, a.Lq);
+        const int limit = mask.limit(at.i);
+        // scores of blocks behind the row tile's last token were not written
+        const f32x4 s = *reinterpret_cast<const f32x4 *>(a.score + ((size_t)bh * rows + r) * a.Lp +
+                                                         j0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (j0 + k < limit) w[k] += exp2_fast(s[k] - z);
+    }
+    float *to = a.weight + (size_t)bh * a.L + j0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (j0 + k < mask.n) to[k] += w[k];
+}
+
+// ------------------------------------------------- weights from Q, K and LSE --
+struct WeightArgs {
+    const void *Q;
+    const uint32_t *kw, *kp;
+    const float *LSE;
+    float *weight;
+    const int32_t *key_len, *q_len;
+    int H, G, Lq, L, Lp, causal, groups;   // workgroups a head
+    float scale_log2;
+};
+
+// A wave keeps 32 tokens' codes and goes through the rows that see them.
+template <typename T, int D, int NP>
+__global__ __launch_bounds__(kThreads)
+void kv4_weights(WeightArgs a) {
+    constexpr int NG = Kv4Dim<D>::kGroups;
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    const int bh = blockIdx.x / a.groups;
+    const int block = (blockIdx.x - bh * a.groups) * kWaves + (threadIdx.x >> 6);
+    const Kv4Mask mask = sequence_mask(a.key_len, a.q_len, bh / a.H, a.L, a.Lq, a.causal);
+    if (32 * block >= mask.n) return;
+
+    const size_t head = (size_t)bh * a.Lp;
+    Kv4Keys<D> key;
+    key.load(a.kw + head * (D / 8), a.kp + head * NG, block, c, g);
+
+    float sum[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[k] = 0.f;
+    const int rows = mask.rows * a.G;
+    const int first_i = a.causal ? max(0, 32 * block - (mask.n - mask.rows)) : 0;
+    for (int r0 = first_i * a.G / kRows * kRows; r0 < rows; r0 += kRows) {
+        const int r = r0 + c;
+        const bool in = r < rows;
+        const RowAt at = row_at(in ? r : 0, bh, a.G, a.Lq);
+        Kv4Query<D, NP> q;
+        q.load(static_cast<const T *>(a.Q) + at.at * D, in, g);
+        const float lse = a.LSE[at.at];
+        const float factor = row_factor(a.scale_log2, q.exponent), off = lse * kLog2e;
+        // nothing from rows without sight (LSE -inf)
+        const int limit = in && lse != -INFINITY ? mask.limit(at.i) : 0;
+        f32x4 s[2];
+        key.scores(s, q);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (32 * block + 8 * g + k < limit)
+                sum[k] += exp2_fast(fmaf(s[k >> 2][k & 3], factor, -off));
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int m = 1; m < 16; m *= 2) sum[k] += xor_lanes(sum[k], m);
+    float *to = a.weight + (size_t)bh * a.L;
+    if (c < 8) {
+        float mine = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) mine = c == k ? sum[k] : mine;
+        const int j = 32 * block + 8 * g + c;
+        if (j < mask.n) to[j] += mine;
+    }
+}
+
+template <typename T, int D, int NP>
+hipError_t rows(const Kv4Attn &p, const Kv4Plan &plan, const void *Q,
+                const Kv4Cache<const uint32_t> &c, void *O, float *LSE, char *ws, hipStream_t s) {
+    const int tiles = (int)((kv4_rows(p) + kRows - 1) / kRows);
+    const RowsArgs a = {Q, c.k, c.v, c.kp, c.vp, O, LSE, (float *)(ws + plan.part),
+                        (float *)(ws + plan.stat),
+                        plan.scores ? (float *)(ws + plan.score) : nullptr, p.key_len, p.q_len,
+                        p.H, p.G, p.Lq, p.L, kv4_padded(p.L), p.causal, p.scale * kLog2e,
+                        plan.splits, tiles};
+    kv4_rows<T, D, NP><<<(unsigned)((int64_t)p.B * p.H * plan.splits * tiles), kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t join(const Kv4Attn &p, const Kv4Plan &plan, void *O, float *LSE, float *weight,
+                const char *ws, hipStream_t s) {
+    const int64_t heads = (int64_t)p.B * p.H;
+    const int64_t outs = plan.splits > 1 ? (heads * kv4_rows(p) + kWaves - 1) / kWaves : 0;
+    const int64_t keys = plan.scores ? heads * cdiv(kv4_padded(p.L), kJoinKeys) : 0;
+    const JoinArgs a = {O, LSE, weight, (const float *)(ws + plan.part),
+                        (const float *)(ws + plan.stat), (const float *)(ws + plan.score),
+                        p.key_len, p.q_len, p.H, p.G, p.Lq, p.L, kv4_padded(p.L), p.causal,
+                        plan.splits, (int)heads, (int)outs};
+    kv4_join<T, D><<<(unsigned)(outs + keys), kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, int D, int NP>
+hipError_t weights(const Kv4Attn &p, const void *Q, const Kv4Cache<const uint32_t> &c,
+                   const float *LSE, float *weight, hipStream_t s) {
+    const int groups = cdiv(kv4_padded(p.L) / 32, kWaves);
+    const WeightArgs a = {Q, c.k, c.kp, LSE, weight, p.key_len, p.q_len, p.H, p.G, p.Lq, p.L,
+                          kv4_padded(p.L), p.causal, groups, p.scale * kLog2e};
+    kv4_weights<T, D, NP><<<(unsigned)((int64_t)p.B * p.H * groups), kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv4_rows(const Kv4Attn &p, const Kv4Plan &plan, const void *Q, bool bf16,
+                           const Kv4Cache<const uint32_t> &c, void *O, float *LSE, void *ws,
+                           hipStream_t s) {
+    char *w = static_cast<char *>(ws);
+    if (bf16)
+        return p.d == 32 ? rows<uint16_t, 32, 1>(p, plan, Q, c, O, LSE, w, s)
+             : p.d == 64 ? rows<uint16_t, 64, 1>(p, plan, Q, c, O, LSE, w, s)
+                         : rows<uint16_t, 128, 1>(p, plan, Q, c, O, LSE, w, s);
+    return p.d == 32 ? rows<float, 32, 2>(p, plan, Q, c, O, LSE, w, s)
+         : p.d == 64 ? rows<float, 64, 2>(p, plan, Q, c, O, LSE, w, s)
+                     : rows<float, 128, 2>(p, plan, Q, c, O, LSE, w, s);
+}
+
+hipError_t launch_kv4_join(const Kv4Attn &p, const Kv4Plan &plan, bool bf16, void *O, float *LSE,
+                           float *weight, const void *ws, hipStream_t s) {
+    const char *w = static_cast<const char *>(ws);
+    if (bf16)
+        return p.d == 32 ? join<uint16_t, 32>(p, plan, O, LSE, weight, w, s)
+             : p.d == 64 ? join<uint16_t, 64>(p, plan, O, LSE, weight, w, s)
+                         : join<uint16_t, 128>(p, plan, O, LSE, weight, w, s);
+    return p.d == 32 ? join<float, 32>(p, plan, O, LSE, weight, w, s)
+         : p.d == 64 ? join<float, 64>(p, plan, O, LSE, weight, w, s)
+                     : join<float, 128>(p, plan, O, LSE, weight, w, s);
+}
+
+hipError_t launch_kv4_weights(const Kv4Attn &p, const void *Q, bool bf16,
+                              const Kv4Cache<const uint32_t> &c, const float *LSE, float *weight,
+                              hipStream_t s) {
+    if (bf16)
+        return p.d == 32 ? weights<uint16_t, 32, 1>(p, Q, c, LSE, weight, s)
+             : p.d == 64 ? weights<uint16_t, 64, 1>(p, Q, c, LSE, weight, s)
+                         : weights<uint16_t, 128, 1>(p, Q, c, LSE, weight, s);
+    return p.d == 32 ? weights<float, 32, 2>(p, Q, c, LSE, weight, s)
+         : p.d == 64 ? weights<float, 64, 2>(p, Q, c, LSE, weight, s)
+                     : weights<float, 128, 2>(p, Q, c, LSE, weight, s);
+}
+
+}  // namespace mg

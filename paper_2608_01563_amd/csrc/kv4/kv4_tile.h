@@ -1,0 +1,177 @@
+// kv4_tile.h -- scores of 16 query rows against 32 cached tokens, on the
+// 4-bit codes themselves.
+//
+//   q . k = sum over groups  scale (q_g . code_g) + min (sum of q_g)
+//
+// A byte that holds a code is that code times 2^-9 as an E4M3 number (the seven
+// subnormals and the first eight normals are evenly spaced), so two masks, a
+// shift and four conversions make the eight f16 operands of a word, exactly and
+// normal: about 24 clocks a wave.  (Codes masked in place into f16 subnormals cost
+// 12, but matrix products align operands by their exponent fields and lose the
+// leading zeros' bits: scores were off by 1.2e-5 where they are now off by 4e-7.)
+//
+// Products are S^T = K Q^T: a wave's 32 tokens are the rows of two 16x16x32
+// products, in the order that leaves lane group g = lane/16 with the eight
+// tokens 8g..8g+7 of its query row lane%16: row i of product t is token
+// 8(i/4) + 4t + i%4.  Those eight are an octet of V's words, so the
+// probabilities feed the second product from the lanes that hold them.
+#pragma once
+
+#include "kv4_device.h"
+
+namespace mg {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+// Which of eight consecutive values operand slot k holds: the order in which
+// code_operand finds a word's nibbles.
+__device__ __forceinline__ constexpr int slot_value(int k) { return k < 4 ? 2 * k : 2 * k - 7; }
+constexpr float kCodeUnit = 0x1p9f;   // an operand is a code over this
+
+__device__ __forceinline__ f16x8 code_operand(uint32_t w) {
+    const uint32_t even = w & 0x0f0f0f0fu, odd = (w >> 4) & 0x0f0f0f0fu;
+    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(even, 1.f, false);
+    const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(even, 1.f, true);
+    const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(odd, 1.f, false);
+    const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(odd, 1.f, true);
+    return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+__device__ __forceinline__ f32x4 mfma16x16x32f16(f16x8 a, f16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Eight f32 values as NP f16 operands in the slots of code_operand: one value
+// each within 2^-12, two parts together within 2^-23.
+template <int NP>
+__device__ __forceinline__ void split_operand(f16x8 (&out)[NP], const float (&x)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float v = x[slot_value(k)];
+        const _Float16 h = (_Float16)v;
+        out[0][k] = h;
+        if (NP > 1) out[1][k] = (_Float16)(v - (float)h);
+    }
+}
+
+// A query row as operands: q[p][s] holds channels 32s + 8g + e of part p, times
+// 2^(15 - exponent of the row's largest value); sum[gr] the group sums in the
+// units of a product with codes.
+template <int D, int NP>
+struct Kv4Query {
+    f16x8 q[NP][D / 32];
+    float sum[Kv4Dim<D>::kGroups];
+    int exponent;   // scores = products * 2^(exponent - 6)
+
+    template <typename T>
+    __device__ __forceinline__ void load(const T *row, bool valid, int g) {
+        constexpr int NS = D / 32, NG = Kv4Dim<D>::kGroups;
+        float x[NS][8];
+        float top = 0.f;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            if (valid) {
+                load_row(x[s], row + 32 * s + 8 * g);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[s][e]));
+        }
+        top = max_over_groups(top);
+        // 0 for zero, infinity and NaN
+        exponent = __builtin_amdgcn_frexp_expf(top);
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr) {
+            float t = 0.f;
+#pragma unroll
+            for (int s = gr * (NS / NG); s < (gr + 1) * (NS / NG); ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) t += ldexpf(x[s][e], -exponent);
+            sum[gr] = sum_over_groups(t) * 0x1p6f;
+        }
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            float y[8];
+            f16x8 part[NP];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = ldexpf(x[s][e], 15 - exponent);
+            split_operand<NP>(part, y);
+#pragma unroll
+            for (int p = 0; p < NP; ++p) q[p][s] = part[p];
+        }
+    }
+};
+
+// The K words of 32 tokens (two products) and their groups: all that scores need.
+template <int D>
+struct Kv4Keys {
+    static constexpr int NG = Kv4Dim<D>::kGroups, NW = D / 32;
+    uint32_t w[2][NW], group[8 * NG];   // group words of tokens 8g + k at k * NG
+
+    // `words`, `groups`: the head's regions.  c = lane%16, g = lane/16.
+    __device__ __forceinline__ void load(const uint32_t *words, const uint32_t *groups, int block,
+                                         int c, int g) {
+        typedef uint32_t wv __attribute__((ext_vector_type(NW)));
+        const int key = 32 * block + 8 * (c >> 2) + (c & 3);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const wv v = *reinterpret_cast<const wv *>(words + (size_t)(key + 4 * t) * (D / 8) +
+                                                       g * NW);
+#pragma unroll
+            for (int i = 0; i < NW; ++i) w[t][i] = v[i];
+        }
+        const uint32_t *p = groups + (size_t)(32 * block + 8 * g) * NG;
+#pragma unroll
+        for (int i = 0; i < 2 * NG; ++i) {
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(p + 4 * i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) group[4 * i + k] = v[k];
+        }
+    }
+
+    // s[t][r] = score of token 8g + 4t + r for the lane's row, before the row's factor.
+    template <int NP>
+    __device__ __forceinline__ void scores(f32x4 (&s)[2], const Kv4Query<D, NP> &q) const {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                f32x4 m = zero4();
+#pragma unroll
+                for (int i = gr * (NW / NG); i < (gr + 1) * (NW / NG); ++i) {
+                    const f16x8 a = code_operand(w[t][i]);
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) m = mfma16x16x32f16(a, q.q[p][i], m);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint32_t gw = group[(4 * t + r) * NG + gr];
+                    const float low = gr == 0 ? group_min(gw) * q.sum[gr]
+                                              : fmaf(group_min(gw), q.sum[gr], s[t][r]);
+                    s[t][r] = fmaf(group_scale(gw), m[r], low);
+                }
+            }
+    }
+};
+
+// A scale times log2 e and the row's power of two.
+__device__ __forceinline__ float row_factor(float scale_log2, int exponent) {
+    return ldexpf(scale_log2, exponent - 6);
+}
+
+// One sequence's lengths and mask: row i sees tokens below limit(i).
+struct Kv4Mask {
+    int n, rows, causal;   // tokens, query rows
+
+    __device__ __forceinline__ int limit(int i) const {
+        return causal ? min(n, i + 1 + n - rows) : n;
+    }
+};
+__device__ __forceinline__ Kv4Mask sequence_mask(const int32_t *key_len, const int32_t *q_len,
+                                                 int b, int L, int Lq, int causal) {
+    return {optional_len(key_len, b, L), optional_len(q_len, b, Lq), causal};
+}
+
+}  // namespace mg
