@@ -29,6 +29,7 @@ inline int64_t kv4_rows(const Kv4Attn &p) { return (int64_t)p.G * p.Lq; }
 
 // How one call runs.
 struct Kv4Plan {
+    int rows;          // of a workgroup: 16 (kv4_rows), 128 or 256 (kv4_many)
     int splits;        // workgroups that share a row tile's keys
     bool scores;       // weights come from scores the forward keeps
     size_t part, stat, score, bytes;   // workspace: offsets of the parts, size
@@ -38,6 +39,9 @@ Kv4Plan kv4_plan(const Kv4Attn &p, bool weights, bool bf16);
 hipError_t launch_kv4_rows(const Kv4Attn &p, const Kv4Plan &plan, const void *Q, bool bf16,
                            const Kv4Cache<const uint32_t> &c, void *O, float *LSE, void *ws,
                            hipStream_t s);
+hipError_t launch_kv4_many(const Kv4Attn &p, const Kv4Plan &plan, const void *Q,
+                           const Kv4Cache<const uint32_t> &c, void *O, float *LSE, void *ws,
+                           hipStream_t s);   // bf16
 // Joins the splits' outputs and adds the kept scores' probabilities to the
 // weights, whichever of the two there is.
 hipError_t launch_kv4_join(const Kv4Attn &p, const Kv4Plan &plan, bool bf16, void *O, float *LSE,

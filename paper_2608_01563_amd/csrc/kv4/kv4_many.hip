@@ -1,0 +1,422 @@
+// kv4_many.hip -- attention over the 4-bit cache for many query rows (bf16).
+//
+// Where kv4_rows.hip has every wave unpack the codes it multiplies, here a
+// workgroup of WAVES x 32 rows unpacks a tile of 64 tokens once into LDS and
+// all of its waves read it there (32x32x16 products, 32 rows a wave):
+//
+//   K   codes as f16, exact; scores are scaled and shifted a group at a time as
+//       in kv4_tile.h, the minima's part by one f32 product over the groups
+//   V   values v 2^(15-E) rounded to f16 (within 2^-11), E bounding all values
+//       so far, so that one product per 16 tokens covers scale and minimum
+//   P   f16, at most 2^15
+//
+// The row order of the score product swaps bits 2 and 3 of the token, which
+// leaves a lane with whole octets of tokens: V's words (8 tokens of a channel)
+// become 16-byte LDS pieces that the second product reads as they are.
+//
+// A tile's words are loaded an iteration before they are unpacked, and its
+// group words one before that, because unpacking V needs them from LDS.
+#include "cdiv.h"
+#include "kv4_launch.h"
+#include "kv4_tile.h"
+
+namespace mg {
+namespace {
+
+constexpr int kTokens = 64;
+constexpr float kManySlack = 4.f;
+constexpr int kLift = 11;      // P is at most 2^(slack + kLift) = 2^15
+constexpr int kManyExp = 100;  // bound on E
+
+typedef _Float16 f16x2v __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ f32x16 mfma32x32x16f16(f16x8 a, f16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma32x32x2(float a, float b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+}
+
+// 16-byte pieces of LDS rows of N pieces, permuted so that 16 rows read at the
+// same piece, or a row's pieces, fall on different banks.
+template <int N>
+__device__ __forceinline__ int piece(int row, int p) {
+    constexpr int ROWS = 16 / N < 1 ? 1 : 16 / N;   // rows that share 256 bytes
+    return row * N + (p ^ ((row / ROWS) & (N - 1)));
+}
+
+struct ManyArgs {
+    const uint16_t *Q;
+    const uint32_t *kw, *vw, *kp, *vp;
+    uint16_t *O;
+    float *LSE, *part, *stat;
+    const int32_t *key_len, *q_len;
+    int H, G, Lq, L, Lp, causal;
+    float scale_log2;
+    int splits, row_tiles;
+};
+
+// 32 query rows as operands of 32x32x16 products: lane column l%32, channels
+// 16s + 8(l/32) + e, in the slots of code_operand.
+template <int D>
+struct Query32 {
+    f16x8 q[D / 16];
+    float sum;      // of group l/32 (0 where there is no second)
+    int exponent;
+
+    __device__ __forceinline__ void load(const uint16_t *row, bool valid, int h) {
+        constexpr int NS = D / 16, NG = Kv4Dim<D>::kGroups;
+        float x[NS][8];
+        float top = 0.f;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            if (valid) {
+                load_row(x[s], row + 16 * s + 8 * h);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[s][e]));
+        }
+        exponent = __builtin_amdgcn_frexp_expf(max_xor32(top));
+        float each[2] = {0.f, 0.f};
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr) {
+            float t = 0.f;
+#pragma unroll
+            for (int s = gr * (NS / NG); s < (gr + 1) * (NS / NG); ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) t += ldexpf(x[s][e], -exponent);
+            each[gr] = sum_xor32(t) * 0x1p6f;
+        }
+        sum = h == 0 ? each[0] : each[1];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            f16x8 part[1];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[s][e] = ldexpf(x[s][e], 15 - exponent);
+            split_operand<1>(part, x[s]);
+            q[s] = part[0];
+        }
+    }
+};
+
+// Token (of 32) in row i of a score product.
+__device__ __forceinline__ int token_of(int i) {
+    return (i & 0x13) | (i & 4) << 1 | (i & 8) >> 1;
+}
+
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8)))
+void kv4_many(ManyArgs a) {
+    constexpr int NG = Kv4Dim<D>::kGroups, NS = D / 16, NB = D / 32, KR = D / 8;
+    constexpr int T = 64 * WAVES, WORDS = kTokens * D / 8;
+    constexpr int N = WORDS / T < 1 ? 1 : WORDS / T;   // words a thread unpacks
+    __shared__ __attribute__((aligned(16))) f16x8 Ks[2][kTokens * KR];
+    __shared__ __attribute__((aligned(16))) f16x8 Vs[2][D * 8];
+    __shared__ __attribute__((aligned(16))) float Ksc[4][NG][kTokens];
+    __shared__ float Kmn[4][2][kTokens];
+    __shared__ __attribute__((aligned(16))) _Float16 Vsc[4][NG][kTokens], Vmn[4][NG][kTokens];
+    __shared__ uint64_t Bad[4][NG];   // tokens whose V is not finite
+    __shared__ int Es[4];
+
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int share = blockIdx.x / a.row_tiles;
+    // causal: the tiles of the last rows, which see the most, first
+    const int tile_at = blockIdx.x - share * a.row_tiles;
+    const int tile = a.causal ? a.row_tiles - 1 - tile_at : tile_at;
+    const int bh = share / a.splits, split = share - bh * a.splits;
+    const int rows = a.G * a.Lq;
+    const Kv4Mask mask = sequence_mask(a.key_len, a.q_len, bh / a.H, a.L, a.Lq, a.causal);
+
+    const int r0 = 32 * (WAVES * tile + w), r = r0 + c;
+    const bool in = r < rows;
+    const int rr = in ? r : rows - 1, i = rr / a.G;
+    const size_t at = ((size_t)bh * a.G + (rr - i * a.G)) * a.Lq + i;
+    const int limit = mask.limit(i);
+    // tokens that some row of the workgroup, some row of the wave, every row
+    // of the wave sees
+    const int wg0 = 32 * WAVES * tile;
+    const int end = wg0 / a.G < mask.rows
+        ? max(mask.limit(min((min(rows, wg0 + 32 * WAVES) - 1) / a.G, mask.rows - 1)), 0) : 0;
+    const int wave_end = r0 < rows && r0 / a.G < mask.rows
+        ? max(mask.limit(min((min(rows, r0 + 32) - 1) / a.G, mask.rows - 1)), 0) : 0;
+    const int wave_all = r0 < rows ? mask.limit(r0 / a.G) : 0;
+
+    const int tiles = (end + kTokens - 1) / kTokens, each = (tiles + a.splits - 1) / a.splits;
+    const int begin = split * each, stop = min(tiles, begin + each);
+
+    const size_t head = (size_t)bh * a.Lp;
+    const uint32_t *kw = a.kw + head * KR, *vw = a.vw + head / 8 * D;
+    const uint32_t *kp = a.kp + head * NG, *vp = a.vp + head * NG;
+
+    // ---- bringing tiles in
+    typedef uint32_t words __attribute__((ext_vector_type(N)));
+    const bool brings = WORDS >= T * N || tid * N < WORDS;
+    const int ktok = tid * N / KR, kat = tid * N % KR;     // K: token, first word
+    const int voct = tid * N / D, vat = tid * N % D;       // V: octet, first word
+    words kraw, vraw;
+    uint32_t params[NG];   // wave 0: K's, wave 1: V's, of token `lane`
+    auto load_words = [&](int t) {
+        if (!brings) return;
+        // past the padded end (which no row sees) the last block again
+        const int k = min(kTokens * t + ktok, a.Lp - 1);
+        const int o = min(8 * t + voct, a.Lp / 8 - 1);
+        kraw = *reinterpret_cast<const words *>(kw + (size_t)k * KR + kat);
+        vraw = *reinterpret_cast<const words *>(vw + (size_t)o * D + vat);
+    };
+    auto load_params = [&](int t) {
+        const int k = kTokens * t + lane;
+        const uint32_t *p = w == 0 ? kp : vp;
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+            params[g] = w < 2 && k < mask.n ? p[(size_t)k * NG + g] : 0u;
+    };
+    int bound = -kManyExp;   // E, in wave 1
+    auto put_params = [&](int t) {
+        const int b = t & 3;
+        if (w == 0) {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                Ksc[b][g][lane] = group_scale(params[g]);
+                Kmn[b][g][lane] = group_min(params[g]);
+            }
+            if (NG == 1) Kmn[b][1][lane] = 0.f;
+        } else if (w == 1) {
+            float most = 0.f;
+            bool good[NG];
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const float sc = group_scale(params[g]), mn = group_min(params[g]);
+                const float v = fmaxf(fabsf(mn), fabsf(fmaf(15.f, sc, mn)));
+                good[g] = v < INFINITY;
+                most = fmaxf(most, good[g] ? v : 0.f);
+                const uint64_t bad = __ballot(!good[g]);
+                if (lane == 0) Bad[b][g] = bad;
+            }
+            for (int m = 1; m < 64; m *= 2) most = fmaxf(most, xor_lanes(most, m));
+            bound = max(bound, min(kManyExp, __builtin_amdgcn_frexp_expf(most)));
+            if (lane == 0) Es[b] = bound;
+            // in the octet's slot order
+            const int slot = (lane & 0x38) | (lane & 1) << 2 | (lane & 6) >> 1;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                Vsc[b][g][slot] = (_Float16)(good[g] ? ldexpf(group_scale(params[g]), 15 - bound)
+                                                     : 0.f);
+                Vmn[b][g][slot] = (_Float16)(good[g] ? ldexpf(group_min(params[g]), 15 - bound)
+                                                     : 0.f);
+            }
+        }
+    };
+    auto put_words = [&](int t) {
+        if (!brings) return;
+        const int b = t & 1;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int at_ = kat + n;   // g * (D/32) + s holds channels 8 (4s + g)
+            const int p = 4 * (at_ % (D / 32)) + at_ / (D / 32);
+            Ks[b][piece<KR>(ktok, p)] = code_operand(N == 1 ? kraw[0] : kraw[n]);
+        }
+        constexpr int W = Kv4Dim<D>::kWide;
+        const int g = NG == 1 ? 0 : vat / 64;
+        const f16x8 sc = *reinterpret_cast<const f16x8 *>(&Vsc[t & 3][g][8 * voct]);
+        const f16x8 mn = *reinterpret_cast<const f16x8 *>(&Vmn[t & 3][g][8 * voct]);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int q = vat + n;
+            const int d = 16 * (W * (q / (16 * W)) + q % W) + q / W % 16;
+            Vs[b][piece<8>(d, voct)] =
+                __builtin_elementwise_fma(code_operand<512>(N == 1 ? vraw[0] : vraw[n]), sc, mn);
+        }
+    };
+
+    Query32<D> q;
+    q.load(a.Q + at * D, in, h);
+    const float factor = row_factor(a.scale_log2, q.exponent);
+    float m = -INFINITY, l = 0.f;
+    int E = -kManyExp;
+    f32x16 o[NB];   // O^T[32 b + 8 (v/4) + 4h + v%4][row c] 2^(kLift + 15 - E)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) o[b] = zero16();
+
+    auto compute = [&](int t) {
+        const int buf = t & 1, pb = t & 3;
+        f32x16 s[2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const int tok = 32 * kb + token_of(c);
+            f32x16 part[NG];
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                part[g] = zero16();
+#pragma unroll
+                for (int st = g * (NS / NG); st < (g + 1) * (NS / NG); ++st)
+                    part[g] = mfma32x32x16f16(Ks[buf][piece<KR>(tok, 2 * st + h)], q.q[st],
+                                              part[g]);
+            }
+            s[kb] = mfma32x32x2(Kmn[pb][h][tok], q.sum, zero16());
+            // register v is token 8 (2 (v/8) + h) + v%8 of the block
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const f32x4 sc = *reinterpret_cast<const f32x4 *>(
+                        &Ksc[pb][g][32 * kb + 16 * (u >> 1) + 8 * h + 4 * (u & 1)]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        s[kb][4 * u + k] = fmaf(part[g][4 * u + k], sc[k], s[kb][4 * u + k]);
+                }
+            s[kb] *= factor;
+        }
+        if (kTokens * (t + 1) > wave_all) {
+            const int left = limit - kTokens * t - 8 * h;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (32 * kb + 16 * (v >> 3) + (v & 7) >= left) s[kb][v] = -INFINITY;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int v = 0; v < 16; v += 2) mx = max3_f32(mx, s[kb][v], s[kb][v + 1]);
+        mx = max_xor32(mx);
+        const int e_new = __builtin_amdgcn_readfirstlane(Es[pb]);
+        if (__any(mx > m + kManySlack) || e_new != E) {
+            const float m_new = fmaxf(m, ceilf(mx));
+            const float alpha = m_new == -INFINITY ? 1.f : exp2_fast(m - m_new);
+            l *= alpha;
+            const float both = ldexpf(alpha, E - e_new);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) o[b] *= both;
+            m = m_new;
+            E = e_new;
+        }
+        const float off = (m == -INFINITY ? 0.f : m) - (float)kLift;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                f16x8 p;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float x = exp2_fast(s[kb][8 * st + slot_value(k)] - off);
+                    l += x;
+                    p[k] = (_Float16)x;
+                }
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+                    o[b] = mfma32x32x16f16(Vs[buf][piece<8>(32 * b + c, 4 * kb + 2 * st + h)], p,
+                                           o[b]);
+            }
+        // a V that is not finite reaches the rows that see its token
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            const uint64_t bad = Bad[pb][g];
+            if (bad != 0) {
+                const int seen = min(max(limit - kTokens * t, 0), kTokens);
+                const uint64_t visible = seen == 64 ? ~0ull : (1ull << seen) - 1;
+                if (bad & visible) {
+#pragma unroll
+                    for (int b = g * (NB / NG); b < (g + 1) * (NB / NG); ++b)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) o[b][v] = __builtin_nanf("");
+                }
+            }
+        }
+    };
+
+    if (begin < stop) {
+        load_params(begin);
+        load_words(begin);
+        put_params(begin);
+        load_params(begin + 1);
+        __syncthreads();
+        put_words(begin);
+        put_params(begin + 1);
+        load_words(begin + 1);
+        load_params(begin + 2);
+        __syncthreads();
+        for (int t = begin; t < stop; ++t) {
+            if (wave_end > kTokens * t) compute(t);
+            // tile t + 1 into the other buffer, whose tile t - 1 all waves are
+            // done with; its parameters came an iteration ago
+            put_words(t + 1);
+            put_params(t + 2);
+            load_words(t + 2);
+            load_params(t + 3);
+            __syncthreads();
+        }
+    }
+
+    l = sum_xor32(l);
+    if (!in) return;
+    const bool valid = i < mask.rows;
+    if (a.splits > 1) {
+        const size_t slot = ((size_t)bh * a.splits + split) * rows + r;
+        float *to = a.part + slot * D;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                f32x4 x;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    x[k] = valid ? ldexpf(o[b][4 * u + k], E - 15 - kLift) : 0.f;
+                *reinterpret_cast<f32x4 *>(to + 32 * b + 8 * u + 4 * h) = x;
+            }
+        if (h == 0) {
+            a.stat[2 * slot] = valid ? m : -INFINITY;
+            a.stat[2 * slot + 1] = valid ? ldexpf(l, -kLift) : 0.f;
+        }
+        return;
+    }
+    if (!valid) l = 0.f;
+    const float inv = l == 0.f ? 0.f : ldexpf(1.f / l, E - 15);
+    uint16_t *to = a.O + at * D;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            uint16_t x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                x[k] = f32_to_bf16_rne(l == 0.f ? 0.f : o[b][4 * u + k] * inv);
+            *reinterpret_cast<u32x2 *>(to + 32 * b + 8 * u + 4 * h) =
+                u32x2{x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16};
+        }
+    if (h == 0) a.LSE[at] = l != l ? l : row_lse(m, ldexpf(l, -kLift));
+}
+
+template <int D, int WAVES>
+hipError_t many(const Kv4Attn &p, const Kv4Plan &plan, const void *Q,
+                const Kv4Cache<const uint32_t> &c, void *O, float *LSE, char *ws, hipStream_t s) {
+    const int tiles = (int)((kv4_rows(p) + 32 * WAVES - 1) / (32 * WAVES));
+    const ManyArgs a = {static_cast<const uint16_t *>(Q), c.k, c.v, c.kp, c.vp,
+                        static_cast<uint16_t *>(O), LSE, (float *)(ws + plan.part),
+                        (float *)(ws + plan.stat), p.key_len, p.q_len, p.H, p.G, p.Lq, p.L,
+                        kv4_padded(p.L), p.causal, p.scale * kLog2e, plan.splits, tiles};
+    kv4_many<D, WAVES><<<(unsigned)((int64_t)p.B * p.H * plan.splits * tiles), 64 * WAVES, 0, s>>>(
+        a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv4_many(const Kv4Attn &p, const Kv4Plan &plan, const void *Q,
+                           const Kv4Cache<const uint32_t> &c, void *O, float *LSE, void *ws,
+                           hipStream_t s) {
+    char *w = static_cast<char *>(ws);
+    if (plan.rows == 256)
+        return p.d == 32 ? many<32, 8>(p, plan, Q, c, O, LSE, w, s)
+             : p.d == 64 ? many<64, 8>(p, plan, Q, c, O, LSE, w, s)
+                         : many<128, 8>(p, plan, Q, c, O, LSE, w, s);
+    return p.d == 32 ? many<32, 4>(p, plan, Q, c, O, LSE, w, s)
+         : p.d == 64 ? many<64, 4>(p, plan, Q, c, O, LSE, w, s)
+                     : many<128, 4>(p, plan, Q, c, O, LSE, w, s);
+}
+
+}  // namespace mg

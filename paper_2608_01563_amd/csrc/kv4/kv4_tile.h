@@ -28,12 +28,13 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ constexpr int slot_value(int k) { return k < 4 ? 2 * k : 2 * k - 7; }
 constexpr float kCodeUnit = 0x1p9f;   // an operand is a code over this
 
+template <int TIMES = 1>   // 512: the codes themselves
 __device__ __forceinline__ f16x8 code_operand(uint32_t w) {
     const uint32_t even = w & 0x0f0f0f0fu, odd = (w >> 4) & 0x0f0f0f0fu;
-    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(even, 1.f, false);
-    const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(even, 1.f, true);
-    const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(odd, 1.f, false);
-    const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(odd, 1.f, true);
+    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(even, TIMES, false);
+    const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(even, TIMES, true);
+    const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(odd, TIMES, false);
+    const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(odd, TIMES, true);
     return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 

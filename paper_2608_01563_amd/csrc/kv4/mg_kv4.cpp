@@ -16,12 +16,13 @@ namespace mg {
 // unit, while each of a workgroup's four waves still has two blocks of 32
 // tokens when the cache is full.
 Kv4Plan kv4_plan(const Kv4Attn &p, bool weights, bool bf16) {
-    (void)bf16;
     const int64_t heads = (int64_t)p.B * p.H, rows = kv4_rows(p);
-    const int64_t tiles = heads * ((rows + 15) / 16);
-    const int64_t most = std::max<int64_t>(1, kv4_padded(p.L) / 32 / 8);
     Kv4Plan plan = {};
-    plan.splits = (int)std::min<int64_t>((512 + tiles - 1) / tiles, most);
+    plan.rows = !bf16 || rows < 64 ? 16 : heads * ((rows + 255) / 256) >= 256 ? 256 : 128;
+    const int64_t tiles = heads * ((rows + plan.rows - 1) / plan.rows);
+    const int64_t most = std::max<int64_t>(1, kv4_padded(p.L) / 32 / 8);
+    const int64_t want = plan.rows == 16 ? 512 : 512;
+    plan.splits = (int)std::min<int64_t>((want + tiles - 1) / tiles, most);
     plan.scores = weights && rows <= 16;
     if (plan.splits > 1) {
         plan.part = plan.bytes;
@@ -166,9 +167,14 @@ mg_status_t mg_attn_fwd_kv4(const void *Q, const void *cache, void *O, float *LS
     if (plan.bytes > 0) MG_TRY(mg::host::check_device_ptrs({{workspace, "workspace"}}, 16));
     MG_TRY(check_arrays({{weight, "weight"}, {key_len, "key_len"}, {q_len, "q_len"}}));
     const auto c = mg::kv4_cache<const uint32_t>(cache, B, H, L, d);
-    MG_TRY(run_kernel("kv4_rows", stream, [&] {
-        return mg::launch_kv4_rows(p, plan, Q, bf16, c, O, LSE, workspace, stream);
-    }));
+    if (plan.rows > 16)
+        MG_TRY(run_kernel("kv4_many", stream, [&] {
+            return mg::launch_kv4_many(p, plan, Q, c, O, LSE, workspace, stream);
+        }));
+    else
+        MG_TRY(run_kernel("kv4_rows", stream, [&] {
+            return mg::launch_kv4_rows(p, plan, Q, bf16, c, O, LSE, workspace, stream);
+        }));
     if (plan.splits > 1 || plan.scores)
         MG_TRY(run_kernel("kv4_join", stream, [&] {
             return mg::launch_kv4_join(p, plan, bf16, O, LSE, weight, workspace, stream);

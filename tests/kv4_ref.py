@@ -142,7 +142,7 @@ def evict(weight, n, keep, recent):
                            np.arange(n - recent, n)]).astype(int)
 
 
-def attention(q, code, group, n, rows, causal, scale, strict):
+def attention(q, code, group, n, rows, causal, scale, strict, many=False):
     """One query head's O, LSE, P over one cache head in 64 bits, and bounds on
     what a kernel may be off by: (O, LSE, P, tol_O, tol_LSE, tol_P).
 
@@ -151,7 +151,9 @@ def attention(q, code, group, n, rows, causal, scale, strict):
     sum of magnitudes.  p is off relatively by what the score is, plus the
     exponential's two ulps and the score's own rounding.  In O each p * scale
     is rounded once to f16 (strict: within 2^-23), n terms are summed in f32
-    and the result is rounded to its type."""
+    and the result is rounded to its type.  With many bf16 rows a head p and v
+    are rounded to f16 each, v in units that leave an error of 2^-34 of the
+    largest v at worst."""
     Lq, d = q.shape
     (kc, vc), ((ks, km), (vs, vm)) = code, group
     f32 = HALF_STEP["f32"]
@@ -181,8 +183,9 @@ def attention(q, code, group, n, rows, causal, scale, strict):
         P[r, at] = p
         O[r] = p @ v[at]
         out = f32 if strict else HALF_STEP["bf16"]
-        part = 2.0 ** -22 if strict else HALF_STEP["f16"]
-        tO[r] = out * np.abs(O[r]) + (part + rel + (len(at) + 8) * f32) * (p @ vv[at])
+        part = 2.0 ** -22 if strict else HALF_STEP["f16"] * (2 if many else 1)
+        tO[r] = out * np.abs(O[r]) + (part + rel + (len(at) + 8) * f32) * (p @ vv[at]) \
+            + (2.0 ** -34 * vv.max() if many else 0)
         tL[r] = rel + 4 * f32 * abs(LSE[r])
         tP[r, at] = 2 * rel * p + 1e-30
     return O, LSE, P, tO, tL, tP

@@ -141,6 +141,13 @@ ATTN = [
     (2, 8, 8, 1, 2000, 64, [2000, 77], None, True),     # split over workgroups
     (1, 8, 2, 2, 5000, 128, [4999], None, True),
     (1, 16, 1, 17, 600, 64, None, [11], True),
+    (2, 4, 1, 16, 97, 64, [97, 0], None, True),         # many rows: short, and none at all
+    (1, 8, 1, 70, 31, 128, None, [64], False),
+    (2, 3, 1, 100, 1000, 32, [1000, 65], [100, 1], True),
+    (1, 4, 2, 300, 640, 128, [639], [299], True),
+    (1, 1, 1, 64, 6000, 64, [5990], None, True),        # split over workgroups
+    (32, 8, 8, 257, 257, 32, None, None, True),         # the larger workgroups
+    (32, 8, 8, 300, 64, 128, None, None, False),
 ]
 
 
@@ -156,7 +163,8 @@ def reference(c, Q, kl, ql, G, causal, scale, strict):
         for hq in range(Hq):
             h = hq // G
             out = ref.attention(Q[b, hq].astype(np.float64), [x[b, h] for x in c.code],
-                                [(s[b, h], m[b, h]) for s, m in grp], n, r, causal, scale, strict)
+                                [(s[b, h], m[b, h]) for s, m in grp], n, r, causal, scale, strict,
+                                not strict and G * Lq >= 64)
             O[b, hq], LSE[b, hq], P, tO[b, hq], tL[b, hq], tP = out
             W[b, h, :n] += P.sum(0)
             tW[b, h, :n] += tP.sum(0)
@@ -231,7 +239,7 @@ def test_attention_over_a_wide_range(gpu_lib, contract):
 
 
 @pytest.mark.parametrize("contract", ["fast_bf16", "strict_f32"])
-@pytest.mark.parametrize("Lq", [1, 40])
+@pytest.mark.parametrize("Lq", [1, 20, 40])
 def test_attention_not_a_number(gpu_lib, contract, Lq):
     """A NaN token reaches the rows that see it, and its own group's channels of
     O if only its V is NaN; rows that do not see it are as without it."""
