@@ -109,8 +109,9 @@ mg_status_t mg_attn_fwd_kv4(const void *Q, const void *cache, void *O, float *LS
 
 /*
  * Bytes of workspace for it: partial outputs of the key splits that small
- * grids are cut into and, when weights are gathered for at most 16 rows a
- * cache head (Hq/H * Lq), their scores.  0 also for invalid arguments.
+ * grids are cut into and, when weights are gathered, for at most 16 rows a
+ * cache head (Hq/H * Lq) their scores, for more the sums of the shares that
+ * their rows are cut into.  0 also for invalid arguments.
  */
 size_t mg_attn_fwd_kv4_workspace_bytes(int B, int Hq, int H, int Lq, int L, int d, int weights,
                                        mg_contract_t contract);

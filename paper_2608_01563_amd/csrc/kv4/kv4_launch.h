@@ -32,7 +32,8 @@ struct Kv4Plan {
     int rows;          // of a workgroup: 16 (kv4_rows), 128 or 256 (kv4_many)
     int splits;        // workgroups that share a row tile's keys
     bool scores;       // weights come from scores the forward keeps
-    size_t part, stat, score, bytes;   // workspace: offsets of the parts, size
+    int shares;        // of the rows, where weights come from Q, K and LSE (else 0)
+    size_t part, stat, score, sums, bytes;   // workspace: offsets of the parts, size
 };
 Kv4Plan kv4_plan(const Kv4Attn &p, bool weights, bool bf16);
 
@@ -46,10 +47,13 @@ hipError_t launch_kv4_many(const Kv4Attn &p, const Kv4Plan &plan, const void *Q,
 // weights, whichever of the two there is.
 hipError_t launch_kv4_join(const Kv4Attn &p, const Kv4Plan &plan, bool bf16, void *O, float *LSE,
                            float *weight, const void *ws, hipStream_t s);
-// Adds every row's probabilities to the weights from Q, K and LSE.
-hipError_t launch_kv4_weights(const Kv4Attn &p, const void *Q, bool bf16,
+// Every row's probabilities from Q, K and LSE, added to the weights or, with
+// several shares, kept for launch_kv4_weight_shares to add.
+hipError_t launch_kv4_weights(const Kv4Attn &p, const Kv4Plan &plan, const void *Q, bool bf16,
                               const Kv4Cache<const uint32_t> &c, const float *LSE, float *weight,
-                              hipStream_t s);
+                              void *ws, hipStream_t s);
+hipError_t launch_kv4_weight_shares(const Kv4Attn &p, const Kv4Plan &plan, float *weight,
+                                    const void *ws, hipStream_t s);
 
 struct Kv4Evict {
     int B, H, L, d, keep, recent;

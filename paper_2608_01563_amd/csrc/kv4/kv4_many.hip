@@ -28,23 +28,6 @@ constexpr float kManySlack = 4.f;
 constexpr int kLift = 11;      // P is at most 2^(slack + kLift) = 2^15
 constexpr int kManyExp = 100;  // bound on E
 
-typedef _Float16 f16x2v __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ f32x16 mfma32x32x16f16(f16x8 a, f16x8 b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x16 mfma32x32x2(float a, float b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
-}
-
-// 16-byte pieces of LDS rows of N pieces, permuted so that 16 rows read at the
-// same piece, or a row's pieces, fall on different banks.
-template <int N>
-__device__ __forceinline__ int piece(int row, int p) {
-    constexpr int ROWS = 16 / N < 1 ? 1 : 16 / N;   // rows that share 256 bytes
-    return row * N + (p ^ ((row / ROWS) & (N - 1)));
-}
-
 struct ManyArgs {
     const uint16_t *Q;
     const uint32_t *kw, *vw, *kp, *vp;
@@ -101,11 +84,6 @@ struct Query32 {
         }
     }
 };
-
-// Token (of 32) in row i of a score product.
-__device__ __forceinline__ int token_of(int i) {
-    return (i & 0x13) | (i & 4) << 1 | (i & 8) >> 1;
-}
 
 template <int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8)))

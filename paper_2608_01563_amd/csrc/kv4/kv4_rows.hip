@@ -382,68 +382,6 @@ void kv4_join(JoinArgs a) {
         if (j0 + k < mask.n) to[k] += w[k];
 }
 
-// ------------------------------------------------- weights from Q, K and LSE --
-struct WeightArgs {
-    const void *Q;
-    const uint32_t *kw, *kp;
-    const float *LSE;
-    float *weight;
-    const int32_t *key_len, *q_len;
-    int H, G, Lq, L, Lp, causal, groups;   // workgroups a head
-    float scale_log2;
-};
-
-// A wave keeps 32 tokens' codes and goes through the rows that see them.
-template <typename T, int D, int NP>
-__global__ __launch_bounds__(kThreads)
-void kv4_weights(WeightArgs a) {
-    constexpr int NG = Kv4Dim<D>::kGroups;
-    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-    const int bh = blockIdx.x / a.groups;
-    const int block = (blockIdx.x - bh * a.groups) * kWaves + (threadIdx.x >> 6);
-    const Kv4Mask mask = sequence_mask(a.key_len, a.q_len, bh / a.H, a.L, a.Lq, a.causal);
-    if (32 * block >= mask.n) return;
-
-    const size_t head = (size_t)bh * a.Lp;
-    Kv4Keys<D> key;
-    key.load(a.kw + head * (D / 8), a.kp + head * NG, block, c, g);
-
-    float sum[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) sum[k] = 0.f;
-    const int rows = mask.rows * a.G;
-    const int first_i = a.causal ? max(0, 32 * block - (mask.n - mask.rows)) : 0;
-    for (int r0 = first_i * a.G / kRows * kRows; r0 < rows; r0 += kRows) {
-        const int r = r0 + c;
-        const bool in = r < rows;
-        const RowAt at = row_at(in ? r : 0, bh, a.G, a.Lq);
-        Kv4Query<D, NP> q;
-        q.load(static_cast<const T *>(a.Q) + at.at * D, in, g);
-        const float lse = a.LSE[at.at];
-        const float factor = row_factor(a.scale_log2, q.exponent), off = lse * kLog2e;
-        // nothing from rows without sight (LSE -inf)
-        const int limit = in && lse != -INFINITY ? mask.limit(at.i) : 0;
-        f32x4 s[2];
-        key.scores(s, q);
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (32 * block + 8 * g + k < limit)
-                sum[k] += exp2_fast(fmaf(s[k >> 2][k & 3], factor, -off));
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-#pragma unroll
-        for (int m = 1; m < 16; m *= 2) sum[k] += xor_lanes(sum[k], m);
-    float *to = a.weight + (size_t)bh * a.L;
-    if (c < 8) {
-        float mine = 0.f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) mine = c == k ? sum[k] : mine;
-        const int j = 32 * block + 8 * g + c;
-        if (j < mask.n) to[j] += mine;
-    }
-}
-
 template <typename T, int D, int NP>
 hipError_t rows(const Kv4Attn &p, const Kv4Plan &plan, const void *Q,
                 const Kv4Cache<const uint32_t> &c, void *O, float *LSE, char *ws, hipStream_t s) {
@@ -468,16 +406,6 @@ hipError_t join(const Kv4Attn &p, const Kv4Plan &plan, void *O, float *LSE, floa
                         p.key_len, p.q_len, p.H, p.G, p.Lq, p.L, kv4_padded(p.L), p.causal,
                         plan.splits, (int)heads, (int)outs};
     kv4_join<T, D><<<(unsigned)(outs + keys), kThreads, 0, s>>>(a);
-    return hipGetLastError();
-}
-
-template <typename T, int D, int NP>
-hipError_t weights(const Kv4Attn &p, const void *Q, const Kv4Cache<const uint32_t> &c,
-                   const float *LSE, float *weight, hipStream_t s) {
-    const int groups = cdiv(kv4_padded(p.L) / 32, kWaves);
-    const WeightArgs a = {Q, c.k, c.kp, LSE, weight, p.key_len, p.q_len, p.H, p.G, p.Lq, p.L,
-                          kv4_padded(p.L), p.causal, groups, p.scale * kLog2e};
-    kv4_weights<T, D, NP><<<(unsigned)((int64_t)p.B * p.H * groups), kThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -506,18 +434,6 @@ hipError_t launch_kv4_join(const Kv4Attn &p, const Kv4Plan &plan, bool bf16, voi
     return p.d == 32 ? join<float, 32>(p, plan, O, LSE, weight, w, s)
          : p.d == 64 ? join<float, 64>(p, plan, O, LSE, weight, w, s)
                      : join<float, 128>(p, plan, O, LSE, weight, w, s);
-}
-
-hipError_t launch_kv4_weights(const Kv4Attn &p, const void *Q, bool bf16,
-                              const Kv4Cache<const uint32_t> &c, const float *LSE, float *weight,
-                              hipStream_t s) {
-    if (bf16)
-        return p.d == 32 ? weights<uint16_t, 32, 1>(p, Q, c, LSE, weight, s)
-             : p.d == 64 ? weights<uint16_t, 64, 1>(p, Q, c, LSE, weight, s)
-                         : weights<uint16_t, 128, 1>(p, Q, c, LSE, weight, s);
-    return p.d == 32 ? weights<float, 32, 2>(p, Q, c, LSE, weight, s)
-         : p.d == 64 ? weights<float, 64, 2>(p, Q, c, LSE, weight, s)
-                     : weights<float, 128, 2>(p, Q, c, LSE, weight, s);
 }
 
 }  // namespace mg

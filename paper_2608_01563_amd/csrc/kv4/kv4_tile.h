@@ -175,4 +175,25 @@ __device__ __forceinline__ Kv4Mask sequence_mask(const int32_t *key_len, const i
     return {optional_len(key_len, b, L), optional_len(q_len, b, Lq), causal};
 }
 
+// ---- 32x32x16 products (many rows)
+__device__ __forceinline__ f32x16 mfma32x32x16f16(f16x8 a, f16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma32x32x2(float a, float b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+}
+
+// 16-byte pieces of LDS rows of N pieces, permuted so that 16 rows read at the
+// same piece, or a row's pieces, fall on different banks.
+template <int N>
+__device__ __forceinline__ int piece(int row, int p) {
+    constexpr int ROWS = 16 / N < 1 ? 1 : 16 / N;   // rows that share 256 bytes
+    return row * N + (p ^ ((row / ROWS) & (N - 1)));
+}
+
+// Token (of 32) in row i of a score product.
+__device__ __forceinline__ int token_of(int i) {
+    return (i & 0x13) | (i & 4) << 1 | (i & 8) >> 1;
+}
+
 }  // namespace mg

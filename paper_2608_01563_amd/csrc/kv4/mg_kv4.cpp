@@ -34,6 +34,17 @@ Kv4Plan kv4_plan(const Kv4Attn &p, bool weights, bool bf16) {
         plan.score = plan.bytes;
         plan.bytes += host::round256((size_t)(heads * rows) * kv4_padded(p.L) * 4);
     }
+    if (weights && !plan.scores) {
+        // enough workgroups of 256 tokens for two on every compute unit, with at
+        // least eight blocks of 32 rows each
+        const int64_t groups = heads * cdiv(p.L, 256);
+        plan.shares = (int)std::min<int64_t>((512 + groups - 1) / groups,
+                                             std::max<int64_t>(1, rows / 256));
+        if (plan.shares > 1) {
+            plan.sums = plan.bytes;
+            plan.bytes += host::round256((size_t)plan.shares * heads * kv4_padded(p.L) * 4);
+        }
+    }
     return plan;
 }
 
@@ -179,9 +190,13 @@ mg_status_t mg_attn_fwd_kv4(const void *Q, const void *cache, void *O, float *LS
         MG_TRY(run_kernel("kv4_join", stream, [&] {
             return mg::launch_kv4_join(p, plan, bf16, O, LSE, weight, workspace, stream);
         }));
-    if (weight != nullptr && !plan.scores)
+    if (plan.shares > 0)
         MG_TRY(run_kernel("kv4_weights", stream, [&] {
-            return mg::launch_kv4_weights(p, Q, bf16, c, LSE, weight, stream);
+            return mg::launch_kv4_weights(p, plan, Q, bf16, c, LSE, weight, workspace, stream);
+        }));
+    if (plan.shares > 1)
+        MG_TRY(run_kernel("kv4_weight_shares", stream, [&] {
+            return mg::launch_kv4_weight_shares(p, plan, weight, workspace, stream);
         }));
     return ok();
 }
