@@ -47,7 +47,7 @@ struct Query32 {
     float sum;      // of group l/32 (0 where there is no second)
     int exponent;
 
-    __device__ __forceinline__ void load(const uint16_t *row, bool valid, int h) {
+    __device__ __forceinline__ void load(const uint16_t *row, bool valid, int h, bool negate) {
         constexpr int NS = D / 16, NG = Kv4Dim<D>::kGroups;
         float x[NS][8];
         float top = 0.f;
@@ -60,7 +60,10 @@ struct Query32 {
                 for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[s][e]));
+            for (int e = 0; e < 8; ++e) {
+                top = fmaxf(top, fabsf(x[s][e]));
+                if (negate) x[s][e] = -x[s][e];
+            }
         }
         exponent = __builtin_amdgcn_frexp_expf(max_xor32(top));
         float each[2] = {0.f, 0.f};
@@ -91,8 +94,8 @@ void kv4_many(ManyArgs a) {
     constexpr int NG = Kv4Dim<D>::kGroups, NS = D / 16, NB = D / 32, KR = D / 8;
     constexpr int T = 64 * WAVES, WORDS = kTokens * D / 8;
     constexpr int N = WORDS / T < 1 ? 1 : WORDS / T;   // words a thread unpacks
-    __shared__ __attribute__((aligned(16))) f16x8 Ks[2][kTokens * KR];
-    __shared__ __attribute__((aligned(16))) f16x8 Vs[2][D * 8];
+    __shared__ __attribute__((aligned(16))) f16x8 Ks[2][kTokens * (KR + 1)];
+    __shared__ __attribute__((aligned(16))) f16x8 Vs[3][D * 9];
     __shared__ __attribute__((aligned(16))) float Ksc[4][NG][kTokens];
     __shared__ float Kmn[4][2][kTokens];
     __shared__ __attribute__((aligned(16))) _Float16 Vsc[4][NG][kTokens], Vmn[4][NG][kTokens];
@@ -188,7 +191,7 @@ void kv4_many(ManyArgs a) {
             }
         }
     };
-    auto put_words = [&](int t) {
+    auto put_words = [&](int t, int vb) {   // vb: V's buffer
         if (!brings) return;
         const int b = t & 1;
 #pragma unroll
@@ -205,64 +208,46 @@ void kv4_many(ManyArgs a) {
         for (int n = 0; n < N; ++n) {
             const int q = vat + n;
             const int d = 16 * (W * (q / (16 * W)) + q % W) + q / W % 16;
-            Vs[b][piece<8>(d, voct)] =
+            Vs[vb][piece<8>(d, voct)] =
                 __builtin_elementwise_fma(code_operand<512>(N == 1 ? vraw[0] : vraw[n]), sc, mn);
         }
     };
 
     Query32<D> q;
-    q.load(a.Q + at * D, in, h);
-    const float factor = row_factor(a.scale_log2, q.exponent);
+    q.load(a.Q + at * D, in, h, a.scale_log2 < 0.f);
+    const float factor = positive_factor(a.scale_log2, q.exponent);
     float m = -INFINITY, l = 0.f;
     int E = -kManyExp;
     f32x16 o[NB];   // O^T[32 b + 8 (v/4) + 4h + v%4][row c] 2^(kLift + 15 - E)
 #pragma unroll
     for (int b = 0; b < NB; ++b) o[b] = zero16();
 
-    auto compute = [&](int t) {
-        const int buf = t & 1, pb = t & 3;
-        f32x16 s[2];
+    // Scores over the row's factor of 32 tokens, register v being token
+    // 8 (2 (v/8) + h) + v%8 of the block; -inf where the row does not see it.
+    f32x16 part[NG], val;
+    auto key_at = [&](int t, int kb, int st) {
+        return Ks[t & 1][piece<KR>(32 * kb + token_of(c), 2 * st + h)];
+    };
+    auto scale_at = [&](int t, int kb, int g, int u) {
+        return *reinterpret_cast<const f32x4 *>(
+            &Ksc[t & 3][g][32 * kb + 16 * (u >> 1) + 8 * h + 4 * (u & 1)]);
+    };
+    auto low_at = [&](int t, int kb) { return Kmn[t & 3][h][32 * kb + token_of(c)]; };
+    auto hide = [&](int t, int kb) {
+        if (kTokens * t + 32 * (kb + 1) > wave_all) {
+            const int left = limit - kTokens * t - 32 * kb - 8 * h;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const int tok = 32 * kb + token_of(c);
-            f32x16 part[NG];
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                part[g] = zero16();
-#pragma unroll
-                for (int st = g * (NS / NG); st < (g + 1) * (NS / NG); ++st)
-                    part[g] = mfma32x32x16f16(Ks[buf][piece<KR>(tok, 2 * st + h)], q.q[st],
-                                              part[g]);
-            }
-            s[kb] = mfma32x32x2(Kmn[pb][h][tok], q.sum, zero16());
-            // register v is token 8 (2 (v/8) + h) + v%8 of the block
-#pragma unroll
-            for (int g = 0; g < NG; ++g)
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const f32x4 sc = *reinterpret_cast<const f32x4 *>(
-                        &Ksc[pb][g][32 * kb + 16 * (u >> 1) + 8 * h + 4 * (u & 1)]);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        s[kb][4 * u + k] = fmaf(part[g][4 * u + k], sc[k], s[kb][4 * u + k]);
-                }
-            s[kb] *= factor;
+            for (int v = 0; v < 16; ++v)
+                if (16 * (v >> 3) + (v & 7) >= left) val[v] = -INFINITY;
         }
-        if (kTokens * (t + 1) > wave_all) {
-            const int left = limit - kTokens * t - 8 * h;
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    if (32 * kb + 16 * (v >> 3) + (v & 7) >= left) s[kb][v] = -INFINITY;
-        }
+    };
+    // Running units that hold the block's scores and tile t's values.
+    auto settle = [&](int t) {
         float mx = -INFINITY;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int v = 0; v < 16; v += 2) mx = max3_f32(mx, s[kb][v], s[kb][v + 1]);
-        mx = max_xor32(mx);
-        const int e_new = __builtin_amdgcn_readfirstlane(Es[pb]);
+        for (int v = 0; v < 16; v += 2) mx = max3_f32(mx, val[v], val[v + 1]);
+        mx = max_xor32(mx) * factor;
+        const int e_new = __builtin_amdgcn_readfirstlane(Es[t & 3]);
         if (__any(mx > m + kManySlack) || e_new != E) {
             const float m_new = fmaxf(m, ceilf(mx));
             const float alpha = m_new == -INFINITY ? 1.f : exp2_fast(m - m_new);
@@ -273,27 +258,70 @@ void kv4_many(ManyArgs a) {
             m = m_new;
             E = e_new;
         }
-        const float off = (m == -INFINITY ? 0.f : m) - (float)kLift;
+    };
+    // One block: softmax and P V of the scores in `val` (block kb of tile t, V in
+    // buffer vb), and meanwhile the scores of the next one (kn of tile tn).
+    // The order is written out: operand reads AHEAD of the products that take
+    // them, the softmax between the score products, the sums of the new scores
+    // between P V's.  (Left to itself the compiler reads each operand right
+    // before its product: 757 against XXX us for 2,048 rows over 8,192 tokens.)
+    constexpr int AHEAD = NS < 4 ? NS : 4;
+    auto step = [&](int t, int kb, int vb, int tn, int kn) {
+        f16x8 reg[AHEAD];
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int k = 0; k < AHEAD; ++k) reg[k] = key_at(tn, kn, k);
+        const float low_next = low_at(tn, kn);
+        settle(t);
+        const float off = (float)kLift - (m == -INFINITY ? 0.f : m);
+        auto value_at = [&](int k) {   // product k of P V: tokens k / NB, channels k % NB
+            return Vs[vb][piece<8>(32 * (k % NB) + c, 4 * kb + 2 * (k / NB) + h)];
+        };
+        f16x8 p[2];
 #pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                f16x8 p;
+        for (int k = 0; k < NS; ++k) {
+            const int g = k / (NS / NG);
+            if (k % (NS / NG) == 0) part[g] = zero16();
+            part[g] = mfma32x32x16f16(reg[k % AHEAD], q.q[k], part[g]);
+            reg[k % AHEAD] = k + AHEAD < NS ? key_at(tn, kn, k + AHEAD) : value_at(k + AHEAD - NS);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float x = exp2_fast(s[kb][8 * st + slot_value(k)] - off);
-                    l += x;
-                    p[k] = (_Float16)x;
-                }
-#pragma unroll
-                for (int b = 0; b < NB; ++b)
-                    o[b] = mfma32x32x16f16(Vs[buf][piece<8>(32 * b + c, 4 * kb + 2 * st + h)], p,
-                                           o[b]);
+            for (int i = k * (16 / NS); i < (k + 1) * (16 / NS); ++i) {
+                const float x = exp2_fast(fmaf(val[(i & 8) + slot_value(i & 7)], factor, off));
+                l += x;
+                p[i >> 3][i & 7] = (_Float16)x;
             }
-        // a V that is not finite reaches the rows that see its token
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        constexpr int SUMS = 4 * NG / NS;   // a slice adds to 4 SUMS scores (one group)
+        f32x4 sc[SUMS], sc_next[SUMS];
+        val = mfma32x32x2(low_next, q.sum, zero16());
+#pragma unroll
+        for (int i = 0; i < SUMS; ++i) sc_next[i] = scale_at(tn, kn, i % NG, i / NG);
+#pragma unroll
+        for (int k = 0; k < NS; ++k) {
+            o[k % NB] = mfma32x32x16f16(reg[k % AHEAD], p[k / NB], o[k % NB]);
+#pragma unroll
+            for (int i = 0; i < SUMS; ++i) {
+                const int at_ = (k + 1) * SUMS + i;
+                sc[i] = sc_next[i];
+                if (k + 1 < NS) sc_next[i] = scale_at(tn, kn, at_ % NG, at_ / NG);
+            }
+            if (k + AHEAD < NS) reg[k % AHEAD] = value_at(k + AHEAD);
+#pragma unroll
+            for (int i = 0; i < SUMS; ++i) {
+                const int at_ = k * SUMS + i, g = at_ % NG, u = at_ / NG;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    val[4 * u + r] = fmaf(part[g][4 * u + r], sc[i][r], val[4 * u + r]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        hide(tn, kn);
+    };
+    // a V that is not finite reaches the rows that see its token
+    auto spread_bad = [&](int t) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            const uint64_t bad = Bad[pb][g];
+            const uint64_t bad = Bad[t & 3][g];
             if (bad != 0) {
                 const int seen = min(max(limit - kTokens * t, 0), kTokens);
                 const uint64_t visible = seen == 64 ? ~0ull : (1ull << seen) - 1;
@@ -313,20 +341,44 @@ void kv4_many(ManyArgs a) {
         put_params(begin);
         load_params(begin + 1);
         __syncthreads();
-        put_words(begin);
+        put_words(begin, 0);
         put_params(begin + 1);
         load_words(begin + 1);
         load_params(begin + 2);
         __syncthreads();
+        // the first block's scores
+#pragma unroll
+        for (int g = 0; g < NG; ++g) part[g] = zero16();
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+            part[k / (NS / NG)] = mfma32x32x16f16(key_at(begin, 0, k), q.q[k], part[k / (NS / NG)]);
+        val = mfma32x32x2(low_at(begin, 0), q.sum, zero16());
+#pragma unroll
+        for (int i = 0; i < 4 * NG; ++i) {
+            const f32x4 sc = scale_at(begin, 0, i % NG, i / NG);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                val[4 * (i / NG) + r] =
+                    fmaf(part[i % NG][4 * (i / NG) + r], sc[r], val[4 * (i / NG) + r]);
+        }
+        hide(begin, 0);
+        int vb = 0;
         for (int t = begin; t < stop; ++t) {
-            if (wave_end > kTokens * t) compute(t);
-            // tile t + 1 into the other buffer, whose tile t - 1 all waves are
-            // done with; its parameters came an iteration ago
-            put_words(t + 1);
+            const int next = vb == 2 ? 0 : vb + 1;
+            const bool works = wave_end > kTokens * t;
+            if (works) step(t, 0, vb, t, 1);
+            // tile t + 1 comes in: K over tile t - 1, which all waves are done
+            // with, V in a third buffer, as tile t - 1's may still be read
+            put_words(t + 1, next);
             put_params(t + 2);
             load_words(t + 2);
             load_params(t + 3);
             __syncthreads();
+            if (works) {
+                step(t, 1, vb, t + 1, 0);
+                spread_bad(t);
+            }
+            vb = next;
         }
     }
 

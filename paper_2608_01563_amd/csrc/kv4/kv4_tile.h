@@ -51,7 +51,7 @@ __device__ __forceinline__ void split_operand(f16x8 (&out)[NP], const float (&x)
         const float v = x[slot_value(k)];
         const _Float16 h = (_Float16)v;
         out[0][k] = h;
-        if (NP > 1) out[1][k] = (_Float16)(v - (float)h);
+        if constexpr (NP > 1) out[1][k] = (_Float16)(v - (float)h);
     }
 }
 
@@ -162,6 +162,12 @@ __device__ __forceinline__ float row_factor(float scale_log2, int exponent) {
     return ldexpf(scale_log2, exponent - 6);
 }
 
+// The same for a row whose negative scale went into Q, at least the smallest
+// normal: -inf times it stays -inf where the scale is 0.
+__device__ __forceinline__ float positive_factor(float scale_log2, int exponent) {
+    return fmaxf(row_factor(fabsf(scale_log2), exponent), 0x1p-126f);
+}
+
 // One sequence's lengths and mask: row i sees tokens below limit(i).
 struct Kv4Mask {
     int n, rows, causal;   // tokens, query rows
@@ -183,12 +189,12 @@ __device__ __forceinline__ f32x16 mfma32x32x2(float a, float b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
 }
 
-// 16-byte pieces of LDS rows of N pieces, permuted so that 16 rows read at the
-// same piece, or a row's pieces, fall on different banks.
+// 16-byte pieces of LDS rows of N (4, 8 or 16) pieces and one of padding: 16
+// rows read at the same piece fall on different banks, and a row's pieces are
+// at constant offsets.
 template <int N>
 __device__ __forceinline__ int piece(int row, int p) {
-    constexpr int ROWS = 16 / N < 1 ? 1 : 16 / N;   // rows that share 256 bytes
-    return row * N + (p ^ ((row / ROWS) & (N - 1)));
+    return row * (N + 1) + p;
 }
 
 // Token (of 32) in row i of a score product.

@@ -34,7 +34,7 @@ __global__ __launch_bounds__(kThreads)
 void kv4_weights(WeightArgs a) {
     constexpr int NG = Kv4Dim<D>::kGroups, NS = D / 16, KR = D / 8;
     constexpr int PER = KR;   // threads that prepare a row, 8 channels each
-    __shared__ __attribute__((aligned(16))) f16x8 Qs[2][NP][32 * KR];
+    __shared__ __attribute__((aligned(16))) f16x8 Qs[2][NP][32 * (KR + 1)];
     __shared__ float Sum[2][2][32], Factor[2][32], Lse[2][32];
     __shared__ int Limit[2][32];
 
