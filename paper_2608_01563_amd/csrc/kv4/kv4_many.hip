@@ -177,7 +177,7 @@ void kv4_many(ManyArgs a) {
                 const uint64_t bad = __ballot(!good[g]);
                 if (lane == 0) Bad[b][g] = bad;
             }
-            for (int m = 1; m < 64; m *= 2) most = fmaxf(most, xor_lanes(most, m));
+            most = max_of_wave(most);
             bound = max(bound, min(kManyExp, __builtin_amdgcn_frexp_expf(most)));
             if (lane == 0) Es[b] = bound;
             // in the octet's slot order
@@ -241,11 +241,8 @@ void kv4_many(ManyArgs a) {
                 if (16 * (v >> 3) + (v & 7) >= left) val[v] = -INFINITY;
         }
     };
-    // Running units that hold the block's scores and tile t's values.
-    auto settle = [&](int t) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int v = 0; v < 16; v += 2) mx = max3_f32(mx, val[v], val[v + 1]);
+    // Running units that hold scores up to mx and tile t's values.
+    auto settle = [&](int t, float mx) {
         mx = max_xor32(mx) * factor;
         const int e_new = __builtin_amdgcn_readfirstlane(Es[t & 3]);
         if (__any(mx > m + kManySlack) || e_new != E) {
@@ -267,51 +264,72 @@ void kv4_many(ManyArgs a) {
     // before its product: 757 against XXX us for 2,048 rows over 8,192 tokens.)
     constexpr int AHEAD = NS < 4 ? NS : 4;
     auto step = [&](int t, int kb, int vb, int tn, int kn) {
+        auto value_at = [&](int k) {   // product k of P V: tokens k / NB, channels k % NB
+            return Vs[vb][piece<8>(32 * (k % NB) + c, 4 * kb + 2 * (k / NB) + h)];
+        };
         f16x8 reg[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) reg[k] = key_at(tn, kn, k);
         const float low_next = low_at(tn, kn);
-        settle(t);
-        const float off = (float)kLift - (m == -INFINITY ? 0.f : m);
-        auto value_at = [&](int k) {   // product k of P V: tokens k / NB, channels k % NB
-            return Vs[vb][piece<8>(32 * (k % NB) + c, 4 * kb + 2 * (k / NB) + h)];
-        };
-        f16x8 p[2];
-#pragma unroll
-        for (int k = 0; k < NS; ++k) {
+        auto score_product = [&](int k) {
             const int g = k / (NS / NG);
             if (k % (NS / NG) == 0) part[g] = zero16();
             part[g] = mfma32x32x16f16(reg[k % AHEAD], q.q[k], part[g]);
             reg[k % AHEAD] = k + AHEAD < NS ? key_at(tn, kn, k + AHEAD) : value_at(k + AHEAD - NS);
+        };
+        // half of the score products hide the maximum ...
+        constexpr int HALF = NS / 2, EACH = 16 / HALF;
+        float mx = -INFINITY;
 #pragma unroll
-            for (int i = k * (16 / NS); i < (k + 1) * (16 / NS); ++i) {
-                const float x = exp2_fast(fmaf(val[(i & 8) + slot_value(i & 7)], factor, off));
-                l += x;
-                p[i >> 3][i & 7] = (_Float16)x;
+        for (int k = 0; k < HALF; ++k) {
+            score_product(k);
+#pragma unroll
+            for (int v = k * EACH; v < (k + 1) * EACH; v += 2) mx = max3_f32(mx, val[v], val[v + 1]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        settle(t, mx);
+        // ... the other half the exponentials
+        const float off = (float)kLift - (m == -INFINITY ? 0.f : m);
+        float x[16];
+        f16x8 p[2];
+#pragma unroll
+        for (int k = 0; k < HALF; ++k) {
+            score_product(HALF + k);
+#pragma unroll
+            for (int i = k * EACH; i < (k + 1) * EACH; ++i) {
+                x[i] = exp2_fast(fmaf(val[(i & 8) + slot_value(i & 7)], factor, off));
+                p[i >> 3][i & 7] = (_Float16)x[i];
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        constexpr int SUMS = 4 * NG / NS;   // a slice adds to 4 SUMS scores (one group)
-        f32x4 sc[SUMS], sc_next[SUMS];
+        // P V, and behind it first the row sums, then, from product FIRST on (the
+        // minima's product takes 64 clocks), the new scores, a group of four at a time
+        constexpr int SUMS = 4 * NG, FIRST = NS < 8 ? 1 : 2;
+        auto sums_before = [](int k) {   // of the SUMS, done before slice k
+            return k <= FIRST ? 0 : (k - FIRST) * SUMS / (NS - FIRST);
+        };
+        constexpr int MOST = (SUMS + NS - FIRST - 1) / (NS - FIRST);
+        f32x4 sc[MOST];
         val = mfma32x32x2(low_next, q.sum, zero16());
-#pragma unroll
-        for (int i = 0; i < SUMS; ++i) sc_next[i] = scale_at(tn, kn, i % NG, i / NG);
 #pragma unroll
         for (int k = 0; k < NS; ++k) {
             o[k % NB] = mfma32x32x16f16(reg[k % AHEAD], p[k / NB], o[k % NB]);
+            const int now = sums_before(k), next = sums_before(k + 1), after = sums_before(k + 2);
 #pragma unroll
-            for (int i = 0; i < SUMS; ++i) {
-                const int at_ = (k + 1) * SUMS + i;
-                sc[i] = sc_next[i];
-                if (k + 1 < NS) sc_next[i] = scale_at(tn, kn, at_ % NG, at_ / NG);
-            }
-            if (k + AHEAD < NS) reg[k % AHEAD] = value_at(k + AHEAD);
-#pragma unroll
-            for (int i = 0; i < SUMS; ++i) {
-                const int at_ = k * SUMS + i, g = at_ % NG, u = at_ / NG;
+            for (int i = now; i < next; ++i) {
+                const int g = i % NG, u = i / NG;
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    val[4 * u + r] = fmaf(part[g][4 * u + r], sc[i][r], val[4 * u + r]);
+                    val[4 * u + r] = fmaf(part[g][4 * u + r], sc[i - now][r], val[4 * u + r]);
+            }
+#pragma unroll
+            for (int i = next; i < (k + 1 < NS ? after : next); ++i)
+                sc[i - next] = scale_at(tn, kn, i % NG, i / NG);
+            if (k + AHEAD < NS) reg[k % AHEAD] = value_at(k + AHEAD);
+            if (k < FIRST) {
+#pragma unroll
+                for (int i = 4 * k; i < 16; i += 4 * FIRST)
+                    l += (x[i] + x[i + 1]) + (x[i + 2] + x[i + 3]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }

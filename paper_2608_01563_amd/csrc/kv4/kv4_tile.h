@@ -197,6 +197,17 @@ __device__ __forceinline__ int piece(int row, int p) {
     return row * (N + 1) + p;
 }
 
+// Maximum over the wave (rotations within its rows of 16, then swaps).
+template <int ROTATE>
+__device__ __forceinline__ float max_rotated(float v) {
+    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(
+                        0, __float_as_int(v), 0x120 + ROTATE, 0xf, 0xf, false)));
+}
+__device__ __forceinline__ float max_of_wave(float v) {
+    v = max_rotated<1>(max_rotated<2>(max_rotated<4>(max_rotated<8>(v))));
+    return max_xor32(max_xor16(v));
+}
+
 // Token (of 32) in row i of a score product.
 __device__ __forceinline__ int token_of(int i) {
     return (i & 0x13) | (i & 4) << 1 | (i & 8) >> 1;
