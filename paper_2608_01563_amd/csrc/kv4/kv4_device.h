@@ -38,6 +38,11 @@ __device__ __forceinline__ int optional_len(const int32_t *len, int b, int full)
 __device__ __forceinline__ float load_elem(const float *p) { return *p; }
 __device__ __forceinline__ float load_elem(const uint16_t *p) { return bf16_to_f32(*p); }
 
+// bf16 bits, nearest even (one conversion instruction for a pair).
+__device__ __forceinline__ uint16_t to_bf16(float x) {
+    return __builtin_bit_cast(uint16_t, (__bf16)x);
+}
+
 // N consecutive elements as f32, N * sizeof(T) a multiple of 8 bytes.
 template <int N>
 __device__ __forceinline__ void load_row(float (&x)[N], const float *p) {
@@ -77,8 +82,7 @@ __device__ __forceinline__ void store_row(uint16_t *p, const float (&x)[N]) {
         words v;
 #pragma unroll
         for (int k = 0; k < W / 2; ++k)
-            v[k] = (uint32_t)f32_to_bf16_rne(x[i + 2 * k]) |
-                   (uint32_t)f32_to_bf16_rne(x[i + 2 * k + 1]) << 16;
+            v[k] = to_bf16(x[i + 2 * k]) | (uint32_t)to_bf16(x[i + 2 * k + 1]) << 16;
         *reinterpret_cast<words *>(p + i) = v;
     }
 }

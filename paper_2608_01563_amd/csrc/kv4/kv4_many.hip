@@ -432,7 +432,7 @@ void kv4_many(ManyArgs a) {
             uint16_t x[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                x[k] = f32_to_bf16_rne(l == 0.f ? 0.f : o[b][4 * u + k] * inv);
+                x[k] = to_bf16(l == 0.f ? 0.f : o[b][4 * u + k] * inv);
             *reinterpret_cast<u32x2 *>(to + 32 * b + 8 * u + 4 * h) =
                 u32x2{x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16};
         }

@@ -49,11 +49,10 @@ __device__ __forceinline__ RowAt row_at(int r, int bh, int G, int Lq) {
 
 template <int D>
 struct Kv4Values {
-    static constexpr int NG = Kv4Dim<D>::kGroups, NB = Kv4Dim<D>::kBlocks, W = Kv4Dim<D>::kWide;
-    uint32_t w[NB], group[8 * NG];   // word of channel 16b + c of the lane's octet
+    static constexpr int NB = Kv4Dim<D>::kBlocks, W = Kv4Dim<D>::kWide;
+    uint32_t w[NB];   // word of channel 16b + c of the lane's octet
 
-    __device__ __forceinline__ void load(const uint32_t *words, const uint32_t *groups, int block,
-                                         int c, int g) {
+    __device__ __forceinline__ void load(const uint32_t *words, int block, int c, int g) {
         typedef uint32_t wv __attribute__((ext_vector_type(W)));
         const uint32_t *p = words + (size_t)(4 * block + g) * D + W * c;
 #pragma unroll
@@ -62,23 +61,47 @@ struct Kv4Values {
 #pragma unroll
             for (int i = 0; i < W; ++i) w[W * h + i] = v[i];
         }
-        const uint32_t *q = groups + (size_t)(32 * block + 8 * g) * NG;
-#pragma unroll
-        for (int i = 0; i < 2 * NG; ++i) {
-            const u32x4 v = *reinterpret_cast<const u32x4 *>(q + 4 * i);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) group[4 * i + k] = v[k];
+    }
+};
+
+// A block's group words, brought in by the wave's lanes (a word of K and one of V
+// each, or with one group a word of either) and handed over through LDS; tokens
+// behind the sequence read as 0.
+template <int NG>
+struct Kv4GroupWords {
+    uint32_t w[NG];   // NG = 2: K's, V's; NG = 1: K's in lanes below 32, else V's
+
+    __device__ __forceinline__ void load(const uint32_t *kp, const uint32_t *vp, int block, int n,
+                                         int lane) {
+        if (NG == 2) {
+            const int at = 64 * block + lane;
+            const bool in = at >> 1 < n;
+            w[0] = in ? kp[at] : 0u;
+            w[NG - 1] = in ? vp[at] : 0u;
+        } else {
+            const int at = 32 * block + (lane & 31);
+            w[0] = at < n ? (lane < 32 ? kp : vp)[at] : 0u;
         }
+    }
+    // K's words at to[0..], V's at to[32 NG..]
+    __device__ __forceinline__ void put(uint32_t *to, int lane) const {
+#pragma unroll
+        for (int i = 0; i < NG; ++i) to[64 * i + lane] = w[i];
+    }
+    // the lane's V word, or 0
+    __device__ __forceinline__ uint32_t value(int lane) const {
+        return NG == 2 || lane >= 32 ? w[NG - 1] : 0u;
     }
 };
 
 template <typename T, int D, int NP>
-__global__ __launch_bounds__(kThreads)
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 8)))
 void kv4_rows(RowsArgs a) {
     constexpr int NG = Kv4Dim<D>::kGroups, NB = Kv4Dim<D>::kBlocks;
     constexpr int LD = D + 4;
     __shared__ __attribute__((aligned(16))) float Os[kWaves][kRows][LD];
     __shared__ float Ms[kWaves][kRows], Ls[kWaves][kRows];
+    __shared__ __attribute__((aligned(16))) uint32_t Gs[kWaves][2][64 * NG];
 
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -106,8 +129,8 @@ void kv4_rows(RowsArgs a) {
     const uint32_t *kp = a.kp + head * NG, *vp = a.vp + head * NG;
 
     Kv4Query<D, NP> q;
-    q.load(static_cast<const T *>(a.Q) + at.at * D, in, g);
-    const float factor = row_factor(a.scale_log2, q.exponent);
+    q.load(static_cast<const T *>(a.Q) + at.at * D, in, g, a.scale_log2 < 0.f);
+    const float factor = positive_factor(a.scale_log2, q.exponent);
 
     float m = -INFINITY;               // running maximum (base 2) rounded up, of the row
     int e = -kExpMax;                  // V's scales are below 2^e
@@ -120,43 +143,46 @@ void kv4_rows(RowsArgs a) {
 #pragma unroll
     for (int i = 0; i < NB; ++i) o[i] = zero4();
 
-    auto step = [&](int block, const Kv4Keys<D> &key, Kv4Values<D> &val) {
+    auto step = [&](int block, const Kv4Keys<D> &key, const Kv4Values<D> &val,
+                    const Kv4GroupWords<NG> &words, uint32_t *groups) {
+        words.put(groups, lane);
+        __builtin_amdgcn_wave_barrier();   // one wave's LDS accesses stay in order
         f32x4 s[2];
-        key.scores(s, q);
-        s[0] *= factor;
-        s[1] *= factor;
+        key.scores(s, q, groups, c, g);
+        uint32_t vg[8 * NG];   // of the lane's octet
+#pragma unroll
+        for (int i = 0; i < 2 * NG; ++i) {
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(groups + (32 + 8 * g) * NG + 4 * i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) vg[4 * i + k] = v[k];
+        }
         if (32 * (block + 1) > all) {
-            // tokens out of sight: no score, and group words (which may hold
-            // anything behind the sequence) that add nothing
+            // tokens out of sight: no score, and group words that add nothing
+            // (a token that is not finite must not reach rows that do not see it)
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 if (32 * block + 8 * g + k >= limit) {
                     s[k >> 2][k & 3] = -INFINITY;
 #pragma unroll
-                    for (int i = 0; i < NG; ++i) val.group[k * NG + i] = 0;
+                    for (int i = 0; i < NG; ++i) vg[k * NG + i] = 0;
                 }
         }
         if (a.score != nullptr && in) {
             float *to = a.score + ((size_t)bh * rows + r) * a.Lp + 32 * block + 8 * g;
-            *reinterpret_cast<f32x4 *>(to) = s[0];
-            *reinterpret_cast<f32x4 *>(to + 4) = s[1];
+            *reinterpret_cast<f32x4 *>(to) = s[0] * factor;
+            *reinterpret_cast<f32x4 *>(to + 4) = s[1] * factor;
         }
-        float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                         fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-        mx = max_over_groups(mx);
-        uint32_t top = 0;
-#pragma unroll
-        for (int k = 0; k < 8 * NG; ++k) top = max(top, val.group[k]);
+        float mx = max3_f32(max3_f32(s[0][0], s[0][1], s[0][2]),
+                            max3_f32(s[0][3], s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]));
+        mx = max_over_groups(mx) * factor;
+        // NaN scales (a token that is not finite) move nothing
+        const uint32_t mine = words.value(lane);
+        const uint32_t top = mine < 0x7f800000u ? mine : 0u;
         if (__any(mx > m + kRowSlack || top > most)) {
-            // NaN scales (a token that is not finite) move nothing
-            top = 0;
-#pragma unroll
-            for (int k = 0; k < 8 * NG; ++k)
-                top = max(top, val.group[k] < 0x7f800000u ? val.group[k] : 0u);
-            top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
-            top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
             const float m_new = fmaxf(m, ceilf(mx));
-            const int e_new = max(e, min(kExpMax, (int)(top >> 23) - 126));
+            // finite words order as the scales in their upper halves do
+            const uint32_t high = __float_as_uint(max_of_wave(__uint_as_float(top)));
+            const int e_new = max(e, min(kExpMax, (int)(high >> 23) - 126));
             const float alpha =
                 m_new == -INFINITY ? 1.f : ldexpf(exp2_fast(m - m_new), e - e_new);
             l *= alpha;
@@ -168,11 +194,11 @@ void kv4_rows(RowsArgs a) {
             e = e_new;
             most = e == kExpMax ? 0xffffffffu : ((uint32_t)(e + 127) << 23) - 1;
         }
-        const float off = (m == -INFINITY ? 0.f : m) + (float)(e - kRaise);
+        const float off = (float)(kRaise - e) - (m == -INFINITY ? 0.f : m);
         float p[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            p[k] = exp2_fast(s[k >> 2][k & 3] - off);
+            p[k] = exp2_fast(fmaf(s[k >> 2][k & 3], factor, off));
             l += p[k];
         }
 #pragma unroll
@@ -181,7 +207,7 @@ void kv4_rows(RowsArgs a) {
             f16x8 part[NP];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const uint32_t gw = val.group[k * NG + i];
+                const uint32_t gw = vg[k * NG + i];
                 x[k] = p[k] * group_scale(gw);
                 low[i] = fmaf(p[k], group_min(gw), low[i]);
             }
@@ -190,7 +216,7 @@ void kv4_rows(RowsArgs a) {
             for (int cb = i * (NB / NG); cb < (i + 1) * (NB / NG); ++cb) {
                 const f16x8 v = code_operand(val.w[cb]);
 #pragma unroll
-                for (int n = 0; n < NP; ++n) o[cb] = mfma16x16x32f16(v, part[n], o[cb]);
+                for (int n = NP - 1; n >= 0; --n) o[cb] = mfma16x16x32f16(v, part[n], o[cb]);
             }
         }
     };
@@ -201,17 +227,21 @@ void kv4_rows(RowsArgs a) {
     if (mine < stop) {
         Kv4Keys<D> k0, k1;
         Kv4Values<D> v0, v1;
-        k0.load(kw, kp, mine, c, g);
-        v0.load(vw, vp, mine, c, g);
+        Kv4GroupWords<NG> g0, g1;
+        k0.load(kw, mine, c, g);
+        v0.load(vw, mine, c, g);
+        g0.load(kp, vp, mine, mask.n, lane);
         for (int block = mine; block < stop; block += 2 * kWaves) {
             const int b1 = min(block + kWaves, stop - 1), b2 = min(block + 2 * kWaves, stop - 1);
-            k1.load(kw, kp, b1, c, g);
-            v1.load(vw, vp, b1, c, g);
-            step(block, k0, v0);
+            k1.load(kw, b1, c, g);
+            v1.load(vw, b1, c, g);
+            g1.load(kp, vp, b1, mask.n, lane);
+            step(block, k0, v0, g0, Gs[w][0]);
             if (block + kWaves >= stop) break;
-            k0.load(kw, kp, b2, c, g);
-            v0.load(vw, vp, b2, c, g);
-            step(block + kWaves, k1, v1);
+            k0.load(kw, b2, c, g);
+            v0.load(vw, b2, c, g);
+            g0.load(kp, vp, b2, mask.n, lane);
+            step(block + kWaves, k1, v1, g1, Gs[w][1]);
         }
     }
 
@@ -270,7 +300,7 @@ void kv4_rows(RowsArgs a) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const float y = sum == 0.f ? 0.f : x[i] * inv;
-        if constexpr (sizeof(T) == 2) out[i] = f32_to_bf16_rne(y);
+        if constexpr (sizeof(T) == 2) out[i] = to_bf16(y);
         else out[i] = y;
     }
     if (d0 == 0) a.LSE[to.at] = sum != sum ? sum : row_lse(top, sum);
@@ -286,20 +316,25 @@ struct JoinArgs {
 };
 constexpr int kJoinKeys = 4 * kThreads;   // tokens of a weights workgroup
 
-// Row's maximum and sum over the splits.
-__device__ __forceinline__ void joined_stat(const float *stat, size_t first, int stride,
-                                            int splits, float *top, float *sum) {
+// A row's splits (at most 64), one a lane: maximum, sum, and the lane's factor.
+struct Joined {
+    float top, sum, factor;
+};
+__device__ __forceinline__ Joined join_stats(const float *stat, size_t first, int stride,
+                                             int splits, int lane) {
     float m = -INFINITY, l = 0.f;
-    for (int k = 0; k < splits; ++k) m = fmaxf(m, stat[2 * (first + (size_t)k * stride)]);
-    if (m > -INFINITY)
-        for (int k = 0; k < splits; ++k) {
-            const float *st = stat + 2 * (first + (size_t)k * stride);
-            l = fmaf(exp2_fast(st[0] - m), st[1], l);
-        }
-    else   // no score above -inf: the sums are 0, or NaN where a score is
-        for (int k = 0; k < splits; ++k) l += stat[2 * (first + (size_t)k * stride) + 1];
-    *top = m;
-    *sum = l;
+    if (lane < splits) {
+        const float *st = stat + 2 * (first + (size_t)lane * stride);
+        m = st[0];
+        l = st[1];
+    }
+    const float top = max_of_wave(m);
+    // without a score above -inf the sums are 0, or NaN where a score is
+    const float factor = top == -INFINITY ? 1.f : exp2_fast(m - top);
+    float sum = factor * l;
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) sum += xor_lanes(sum, k);
+    return {top, sum, factor};
 }
 
 template <typename T, int D>
@@ -312,31 +347,37 @@ void kv4_join(JoinArgs a) {
         const int bh = id / rows, r = id - bh * rows;
         if (bh >= a.heads) return;
         const size_t first = (size_t)bh * a.splits * rows + r;
-        float top, sum;
-        joined_stat(a.stat, first, rows, a.splits, &top, &sum);
-        constexpr int N = D < 64 ? 1 : D / 64;
-        const bool mine = D >= 64 || lane < D;
-        const int d0 = mine ? N * lane : 0;
-        float x[N];
+        const Joined j = join_stats(a.stat, first, rows, a.splits, lane);
+        // lanes in teams of D / 4, four channels each, take splits in turn
+        constexpr int TEAMS = 256 / D;
+        const int team = lane / (D / 4), d0 = 4 * (lane % (D / 4));
+        f32x4 x = zero4();
+        // (four reads at a time; past the end the last split again, unused)
+        for (int k0 = 0; k0 < a.splits; k0 += 4 * TEAMS)
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = 0.f;
-        for (int k = 0; k < a.splits; ++k) {
-            const size_t slot = first + (size_t)k * rows;
-            const float f = top > -INFINITY ? exp2_fast(a.stat[2 * slot] - top) : 1.f;
+            for (int u = 0; u < 4; ++u) {
+                const int k = k0 + u * TEAMS + team;
+                const float f = __shfl(j.factor, min(k, 63), 64);
+                const f32x4 y = *reinterpret_cast<const f32x4 *>(
+                    a.part + (first + (size_t)min(k, a.splits - 1) * rows) * D + d0);
+                if (k < a.splits) x += f * y;
+            }
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = fmaf(f, a.part[slot * D + d0 + i], x[i]);
+        for (int i = 0; i < 4; ++i) {
+            if (TEAMS >= 2) x[i] = sum_xor32(x[i]);
+            if (TEAMS >= 4) x[i] = sum_xor16(x[i]);
+            if (TEAMS >= 8) x[i] += xor_lanes(x[i], 8);
         }
         const RowAt to = row_at(r, bh, a.G, a.Lq);
-        if (mine) {
+        if (team == 0) {
+            const float inv = 1.f / j.sum;
             T *out = static_cast<T *>(a.O) + to.at * D + d0;
+            float y[4];
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float y = sum == 0.f ? 0.f : x[i] / sum;
-                if constexpr (sizeof(T) == 2) out[i] = f32_to_bf16_rne(y);
-                else out[i] = y;
-            }
+            for (int i = 0; i < 4; ++i) y[i] = j.sum == 0.f ? 0.f : x[i] * inv;
+            store_row(out, y);
         }
-        if (lane == 0) a.LSE[to.at] = sum != sum ? sum : row_lse(top, sum);
+        if (lane == 0) a.LSE[to.at] = j.sum != j.sum ? j.sum : row_lse(j.top, j.sum);
         return;
     }
     // weights: a thread adds the rows' probabilities of four tokens
@@ -347,19 +388,20 @@ void kv4_join(JoinArgs a) {
     const int b = bh / a.H;
     const Kv4Mask mask = sequence_mask(a.key_len, a.q_len, b, a.L, a.Lq, a.causal);
     if ((id - bh * per) * kJoinKeys >= mask.n) return;
-    if ((int)threadIdx.x < rows) {
-        const int r = threadIdx.x;
+    // a row without sight adds nothing
+    for (int r = threadIdx.x >> 6; r < rows; r += kWaves) {
         const RowAt at = row_at(r, bh, a.G, a.Lq);
+        const int lane = threadIdx.x & 63;
         float v;
         if (a.splits > 1) {
-            float top, sum;
-            joined_stat(a.stat, (size_t)bh * a.splits * rows + r, rows, a.splits, &top, &sum);
-            v = sum == 0.f ? INFINITY : top + log2f(sum);
+            const Joined j =
+                join_stats(a.stat, (size_t)bh * a.splits * rows + r, rows, a.splits, lane);
+            v = j.sum == 0.f ? INFINITY : j.top + log2f(j.sum);
         } else {
             v = a.LSE[at.at] * kLog2e;
             if (v == -INFINITY) v = INFINITY;
         }
-        lse2[r] = at.i < mask.rows ? v : INFINITY;   // a row without sight adds nothing
+        if (lane == 0) lse2[r] = at.i < mask.rows ? v : INFINITY;
     }
     __syncthreads();
     if (j0 >= mask.n) return;

@@ -56,16 +56,16 @@ __device__ __forceinline__ void split_operand(f16x8 (&out)[NP], const float (&x)
 }
 
 // A query row as operands: q[p][s] holds channels 32s + 8g + e of part p, times
-// 2^(15 - exponent of the row's largest value); sum[gr] the group sums in the
+// 2^(15 - exponent of the row's largest value); sum is one group's sum in the
 // units of a product with codes.
 template <int D, int NP>
 struct Kv4Query {
     f16x8 q[NP][D / 32];
-    float sum[Kv4Dim<D>::kGroups];
+    float sum;      // of group g (0 where there is none)
     int exponent;   // scores = products * 2^(exponent - 6)
 
     template <typename T>
-    __device__ __forceinline__ void load(const T *row, bool valid, int g) {
+    __device__ __forceinline__ void load(const T *row, bool valid, int g, bool negate) {
         constexpr int NS = D / 32, NG = Kv4Dim<D>::kGroups;
         float x[NS][8];
         float top = 0.f;
@@ -78,11 +78,15 @@ struct Kv4Query {
                 for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[s][e]));
+            for (int e = 0; e < 8; ++e) {
+                top = fmaxf(top, fabsf(x[s][e]));
+                if (negate) x[s][e] = -x[s][e];
+            }
         }
         top = max_over_groups(top);
         // 0 for zero, infinity and NaN
         exponent = __builtin_amdgcn_frexp_expf(top);
+        sum = 0.f;
 #pragma unroll
         for (int gr = 0; gr < NG; ++gr) {
             float t = 0.f;
@@ -90,7 +94,8 @@ struct Kv4Query {
             for (int s = gr * (NS / NG); s < (gr + 1) * (NS / NG); ++s)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) t += ldexpf(x[s][e], -exponent);
-            sum[gr] = sum_over_groups(t) * 0x1p6f;
+            t = sum_over_groups(t) * 0x1p6f;
+            if (g == gr) sum = t;
         }
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
@@ -105,15 +110,14 @@ struct Kv4Query {
     }
 };
 
-// The K words of 32 tokens (two products) and their groups: all that scores need.
+// The K words of 32 tokens, two products' worth.
 template <int D>
 struct Kv4Keys {
     static constexpr int NG = Kv4Dim<D>::kGroups, NW = D / 32;
-    uint32_t w[2][NW], group[8 * NG];   // group words of tokens 8g + k at k * NG
+    uint32_t w[2][NW];
 
-    // `words`, `groups`: the head's regions.  c = lane%16, g = lane/16.
-    __device__ __forceinline__ void load(const uint32_t *words, const uint32_t *groups, int block,
-                                         int c, int g) {
+    // `words`: the head's region.  c = lane%16, g = lane/16.
+    __device__ __forceinline__ void load(const uint32_t *words, int block, int c, int g) {
         typedef uint32_t wv __attribute__((ext_vector_type(NW)));
         const int key = 32 * block + 8 * (c >> 2) + (c & 3);
 #pragma unroll
@@ -121,37 +125,42 @@ struct Kv4Keys {
             const wv v = *reinterpret_cast<const wv *>(words + (size_t)(key + 4 * t) * (D / 8) +
                                                        g * NW);
 #pragma unroll
-            for (int i = 0; i < NW; ++i) w[t][i] = v[i];
-        }
-        const uint32_t *p = groups + (size_t)(32 * block + 8 * g) * NG;
-#pragma unroll
-        for (int i = 0; i < 2 * NG; ++i) {
-            const u32x4 v = *reinterpret_cast<const u32x4 *>(p + 4 * i);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) group[4 * i + k] = v[k];
+            for (int i = 0; i < NW; ++i) w[t][i] = NW == 1 ? v[0] : v[i];
         }
     }
 
-    // s[t][r] = score of token 8g + 4t + r for the lane's row, before the row's factor.
+    // s[t][r] = score of token 8g + 4t + r for the lane's row, before the row's
+    // factor.  `group`: the block's group words in LDS, token k's at k * NG.
     template <int NP>
-    __device__ __forceinline__ void scores(f32x4 (&s)[2], const Kv4Query<D, NP> &q) const {
+    __device__ __forceinline__ void scores(f32x4 (&s)[2], const Kv4Query<D, NP> &q,
+                                           const uint32_t *group, int c, int g) const {
+        f32x4 m[2][NG];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t) {
+            // the minima's part: one product over the groups (sum is 0 behind them)
+            const uint32_t low = group[(8 * (c >> 2) + 4 * t + (c & 3)) * NG + g % NG];
+            s[t] = mfma16x16x4(group_min(low), q.sum, zero4());
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
-                f32x4 m = zero4();
+                m[t][gr] = zero4();
 #pragma unroll
                 for (int i = gr * (NW / NG); i < (gr + 1) * (NW / NG); ++i) {
                     const f16x8 a = code_operand(w[t][i]);
 #pragma unroll
-                    for (int p = 0; p < NP; ++p) m = mfma16x16x32f16(a, q.q[p][i], m);
+                    for (int p = NP - 1; p >= 0; --p)
+                        m[t][gr] = mfma16x16x32f16(a, q.q[p][i], m[t][gr]);
                 }
+            }
+        }
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t gw = group[(4 * t + r) * NG + gr];
-                    const float low = gr == 0 ? group_min(gw) * q.sum[gr]
-                                              : fmaf(group_min(gw), q.sum[gr], s[t][r]);
-                    s[t][r] = fmaf(group_scale(gw), m[r], low);
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {   // words (8g + 4t) NG + 4i ..+3
+                const u32x4 v = *reinterpret_cast<const u32x4 *>(group + (8 * g + 4 * t) * NG + 4 * i);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int r = (4 * i + k) / NG, gr = (4 * i + k) % NG;
+                    s[t][r] = fmaf(group_scale(v[k]), m[t][gr][r], s[t][r]);
                 }
             }
     }

@@ -20,7 +20,7 @@ Kv4Plan kv4_plan(const Kv4Attn &p, bool weights, bool bf16) {
     Kv4Plan plan = {};
     plan.rows = !bf16 || rows < 64 ? 16 : heads * ((rows + 255) / 256) >= 256 ? 256 : 128;
     const int64_t tiles = heads * ((rows + plan.rows - 1) / plan.rows);
-    const int64_t most = std::max<int64_t>(1, kv4_padded(p.L) / 32 / 8);
+    const int64_t most = std::min<int64_t>(64, std::max<int64_t>(1, kv4_padded(p.L) / 32 / 8));
     const int64_t want = plan.rows == 256 ? 256 : 512;
     plan.splits = (int)std::min<int64_t>((want + tiles - 1) / tiles, most);
     plan.scores = weights && rows <= 16;
