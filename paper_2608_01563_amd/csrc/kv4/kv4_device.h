@@ -6,6 +6,7 @@
 namespace mg {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 template <int D>
 struct Kv4Dim {

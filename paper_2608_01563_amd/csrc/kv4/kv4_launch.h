@@ -30,7 +30,8 @@ inline int64_t kv4_rows(const Kv4Attn &p) { return (int64_t)p.G * p.Lq; }
 // How one call runs.
 struct Kv4Plan {
     int rows;          // of a workgroup: 16 (kv4_rows), 128 or 256 (kv4_many)
-    int splits;        // workgroups that share a row tile's keys
+    int splits;        // workgroups that share a row tile's tokens
+    int chunk;         // kv4_rows: blocks of 32 tokens of each
     bool scores;       // weights come from scores the forward keeps
     int shares;        // of the rows, where weights come from Q, K and LSE (else 0)
     size_t part, stat, score, sums, bytes;   // workspace: offsets of the parts, size

@@ -52,19 +52,15 @@ struct Query32 {
         float x[NS][8];
         float top = 0.f;
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            if (valid) {
-                load_row(x[s], row + 16 * s + 8 * h);
-            } else {
+        for (int s = 0; s < NS; ++s) load_row(x[s], row + 16 * s + 8 * h);   // a row that is there
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
-            }
+        for (int s = 0; s < NS; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
+                x[s][e] = valid ? x[s][e] : 0.f;
                 top = fmaxf(top, fabsf(x[s][e]));
                 if (negate) x[s][e] = -x[s][e];
             }
-        }
         exponent = __builtin_amdgcn_frexp_expf(max_xor32(top));
         float each[2] = {0.f, 0.f};
 #pragma unroll

@@ -1,7 +1,12 @@
 // kv4_rows.hip -- attention over the 4-bit cache: a workgroup takes 16 of the
-// query rows that share a cache head and one share of the tokens; its four
+// query rows that share a cache head and one chunk of the tokens; its four
 // waves take 32-token blocks in turn, each with its own online softmax, and
-// join through LDS; shares join in kv4_join.
+// join through LDS; chunks join in kv4_join.
+//
+// A chunk is a fixed number of blocks whatever the sequence's length: chunks
+// behind its end are gone at once and the dispatcher evens out sequences of
+// different length; and where a wave's first block lies does not wait for the
+// length, so words, groups, query row and length are all asked for together.
 //
 // Scores: kv4_tile.h.  The second product is O^T = V^T P^T on V's codes:
 //   O = sum_j (p_j scale_j) code_j + sum_j p_j min_j
@@ -34,7 +39,7 @@ struct RowsArgs {
     const int32_t *key_len, *q_len;
     int H, G, Lq, L, Lp, causal;
     float scale_log2;
-    int splits, row_tiles;
+    int splits, chunk, row_tiles;   // chunk: blocks
 };
 
 // Where row r = i * G + g of a cache head lies among the query rows.
@@ -65,28 +70,28 @@ struct Kv4Values {
 };
 
 // A block's group words, brought in by the wave's lanes (a word of K and one of V
-// each, or with one group a word of either) and handed over through LDS; tokens
-// behind the sequence read as 0.
+// each, or with one group a word of either) and handed over through LDS.
 template <int NG>
 struct Kv4GroupWords {
     uint32_t w[NG];   // NG = 2: K's, V's; NG = 1: K's in lanes below 32, else V's
 
-    __device__ __forceinline__ void load(const uint32_t *kp, const uint32_t *vp, int block, int n,
+    __device__ __forceinline__ void load(const uint32_t *kp, const uint32_t *vp, int block,
                                          int lane) {
         if (NG == 2) {
-            const int at = 64 * block + lane;
-            const bool in = at >> 1 < n;
-            w[0] = in ? kp[at] : 0u;
-            w[NG - 1] = in ? vp[at] : 0u;
+            w[0] = kp[64 * block + lane];
+            w[NG - 1] = vp[64 * block + lane];
         } else {
-            const int at = 32 * block + (lane & 31);
-            w[0] = at < n ? (lane < 32 ? kp : vp)[at] : 0u;
+            w[0] = (lane < 32 ? kp : vp)[32 * block + (lane & 31)];
         }
     }
-    // K's words at to[0..], V's at to[32 NG..]
-    __device__ __forceinline__ void put(uint32_t *to, int lane) const {
+    // K's words at to[0..], V's at to[32 NG..]; 0 for tokens at or behind n
+    __device__ __forceinline__ void put(uint32_t *to, int block, int n, int lane) {
+        const bool in = 32 * block + (NG == 2 ? lane >> 1 : lane & 31) < n;
 #pragma unroll
-        for (int i = 0; i < NG; ++i) to[64 * i + lane] = w[i];
+        for (int i = 0; i < NG; ++i) {
+            w[i] = in ? w[i] : 0u;
+            to[64 * i + lane] = w[i];
+        }
     }
     // the lane's V word, or 0
     __device__ __forceinline__ uint32_t value(int lane) const {
@@ -111,26 +116,33 @@ void kv4_rows(RowsArgs a) {
     const int rows = a.G * a.Lq;
     const Kv4Mask mask = sequence_mask(a.key_len, a.q_len, b, a.L, a.Lq, a.causal);
 
-    // the tile's rows, and the tokens that its last and its first row see
+    // blocks begin + w, + kWaves, ... are the wave's; its first one's words
+    const size_t head = (size_t)bh * a.Lp;
+    const uint32_t *kw = a.kw + head * (D / 8), *vw = a.vw + head / 8 * D;
+    const uint32_t *kp = a.kp + head * NG, *vp = a.vp + head * NG;
+    const int begin = split * a.chunk, mine = begin + w, last = a.Lp / 32 - 1;
+    Kv4Keys<D> k0, k1;
+    Kv4Values<D> v0, v1;
+    Kv4GroupWords<NG> g0, g1;
+    k0.load(kw, min(mine, last), c, g);
+    v0.load(vw, min(mine, last), c, g);
+    g0.load(kp, vp, min(mine, last), lane);
+
     const int r = kRows * tile + c;
     const bool in = r < rows;
     const RowAt at = row_at(in ? r : rows - 1, bh, a.G, a.Lq);
+    Kv4Query<D, NP> q;
+    q.load(static_cast<const T *>(a.Q) + at.at * D, in, g, a.scale_log2 < 0.f);
+    const float factor = positive_factor(a.scale_log2, q.exponent);
+
+    // the tokens that the tile's last and its first row see
+    if (32 * begin >= mask.n && begin > 0) return;   // kv4_join knows
     const int first_i = kRows * tile / a.G;
     const int last_i = min((min(rows, kRows * (tile + 1)) - 1) / a.G, mask.rows - 1);
     const int end = first_i < mask.rows ? max(mask.limit(last_i), 0) : 0;
     const int all = mask.limit(first_i);   // below: every row sees the token
     const int limit = mask.limit(at.i);
-
-    const int blocks = (end + 31) / 32, each = (blocks + a.splits - 1) / a.splits;
-    const int begin = split * each, stop = min(blocks, begin + each);
-
-    const size_t head = (size_t)bh * a.Lp;
-    const uint32_t *kw = a.kw + head * (D / 8), *vw = a.vw + head / 8 * D;
-    const uint32_t *kp = a.kp + head * NG, *vp = a.vp + head * NG;
-
-    Kv4Query<D, NP> q;
-    q.load(static_cast<const T *>(a.Q) + at.at * D, in, g, a.scale_log2 < 0.f);
-    const float factor = positive_factor(a.scale_log2, q.exponent);
+    const int stop = min((end + 31) / 32, begin + a.chunk);
 
     float m = -INFINITY;               // running maximum (base 2) rounded up, of the row
     int e = -kExpMax;                  // V's scales are below 2^e
@@ -144,8 +156,8 @@ void kv4_rows(RowsArgs a) {
     for (int i = 0; i < NB; ++i) o[i] = zero4();
 
     auto step = [&](int block, const Kv4Keys<D> &key, const Kv4Values<D> &val,
-                    const Kv4GroupWords<NG> &words, uint32_t *groups) {
-        words.put(groups, lane);
+                    Kv4GroupWords<NG> &words, uint32_t *groups) {
+        words.put(groups, block, mask.n, lane);
         __builtin_amdgcn_wave_barrier();   // one wave's LDS accesses stay in order
         f32x4 s[2];
         key.scores(s, q, groups, c, g);
@@ -221,28 +233,19 @@ void kv4_rows(RowsArgs a) {
         }
     };
 
-    // blocks begin + w, + kWaves, ...; the next one's words load while one is
-    // worked on (past the end the last block again)
-    const int mine = begin + w;
-    if (mine < stop) {
-        Kv4Keys<D> k0, k1;
-        Kv4Values<D> v0, v1;
-        Kv4GroupWords<NG> g0, g1;
-        k0.load(kw, mine, c, g);
-        v0.load(vw, mine, c, g);
-        g0.load(kp, vp, mine, mask.n, lane);
-        for (int block = mine; block < stop; block += 2 * kWaves) {
-            const int b1 = min(block + kWaves, stop - 1), b2 = min(block + 2 * kWaves, stop - 1);
-            k1.load(kw, b1, c, g);
-            v1.load(vw, b1, c, g);
-            g1.load(kp, vp, b1, mask.n, lane);
-            step(block, k0, v0, g0, Gs[w][0]);
-            if (block + kWaves >= stop) break;
-            k0.load(kw, b2, c, g);
-            v0.load(vw, b2, c, g);
-            g0.load(kp, vp, b2, mask.n, lane);
-            step(block + kWaves, k1, v1, g1, Gs[w][1]);
-        }
+    // the next block's words load while one is worked on (past the end the last
+    // block again)
+    for (int block = mine; block < stop; block += 2 * kWaves) {
+        const int b1 = min(block + kWaves, stop - 1), b2 = min(block + 2 * kWaves, stop - 1);
+        k1.load(kw, b1, c, g);
+        v1.load(vw, b1, c, g);
+        g1.load(kp, vp, b1, lane);
+        step(block, k0, v0, g0, Gs[w][0]);
+        if (block + kWaves >= stop) break;
+        k0.load(kw, b2, c, g);
+        v0.load(vw, b2, c, g);
+        g0.load(kp, vp, b2, lane);
+        step(block + kWaves, k1, v1, g1, Gs[w][1]);
     }
 
     // out of the running units, then the waves' shares through LDS
@@ -312,29 +315,29 @@ struct JoinArgs {
     float *LSE, *weight;
     const float *part, *stat, *score;
     const int32_t *key_len, *q_len;
-    int H, G, Lq, L, Lp, causal, splits, heads, out_groups;
+    int H, G, Lq, L, Lp, causal, splits, chunk, heads, out_groups;   // chunk: blocks, or 0
 };
 constexpr int kJoinKeys = 4 * kThreads;   // tokens of a weights workgroup
 
 // A row's splits (at most 64), one a lane: maximum, sum, and the lane's factor.
+// Splits whose chunk lies behind the sequence's n tokens wrote nothing.
 struct Joined {
     float top, sum, factor;
 };
-__device__ __forceinline__ Joined join_stats(const float *stat, size_t first, int stride,
-                                             int splits, int lane) {
-    float m = -INFINITY, l = 0.f;
-    if (lane < splits) {
-        const float *st = stat + 2 * (first + (size_t)lane * stride);
-        m = st[0];
-        l = st[1];
-    }
+__device__ __forceinline__ int written_splits(const JoinArgs &a, int n) {
+    return a.chunk == 0 ? a.splits : max(1, min(a.splits, (n + 32 * a.chunk - 1) / (32 * a.chunk)));
+}
+__device__ __forceinline__ Joined join_stats(f32x2 stat, int count, int lane) {
+    const float m = lane < count ? stat[0] : -INFINITY, l = lane < count ? stat[1] : 0.f;
     const float top = max_of_wave(m);
     // without a score above -inf the sums are 0, or NaN where a score is
     const float factor = top == -INFINITY ? 1.f : exp2_fast(m - top);
-    float sum = factor * l;
-#pragma unroll
-    for (int k = 1; k < 64; k *= 2) sum += xor_lanes(sum, k);
-    return {top, sum, factor};
+    return {top, sum_of_wave(factor * l), factor};
+}
+__device__ __forceinline__ f32x2 load_stat(const float *stat, size_t first, int stride, int splits,
+                                           int lane) {
+    return *reinterpret_cast<const f32x2 *>(stat +
+                                            2 * (first + (size_t)min(lane, splits - 1) * stride));
 }
 
 template <typename T, int D>
@@ -347,20 +350,29 @@ void kv4_join(JoinArgs a) {
         const int bh = id / rows, r = id - bh * rows;
         if (bh >= a.heads) return;
         const size_t first = (size_t)bh * a.splits * rows + r;
-        const Joined j = join_stats(a.stat, first, rows, a.splits, lane);
-        // lanes in teams of D / 4, four channels each, take splits in turn
+        // lanes in teams of D / 4, four channels each, take splits in turn, four
+        // reads at a time (the first ones do not wait for length or maxima; past
+        // the end the last split again, unused)
         constexpr int TEAMS = 256 / D;
         const int team = lane / (D / 4), d0 = 4 * (lane % (D / 4));
-        f32x4 x = zero4();
-        // (four reads at a time; past the end the last split again, unused)
-        for (int k0 = 0; k0 < a.splits; k0 += 4 * TEAMS)
+        auto part_at = [&](int k) {
+            return *reinterpret_cast<const f32x4 *>(
+                a.part + (first + (size_t)min(k, a.splits - 1) * rows) * D + d0);
+        };
+        const f32x2 stat = load_stat(a.stat, first, rows, a.splits, lane);
+        const int n = optional_len(a.key_len, bh / a.H, a.L);
+        f32x4 y[4], x = zero4();
+#pragma unroll
+        for (int u = 0; u < 4; ++u) y[u] = part_at(u * TEAMS + team);
+        const int count = written_splits(a, n);
+        const Joined j = join_stats(stat, count, lane);
+        for (int k0 = 0; k0 < count; k0 += 4 * TEAMS)
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int k = k0 + u * TEAMS + team;
-                const float f = __shfl(j.factor, min(k, 63), 64);
-                const f32x4 y = *reinterpret_cast<const f32x4 *>(
-                    a.part + (first + (size_t)min(k, a.splits - 1) * rows) * D + d0);
-                if (k < a.splits) x += f * y;
+                const float f = __shfl(j.factor, k & 63, 64);
+                if (k < count) x += f * y[u];
+                if (k0 + 4 * TEAMS < count) y[u] = part_at(k + 4 * TEAMS);
             }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -394,8 +406,9 @@ void kv4_join(JoinArgs a) {
         const int lane = threadIdx.x & 63;
         float v;
         if (a.splits > 1) {
-            const Joined j =
-                join_stats(a.stat, (size_t)bh * a.splits * rows + r, rows, a.splits, lane);
+            const f32x2 stat =
+                load_stat(a.stat, (size_t)bh * a.splits * rows + r, rows, a.splits, lane);
+            const Joined j = join_stats(stat, written_splits(a, mask.n), lane);
             v = j.sum == 0.f ? INFINITY : j.top + log2f(j.sum);
         } else {
             v = a.LSE[at.at] * kLog2e;
@@ -432,7 +445,7 @@ hipError_t rows(const Kv4Attn &p, const Kv4Plan &plan, const void *Q,
                         (float *)(ws + plan.stat),
                         plan.scores ? (float *)(ws + plan.score) : nullptr, p.key_len, p.q_len,
                         p.H, p.G, p.Lq, p.L, kv4_padded(p.L), p.causal, p.scale * kLog2e,
-                        plan.splits, tiles};
+                        plan.splits, plan.chunk, tiles};
     kv4_rows<T, D, NP><<<(unsigned)((int64_t)p.B * p.H * plan.splits * tiles), kThreads, 0, s>>>(a);
     return hipGetLastError();
 }
@@ -446,7 +459,7 @@ hipError_t join(const Kv4Attn &p, const Kv4Plan &plan, void *O, float *LSE, floa
     const JoinArgs a = {O, LSE, weight, (const float *)(ws + plan.part),
                         (const float *)(ws + plan.stat), (const float *)(ws + plan.score),
                         p.key_len, p.q_len, p.H, p.G, p.Lq, p.L, kv4_padded(p.L), p.causal,
-                        plan.splits, (int)heads, (int)outs};
+                        plan.splits, plan.rows == kRows ? plan.chunk : 0, (int)heads, (int)outs};
     kv4_join<T, D><<<(unsigned)(outs + keys), kThreads, 0, s>>>(a);
     return hipGetLastError();
 }

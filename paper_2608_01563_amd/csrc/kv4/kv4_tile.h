@@ -70,19 +70,15 @@ struct Kv4Query {
         float x[NS][8];
         float top = 0.f;
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            if (valid) {
-                load_row(x[s], row + 32 * s + 8 * g);
-            } else {
+        for (int s = 0; s < NS; ++s) load_row(x[s], row + 32 * s + 8 * g);   // a row that is there
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[s][e] = 0.f;
-            }
+        for (int s = 0; s < NS; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
+                x[s][e] = valid ? x[s][e] : 0.f;
                 top = fmaxf(top, fabsf(x[s][e]));
                 if (negate) x[s][e] = -x[s][e];
             }
-        }
         top = max_over_groups(top);
         // 0 for zero, infinity and NaN
         exponent = __builtin_amdgcn_frexp_expf(top);
@@ -206,7 +202,7 @@ __device__ __forceinline__ int piece(int row, int p) {
     return row * (N + 1) + p;
 }
 
-// Maximum over the wave (rotations within its rows of 16, then swaps).
+// Maximum and sum over the wave (rotations within its rows of 16, then swaps).
 template <int ROTATE>
 __device__ __forceinline__ float max_rotated(float v) {
     return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(
@@ -215,6 +211,16 @@ __device__ __forceinline__ float max_rotated(float v) {
 __device__ __forceinline__ float max_of_wave(float v) {
     v = max_rotated<1>(max_rotated<2>(max_rotated<4>(max_rotated<8>(v))));
     return max_xor32(max_xor16(v));
+}
+
+template <int ROTATE>
+__device__ __forceinline__ float sum_rotated(float v) {
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + ROTATE,
+                                                          0xf, 0xf, false));
+}
+__device__ __forceinline__ float sum_of_wave(float v) {
+    v = sum_rotated<1>(sum_rotated<2>(sum_rotated<4>(sum_rotated<8>(v))));
+    return sum_xor32(sum_xor16(v));
 }
 
 // Token (of 32) in row i of a score product.

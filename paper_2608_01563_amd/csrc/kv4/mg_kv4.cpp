@@ -12,17 +12,21 @@
 
 namespace mg {
 
-// Splits: enough workgroups of the row kernel to put two on every compute
-// unit, while each of a workgroup's four waves still has two blocks of 32
-// tokens when the cache is full.
+// How a call runs.  kv4_many from 64 rows a cache head on, with 256 rows a
+// workgroup where that gives every compute unit one, its tokens split over
+// workgroups where there are fewer.  Else kv4_rows, its tokens cut into chunks:
+// three workgroups fit a compute unit, and caches are seldom full, so up to 1,280
+// workgroups.  A split has at least 256 tokens.
 Kv4Plan kv4_plan(const Kv4Attn &p, bool weights, bool bf16) {
     const int64_t heads = (int64_t)p.B * p.H, rows = kv4_rows(p);
     Kv4Plan plan = {};
     plan.rows = !bf16 || rows < 64 ? 16 : heads * ((rows + 255) / 256) >= 256 ? 256 : 128;
     const int64_t tiles = heads * ((rows + plan.rows - 1) / plan.rows);
-    const int64_t most = std::min<int64_t>(64, std::max<int64_t>(1, kv4_padded(p.L) / 32 / 8));
-    const int64_t want = plan.rows == 256 ? 256 : 512;
-    plan.splits = (int)std::min<int64_t>((want + tiles - 1) / tiles, most);
+    const int64_t want = plan.rows == 16 ? 1280 : plan.rows == 256 ? 256 : 512;
+    const int blocks = kv4_padded(p.L) / 32;
+    plan.splits = (int)std::max<int64_t>(
+        1, std::min({(want + tiles - 1) / tiles, (int64_t)64, (int64_t)blocks / 8}));
+    plan.chunk = cdiv(blocks, plan.splits);
     plan.scores = weights && rows <= 16;
     if (plan.splits > 1) {
         plan.part = plan.bytes;
