@@ -59,18 +59,25 @@ struct Kv4Values {
 
     __device__ __forceinline__ void load(const uint32_t *words, int block, int c, int g) {
         typedef uint32_t wv __attribute__((ext_vector_type(W)));
-        const uint32_t *p = words + (size_t)(4 * block + g) * D + W * c;
+        const uint32_t at = 4u * ((4 * block + g) * D + W * c);
 #pragma unroll
         for (int h = 0; h < NB / W; ++h) {
-            const wv v = *reinterpret_cast<const wv *>(p + 16 * W * h);
+            const wv v = *reinterpret_cast<const wv *>(reinterpret_cast<const char *>(words) +
+                                                       (at + 64u * W * h));
 #pragma unroll
             for (int i = 0; i < W; ++i) w[W * h + i] = v[i];
         }
     }
 };
 
+template <int NG>
+struct BlockGroups {   // a block's groups in LDS, token k's at k * NG
+    float scale[2][32 * NG], min[2][32 * NG];   // of K, V
+};
+
 // A block's group words, brought in by the wave's lanes (a word of K and one of V
-// each, or with one group a word of either) and handed over through LDS.
+// each, or with one group a word of either), taken apart there and handed over
+// through LDS.
 template <int NG>
 struct Kv4GroupWords {
     uint32_t w[NG];   // NG = 2: K's, V's; NG = 1: K's in lanes below 32, else V's
@@ -78,19 +85,22 @@ struct Kv4GroupWords {
     __device__ __forceinline__ void load(const uint32_t *kp, const uint32_t *vp, int block,
                                          int lane) {
         if (NG == 2) {
-            w[0] = kp[64 * block + lane];
-            w[NG - 1] = vp[64 * block + lane];
+            const uint32_t at = 4u * (64 * block + lane);
+            w[0] = *reinterpret_cast<const uint32_t *>(reinterpret_cast<const char *>(kp) + at);
+            w[NG - 1] = *reinterpret_cast<const uint32_t *>(reinterpret_cast<const char *>(vp) + at);
         } else {
             w[0] = (lane < 32 ? kp : vp)[32 * block + (lane & 31)];
         }
     }
-    // K's words at to[0..], V's at to[32 NG..]; 0 for tokens at or behind n
-    __device__ __forceinline__ void put(uint32_t *to, int block, int n, int lane) {
+    // 0 for tokens at or behind n
+    __device__ __forceinline__ void put(BlockGroups<NG> &to, int block, int n, int lane) {
         const bool in = 32 * block + (NG == 2 ? lane >> 1 : lane & 31) < n;
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
             w[i] = in ? w[i] : 0u;
-            to[64 * i + lane] = w[i];
+            float *scale = &to.scale[0][0], *min = &to.min[0][0];
+            scale[64 * i + lane] = group_scale(w[i]);
+            min[64 * i + lane] = group_min(w[i]);
         }
     }
     // the lane's V word, or 0
@@ -106,7 +116,7 @@ void kv4_rows(RowsArgs a) {
     constexpr int LD = D + 4;
     __shared__ __attribute__((aligned(16))) float Os[kWaves][kRows][LD];
     __shared__ float Ms[kWaves][kRows], Ls[kWaves][kRows];
-    __shared__ __attribute__((aligned(16))) uint32_t Gs[kWaves][2][64 * NG];
+    __shared__ __attribute__((aligned(16))) BlockGroups<NG> Gs[kWaves][2];
 
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -156,27 +166,31 @@ void kv4_rows(RowsArgs a) {
     for (int i = 0; i < NB; ++i) o[i] = zero4();
 
     auto step = [&](int block, const Kv4Keys<D> &key, const Kv4Values<D> &val,
-                    Kv4GroupWords<NG> &words, uint32_t *groups) {
+                    Kv4GroupWords<NG> &words, BlockGroups<NG> &groups) {
         words.put(groups, block, mask.n, lane);
         __builtin_amdgcn_wave_barrier();   // one wave's LDS accesses stay in order
         f32x4 s[2];
-        key.scores(s, q, groups, c, g);
-        uint32_t vg[8 * NG];   // of the lane's octet
+        key.scores(s, q, groups.scale[0], groups.min[0], c, g);
+        float vs[8 * NG], vm[8 * NG];   // of the lane's octet
 #pragma unroll
         for (int i = 0; i < 2 * NG; ++i) {
-            const u32x4 v = *reinterpret_cast<const u32x4 *>(groups + (32 + 8 * g) * NG + 4 * i);
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(&groups.scale[1][8 * g * NG + 4 * i]);
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(&groups.min[1][8 * g * NG + 4 * i]);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) vg[4 * i + k] = v[k];
+            for (int k = 0; k < 4; ++k) {
+                vs[4 * i + k] = x[k];
+                vm[4 * i + k] = y[k];
+            }
         }
         if (32 * (block + 1) > all) {
-            // tokens out of sight: no score, and group words that add nothing
-            // (a token that is not finite must not reach rows that do not see it)
+            // tokens out of sight: no score, and groups that add nothing (a token
+            // that is not finite must not reach rows that do not see it)
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 if (32 * block + 8 * g + k >= limit) {
                     s[k >> 2][k & 3] = -INFINITY;
 #pragma unroll
-                    for (int i = 0; i < NG; ++i) vg[k * NG + i] = 0;
+                    for (int i = 0; i < NG; ++i) vs[k * NG + i] = vm[k * NG + i] = 0.f;
                 }
         }
         if (a.score != nullptr && in) {
@@ -219,9 +233,8 @@ void kv4_rows(RowsArgs a) {
             f16x8 part[NP];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const uint32_t gw = vg[k * NG + i];
-                x[k] = p[k] * group_scale(gw);
-                low[i] = fmaf(p[k], group_min(gw), low[i]);
+                x[k] = p[k] * vs[k * NG + i];
+                low[i] = fmaf(p[k], vm[k * NG + i], low[i]);
             }
             split_operand<NP>(part, x);
 #pragma unroll

@@ -112,30 +112,32 @@ struct Kv4Keys {
     static constexpr int NG = Kv4Dim<D>::kGroups, NW = D / 32;
     uint32_t w[2][NW];
 
-    // `words`: the head's region.  c = lane%16, g = lane/16.
+    // `words`: the head's region (below 4 GiB).  c = lane%16, g = lane/16.
     __device__ __forceinline__ void load(const uint32_t *words, int block, int c, int g) {
         typedef uint32_t wv __attribute__((ext_vector_type(NW)));
-        const int key = 32 * block + 8 * (c >> 2) + (c & 3);
+        const uint32_t at = (32 * block + 8 * (c >> 2) + (c & 3)) * (D / 8u) + g * NW;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const wv v = *reinterpret_cast<const wv *>(words + (size_t)(key + 4 * t) * (D / 8) +
-                                                       g * NW);
+            const wv v = *reinterpret_cast<const wv *>(
+                reinterpret_cast<const char *>(words) + (4 * at + 2u * t * D));
 #pragma unroll
             for (int i = 0; i < NW; ++i) w[t][i] = NW == 1 ? v[0] : v[i];
         }
     }
 
     // s[t][r] = score of token 8g + 4t + r for the lane's row, before the row's
-    // factor.  `group`: the block's group words in LDS, token k's at k * NG.
+    // factor.  `scale`, `low`: the block's group scales and minima in LDS, token
+    // k's at k * NG.
     template <int NP>
     __device__ __forceinline__ void scores(f32x4 (&s)[2], const Kv4Query<D, NP> &q,
-                                           const uint32_t *group, int c, int g) const {
+                                           const float *scale, const float *low, int c,
+                                           int g) const {
         f32x4 m[2][NG];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             // the minima's part: one product over the groups (sum is 0 behind them)
-            const uint32_t low = group[(8 * (c >> 2) + 4 * t + (c & 3)) * NG + g % NG];
-            s[t] = mfma16x16x4(group_min(low), q.sum, zero4());
+            s[t] = mfma16x16x4(low[(8 * (c >> 2) + 4 * t + (c & 3)) * NG + g % NG], q.sum,
+                               zero4());
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
                 m[t][gr] = zero4();
@@ -151,12 +153,13 @@ struct Kv4Keys {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int i = 0; i < NG; ++i) {   // words (8g + 4t) NG + 4i ..+3
-                const u32x4 v = *reinterpret_cast<const u32x4 *>(group + (8 * g + 4 * t) * NG + 4 * i);
+            for (int i = 0; i < NG; ++i) {   // (8g + 4t) NG + 4i ..+3
+                const f32x4 v = *reinterpret_cast<const f32x4 *>(scale + (8 * g + 4 * t) * NG +
+                                                                 4 * i);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int r = (4 * i + k) / NG, gr = (4 * i + k) % NG;
-                    s[t][r] = fmaf(group_scale(v[k]), m[t][gr][r], s[t][r]);
+                    s[t][r] = fmaf(v[k], m[t][gr][r], s[t][r]);
                 }
             }
     }

@@ -14,15 +14,16 @@ namespace mg {
 
 // How a call runs.  kv4_many from 64 rows a cache head on, with 256 rows a
 // workgroup where that gives every compute unit one, its tokens split over
-// workgroups where there are fewer.  Else kv4_rows, its tokens cut into chunks:
-// three workgroups fit a compute unit, and caches are seldom full, so up to 1,280
-// workgroups.  A split has at least 256 tokens.
+// workgroups where there are fewer.  Else kv4_rows, its tokens cut into chunks for
+// two workgroups on every compute unit (with 1,280 workgroups drafted rows took
+// 22.9 instead of 19.9 us, a long batch 51 either way: each workgroup prepares
+// its query rows and joins its waves).  A split has at least 256 tokens.
 Kv4Plan kv4_plan(const Kv4Attn &p, bool weights, bool bf16) {
     const int64_t heads = (int64_t)p.B * p.H, rows = kv4_rows(p);
     Kv4Plan plan = {};
     plan.rows = !bf16 || rows < 64 ? 16 : heads * ((rows + 255) / 256) >= 256 ? 256 : 128;
     const int64_t tiles = heads * ((rows + plan.rows - 1) / plan.rows);
-    const int64_t want = plan.rows == 16 ? 1280 : plan.rows == 256 ? 256 : 512;
+    const int64_t want = plan.rows == 256 ? 256 : 512;
     const int blocks = kv4_padded(p.L) / 32;
     plan.splits = (int)std::max<int64_t>(
         1, std::min({(want + tiles - 1) / tiles, (int64_t)64, (int64_t)blocks / 8}));
