@@ -5,10 +5,10 @@ Every function checks the tensors it is given, runs on the tensors' own
 device (which need not be the current one) and raises MgError on a non-MG_OK
 status.  A cache is a uint8 tensor of mg_kv4_cache_bytes(B, H, L, d) bytes.
 """
-import contextlib
+import functools
 
-from ._binding import (_alloc_stream, _check, _contract_id, _empty_bytes, _ptr,
-                       _stream_handle, FAST_BF16, load_library)
+from ._binding import (_alloc_stream, _check, _contract_id, _empty_bytes, _ptr, FAST_BF16,
+                       load_library)
 
 
 def _elem(contract):
@@ -16,65 +16,64 @@ def _elem(contract):
     return torch.bfloat16 if contract == FAST_BF16 else torch.float32
 
 
-def _need(name, t, dtype, shape, device):
-    """`t` must be a contiguous tensor of `dtype` and `shape` (None: any) on `device`."""
-    if not t.is_cuda:
-        raise ValueError("%s must be a GPU tensor" % name)
-    if t.device != device:
-        raise ValueError("%s is on %s, the others on %s" % (name, t.device, device))
-    if t.dtype != dtype:
-        raise ValueError("%s has dtype %s, expected %s" % (name, t.dtype, dtype))
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
-    if not t.is_contiguous():
+def _need(dev, named):
+    """Every (name, tensor, dtype, shape) of `named` that is not None must be a
+    contiguous tensor of that dtype and shape (None: any) on GPU `dev`."""
+    if dev < 0:
+        raise ValueError("%s must be a GPU tensor" % named[0][0])
+    for name, t, dtype, shape in named:
+        if t is None or (t.get_device() == dev and t.dtype is dtype and
+                         (shape is None or t.shape == shape) and t.is_contiguous()):
+            continue
+        if not t.is_cuda:
+            raise ValueError("%s must be a GPU tensor" % name)
+        if t.get_device() != dev:
+            raise ValueError("%s is on %s, the others on cuda:%d" % (name, t.device, dev))
+        if t.dtype is not dtype:
+            raise ValueError("%s has dtype %s, expected %s" % (name, t.dtype, dtype))
+        if shape is not None and tuple(t.shape) != tuple(shape):
+            raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
         raise ValueError("%s must be contiguous" % name)
 
 
-def _need_cache(name, cache, B, H, L, d, device):
-    import torch
-    _need(name, cache, torch.uint8, None, device)
-    need = mg_kv4_cache_bytes(B, H, L, d)
-    if need == 0:   # let the library say why
-        return
+def _need_room(cache, B, H, L, d):
+    need = mg_kv4_cache_bytes(B, H, L, d)   # 0 for bad sizes: the library says why
     if cache.numel() < need:
-        raise ValueError("%s has %d bytes, a cache of B=%d H=%d L=%d d=%d needs %d"
-                         % (name, cache.numel(), B, H, L, d, need))
+        raise ValueError("the cache has %d bytes, B=%d H=%d L=%d d=%d needs %d"
+                         % (cache.numel(), B, H, L, d, need))
 
 
-def _need_lens(named, B, device):
+def _call(dev, stream, function, *args):
+    """function(*args, stream handle) with the tensors' GPU the current one; a
+    given stream must be that GPU's."""
     import torch
-    for name, t in named:
-        if t is not None:
-            _need(name, t, torch.int32, (B,), device)
-
-
-@contextlib.contextmanager
-def _on(device, stream):
-    """Make `device` the current one for the launch; a given stream must be its."""
-    import torch
-    if stream is not None and stream.device != device:
-        raise ValueError("the stream belongs to %s, the tensors to %s" % (stream.device, device))
-    if device.index == torch.cuda.current_device():
-        yield
+    if stream is not None and stream.device.index != dev:
+        raise ValueError("the stream belongs to %s, the tensors to cuda:%d" % (stream.device, dev))
+    handle = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if dev == torch.cuda.current_device():
+        _check(function(*args, handle))
     else:
-        with torch.cuda.device(device):
-            yield
+        with torch.cuda.device(dev):
+            _check(function(*args, handle))
 
 
+@functools.lru_cache(maxsize=256)
 def mg_kv4_cache_bytes(B, H, L, d):
     """Bytes of a cache of B sequences, H heads, L tokens; 0 for invalid sizes."""
     return int(load_library().mg_kv4_cache_bytes(int(B), int(H), int(L), int(d)))
 
 
-def _move(K, V, cache, start, count, L, contract):
+def _move(K, V, cache, start, count, L, contract, weight=None):
+    import torch
     if K.dim() != 4:
         raise ValueError("K must be [B,H,n,d]")
     B, H, n, d = K.shape
-    for what, t in (("K", K), ("V", V)):
-        _need(what, t, _elem(contract), K.shape, K.device)
-    _need_cache("cache", cache, B, H, L, d, K.device)
-    _need_lens((("start", start), ("count", count)), B, K.device)
-    return B, H, n, d
+    dev, elem = K.get_device(), _elem(contract)
+    _need(dev, (("K", K, elem, K.shape), ("V", V, elem, K.shape),
+                ("cache", cache, torch.uint8, None), ("start", start, torch.int32, (B,)),
+                ("count", count, torch.int32, (B,)), ("weight", weight, torch.float32, (B, H, L))))
+    _need_room(cache, B, H, L, d)
+    return dev, B, H, n, d
 
 
 def mg_kv4_append(K, V, cache, start=None, count=None, *, L, weight=None, contract=FAST_BF16,
@@ -82,24 +81,19 @@ def mg_kv4_append(K, V, cache, start=None, count=None, *, L, weight=None, contra
     """Write rows j < count[b] of K, V [B,H,n,d] as tokens start[b] + j of a
     cache with room for L tokens (count None: n; start None: 0); `weight`
     [B,H,L], if given, is cleared for them."""
-    import torch
-    lib, c = load_library(), _contract_id(contract)
-    B, H, n, d = _move(K, V, cache, start, count, L, c)
-    if weight is not None:
-        _need("weight", weight, torch.float32, (B, H, L), K.device)
-    with _on(K.device, stream):
-        _check(lib.mg_kv4_append(_ptr(K), _ptr(V), _ptr(cache), _ptr(weight), _ptr(start),
-                                 _ptr(count), B, H, n, int(L), d, c, _stream_handle(stream)))
+    c = _contract_id(contract)
+    dev, B, H, n, d = _move(K, V, cache, start, count, L, c, weight)
+    _call(dev, stream, load_library().mg_kv4_append, K.data_ptr(), V.data_ptr(),
+          cache.data_ptr(), _ptr(weight), _ptr(start), _ptr(count), B, H, n, L, d, c)
 
 
 def mg_kv4_read(cache, K, V, start=None, count=None, *, L, contract=FAST_BF16, stream=None):
     """Read tokens start[b] + j, j < count[b], back into rows j of K, V
     [B,H,n,d]; other rows are left as they were."""
-    lib, c = load_library(), _contract_id(contract)
-    B, H, n, d = _move(K, V, cache, start, count, L, c)
-    with _on(K.device, stream):
-        _check(lib.mg_kv4_read(_ptr(cache), _ptr(K), _ptr(V), _ptr(start), _ptr(count), B, H, n,
-                               int(L), d, c, _stream_handle(stream)))
+    c = _contract_id(contract)
+    dev, B, H, n, d = _move(K, V, cache, start, count, L, c)
+    _call(dev, stream, load_library().mg_kv4_read, cache.data_ptr(), K.data_ptr(), V.data_ptr(),
+          _ptr(start), _ptr(count), B, H, n, L, d, c)
 
 
 def mg_attn_fwd_kv4_workspace_bytes(B, Hq, H, Lq, L, d, weights=False, contract=FAST_BF16):
@@ -114,32 +108,28 @@ def mg_attn_fwd_kv4(Q, cache, O, LSE, key_len=None, q_len=None, *, H, L, causal,
     probabilities.  `workspace` as for mg_attn_bwd (sized by
     mg_attn_fwd_kv4_workspace_bytes; allocated here with torch when None)."""
     import torch
-    lib, c = load_library(), _contract_id(contract)
+    c = _contract_id(contract)
     if Q.dim() != 4:
         raise ValueError("Q must be [B,Hq,Lq,d]")
     B, Hq, Lq, d = Q.shape
-    dev = Q.device
-    for name, t in (("Q", Q), ("O", O)):
-        _need(name, t, _elem(c), Q.shape, dev)
-    _need("LSE", LSE, torch.float32, Q.shape[:3], dev)
-    _need_cache("cache", cache, B, H, L, d, dev)
-    _need_lens((("key_len", key_len), ("q_len", q_len)), B, dev)
-    if weight is not None:
-        _need("weight", weight, torch.float32, (B, H, L), dev)
-    with _on(dev, stream):
-        if workspace is None:
-            need = mg_attn_fwd_kv4_workspace_bytes(B, Hq, H, Lq, L, d, weight is not None, c)
-            if need > 0:
-                workspace = _empty_bytes(need, dev, stream)
-        nbytes = 0
-        if workspace is not None:
-            if workspace.device != dev or not workspace.is_contiguous():
-                raise ValueError("workspace must be contiguous and on %s" % dev)
-            nbytes = workspace.numel() * workspace.element_size()
-        _check(lib.mg_attn_fwd_kv4(_ptr(Q), _ptr(cache), _ptr(O), _ptr(LSE), _ptr(weight),
-                                   _ptr(key_len), _ptr(q_len), B, Hq, int(H), Lq, int(L), d,
-                                   int(bool(causal)), float(scale), c, _ptr(workspace), nbytes,
-                                   _stream_handle(stream)))
+    dev, elem = Q.get_device(), _elem(c)
+    _need(dev, (("Q", Q, elem, Q.shape), ("O", O, elem, Q.shape),
+                ("LSE", LSE, torch.float32, Q.shape[:3]), ("cache", cache, torch.uint8, None),
+                ("key_len", key_len, torch.int32, (B,)), ("q_len", q_len, torch.int32, (B,)),
+                ("weight", weight, torch.float32, (B, H, L))))
+    _need_room(cache, B, H, L, d)
+    if workspace is None:
+        need = mg_attn_fwd_kv4_workspace_bytes(B, Hq, H, Lq, L, d, weight is not None, c)
+        if need > 0:
+            workspace = _empty_bytes(need, Q.device, stream)
+    nbytes = 0
+    if workspace is not None:
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous and on cuda:%d" % dev)
+        nbytes = workspace.numel() * workspace.element_size()
+    _call(dev, stream, load_library().mg_attn_fwd_kv4, Q.data_ptr(), cache.data_ptr(),
+          O.data_ptr(), LSE.data_ptr(), _ptr(weight), _ptr(key_len), _ptr(q_len), B, Hq, H, Lq,
+          L, d, 1 if causal else 0, scale, c, _ptr(workspace), nbytes)
 
 
 def mg_kv4_evict(cache, weight, index, new_len, key_len=None, *, d, recent, out_cache=None,
@@ -149,26 +139,25 @@ def mg_kv4_evict(cache, weight, index, new_len, key_len=None, *, d, recent, out_
     out_weight; index [B,H,keep] gets where they were (-1 behind the last) and
     new_len [B] how many stay (it may be key_len itself)."""
     import torch
-    lib = load_library()
     if weight.dim() != 3 or index.dim() != 3:
         raise ValueError("weight must be [B,H,L] and index [B,H,keep]")
     B, H, L = weight.shape
-    keep, dev = index.shape[2], weight.device
+    keep, dev = index.shape[2], weight.get_device()
     if (out_cache is None) != (out_weight is None):
         raise ValueError("give out_cache and out_weight together")
     if out_cache is None:
         out_cache, out_weight = cache, weight
-    for name, t in (("weight", weight), ("out_weight", out_weight)):
-        _need(name, t, torch.float32, (B, H, L), dev)
-    _need("index", index, torch.int32, (B, H, keep), dev)
-    _need("new_len", new_len, torch.int32, (B,), dev)
-    for name, t in (("cache", cache), ("out_cache", out_cache)):
-        _need_cache(name, t, B, H, L, d, dev)
-    _need_lens((("key_len", key_len),), B, dev)
-    with _on(dev, stream):
-        _check(lib.mg_kv4_evict(_ptr(cache), _ptr(weight), _ptr(out_cache), _ptr(out_weight),
-                                _ptr(index), _ptr(new_len), _ptr(key_len), B, H, L, int(d), keep,
-                                int(recent), _stream_handle(stream)))
+    _need(dev, (("weight", weight, torch.float32, (B, H, L)),
+                ("out_weight", out_weight, torch.float32, (B, H, L)),
+                ("index", index, torch.int32, (B, H, keep)),
+                ("new_len", new_len, torch.int32, (B,)),
+                ("key_len", key_len, torch.int32, (B,)),
+                ("cache", cache, torch.uint8, None), ("out_cache", out_cache, torch.uint8, None)))
+    _need_room(cache, B, H, L, d)
+    _need_room(out_cache, B, H, L, d)
+    _call(dev, stream, load_library().mg_kv4_evict, cache.data_ptr(), weight.data_ptr(),
+          out_cache.data_ptr(), out_weight.data_ptr(), index.data_ptr(), new_len.data_ptr(),
+          _ptr(key_len), B, H, L, d, keep, recent)
 
 
 # ------------------------------------------------------------ conveniences --

@@ -4,14 +4,16 @@
 // the older tokens by radix selection (11 + 11 + 10 bits of a key whose order is
 // the weights', LDS histograms of whole-number counts, so the result does not
 // depend on the order of the counting), then writes the indices of what stays
-// in order: each wave counts its share, one scan over the waves places it.  Of
-// the tokens that equal the last weight, the first ones stay.
+// in order: counts of every 64 tokens, one scan over them, places.  Of the tokens
+// that equal the last weight, the first ones stay.  Weights are read once and kept
+// in registers for sequences up to 32,768 tokens; counting takes a wave's most
+// common first digit in one addition (many tokens share a small weight).
 //
 // kv4_compact: moves rows to where select's indices put them.  A workgroup owns
-// a column of the cache (16 bytes of the K rows, 64 bytes of the V octets, or
-// the group words and weights).  index[p] >= p, so going through p upwards,
-// reading a stretch before any of it is written, is safe in place; into another
-// cache, stretches are shared out over workgroups.
+// whole 128-byte columns of the cache (the K rows, 128 bytes of the V octets, or the
+// group words and weights).  index[p] >= p, so going through p upwards, reading a
+// stretch of 1,024 tokens before any of it is written, is safe in place; into
+// another cache, stretches are shared out over workgroups.
 #include "cdiv.h"
 #include "kv4_device.h"
 #include "kv4_launch.h"
@@ -30,17 +32,48 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// Inclusive sum over the wave's lanes.
+__device__ __forceinline__ uint32_t scan_wave(uint32_t v, int lane) {
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        const uint32_t x = __shfl_up((int)v, m, 64);
+        if (lane >= m) v += x;
+    }
+    return v;
+}
+// Inclusive sum over the workgroup's threads; sums: kWaves words of LDS.
+__device__ __forceinline__ uint32_t scan_group(uint32_t v, uint32_t *sums, int lane, int wave) {
+    v = scan_wave(v, lane);
+    if (lane == 63) sums[wave] = v;
+    __syncthreads();
+    uint32_t before = 0;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) before += k < wave ? sums[k] : 0u;
+    __syncthreads();
+    return v + before;
+}
+
+// SLABS: 1,024 tokens each, the most a sequence has; 0: any number, not kept in
+// registers.
+template <int SLABS>
 __global__ __launch_bounds__(kThreads)
 void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
                 const int32_t *key_len, int H, int L, int keep, int recent) {
     __shared__ uint32_t hist[kBins];
-    __shared__ uint32_t above[kWaves], equal[kWaves];
+    __shared__ uint32_t sums[kWaves];
     __shared__ uint32_t found[2];   // digit, and how many of its bin stay
+    __shared__ uint32_t counts[SLABS > 0 ? SLABS * kWaves : 1];
     const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n = optional_len(key_len, bh / H, L);
     const float *w = weight + (size_t)bh * L;
     int32_t *to = index + (size_t)bh * keep;
+    constexpr int KEYS = SLABS > 0 ? SLABS : 1;
+    float raw[KEYS];
+    if (SLABS > 0) {   // asked for before the length is known
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) raw[i] = w[min(kThreads * i + tid, L - 1)];
+    }
+    const int n = optional_len(key_len, bh / H, L);
     if (n <= keep) {
         for (int p = tid; p < keep; p += kThreads) to[p] = p < n ? p : -1;
         return;
@@ -49,6 +82,22 @@ void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
     uint32_t want = keep - recent;   // of the old tokens; old > want
     for (int p = tid; p < recent; p += kThreads) to[want + p] = old + p;
     if (want == 0) return;
+    uint32_t kept[KEYS];
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) kept[i] = SLABS > 0 ? weight_key(raw[i]) : 0u;
+    // token and key of the thread's i-th turn
+    const int turns = SLABS > 0 ? KEYS : (old + kThreads - 1) / kThreads;
+    auto each = [&](auto &&f) {
+        if (SLABS > 0) {
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i) f(i, kThreads * i + tid, kept[i]);
+        } else {
+            for (int i = 0; i < turns; ++i) {
+                const int j = kThreads * i + tid;
+                f(i, j, weight_key(w[min(j, L - 1)]));
+            }
+        }
+    };
 
     // the key of rank `want` from the top, digit by digit
     uint32_t prefix = 0;
@@ -56,38 +105,28 @@ void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
         const int bits = pass == 2 ? 10 : 11, below = shift - bits;
+        const uint32_t mask = (1u << bits) - 1;
         for (int k = tid; k < kBins; k += kThreads) hist[k] = 0;
         __syncthreads();
-        for (int j = tid; j < old; j += kThreads) {
-            const uint32_t key = weight_key(w[j]);
-            if (shift == 32 || key >> shift == prefix >> shift)
-                atomicAdd(&hist[(key >> below) & ((1u << bits) - 1)], 1u);
-        }
+        each([&](int, int j, uint32_t key) {
+            const bool in = j < old && (pass == 0 || (key ^ prefix) >> shift == 0);
+            const uint64_t votes = __ballot(in);
+            if (votes == 0) return;
+            const uint32_t digit = (key >> below) & mask;
+            const uint32_t first = __builtin_amdgcn_readlane(digit, __builtin_ctzll(votes));
+            const uint64_t same = __ballot(in && digit == first);
+            if (in && digit != first) atomicAdd(&hist[digit], 1u);
+            if (lane == 0) atomicAdd(&hist[first], (uint32_t)__popcll(same));
+        });
         __syncthreads();
-        if (wave == 0) {
-            // lanes take bins from the top, 32 each
-            uint32_t mine = 0;
-            const int hi = kBins - 1 - 32 * lane;
-            for (int k = 0; k < 32; ++k) mine += hist[hi - k];
-            uint32_t before = mine;
-#pragma unroll
-            for (int m = 1; m < 64; m *= 2) {
-                const uint32_t v = __shfl_up((int)before, m, 64);
-                if (lane >= m) before += v;
-            }
-            before -= mine;
-            if (before < want && before + mine >= want) {
-                uint32_t left = want - before;
-                for (int k = 0; k < 32; ++k) {
-                    const uint32_t h = hist[hi - k];
-                    if (left <= h) {
-                        found[0] = hi - k;
-                        found[1] = left;
-                        break;
-                    }
-                    left -= h;
-                }
-            }
+        // threads take bins from the top, two each
+        const int bin = kBins - 1 - 2 * tid;
+        const uint32_t h0 = hist[bin], h1 = hist[bin - 1];
+        const uint32_t upto = scan_group(h0 + h1, sums, lane, wave), before = upto - h0 - h1;
+        if (before < want && upto >= want) {
+            const bool second = before + h0 < want;
+            found[0] = second ? bin - 1 : bin;
+            found[1] = want - before - (second ? h0 : 0u);
         }
         __syncthreads();
         prefix |= found[0] << below;
@@ -96,32 +135,55 @@ void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
     }
 
     // every key above prefix stays, and the first `want` that equal it
-    const int share = (old + kWaves - 1) / kWaves, j0 = wave * share, j1 = min(old, j0 + share);
-    uint32_t up = 0, same = 0;
-    for (int j = j0; j < j1; j += 64) {
-        const uint32_t key = j + lane < j1 ? weight_key(w[j + lane]) : 0;
-        up += __popcll(__ballot(j + lane < j1 && key > prefix));
-        same += __popcll(__ballot(j + lane < j1 && key == prefix));
-    }
-    if (lane == 0) {
-        above[wave] = up;
-        equal[wave] = same;
-    }
-    __syncthreads();
-    up = same = 0;
-    for (int k = 0; k < wave; ++k) {
-        up += above[k];
-        same += equal[k];
-    }
     const uint64_t lower = (1ull << lane) - 1;
-    for (int j = j0; j < j1; j += 64) {
-        const bool in = j + lane < j1;
-        const uint32_t key = in ? weight_key(w[j + lane]) : 0;
-        const uint64_t gt = __ballot(in && key > prefix), eq = __ballot(in && key == prefix);
+    auto place = [&](int j, uint32_t key, uint64_t gt, uint64_t eq, uint32_t up, uint32_t same) {
         const uint32_t u = up + __popcll(gt & lower), s = same + __popcll(eq & lower);
-        if (in && (key > prefix || (key == prefix && s < want))) to[u + min(s, want)] = j + lane;
-        up += __popcll(gt);
-        same += __popcll(eq);
+        if (j < old && (key > prefix || (key == prefix && s < want))) to[u + min(s, want)] = j;
+    };
+    if constexpr (SLABS > 0) {
+        // counts of each 64 tokens: above in the upper half, equal in the lower
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            const int j = kThreads * i + tid;
+            const uint32_t gt = __popcll(__ballot(j < old && kept[i] > prefix));
+            const uint32_t eq = __popcll(__ballot(j < old && kept[i] == prefix));
+            if (lane == 0) counts[kWaves * i + wave] = gt << 16 | eq;
+        }
+        __syncthreads();
+        const uint32_t mine = tid < SLABS * kWaves ? counts[tid] : 0u;
+        const uint32_t upto = scan_group(mine, sums, lane, wave);
+        if (tid < SLABS * kWaves) counts[tid] = upto - mine;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            const int j = kThreads * i + tid;
+            const uint64_t gt = __ballot(j < old && kept[i] > prefix);
+            const uint64_t eq = __ballot(j < old && kept[i] == prefix);
+            const uint32_t at = counts[kWaves * i + wave];
+            place(j, kept[i], gt, eq, at >> 16, at & 0xffffu);
+        }
+    } else {
+        // the same, a slab at a time
+        uint32_t up = 0, same = 0;
+#pragma unroll 1
+        for (int i = 0; i < turns; ++i) {
+            const int j = kThreads * i + tid;
+            const uint32_t key = weight_key(w[min(j, L - 1)]);
+            const uint64_t gt = __ballot(j < old && key > prefix);
+            const uint64_t eq = __ballot(j < old && key == prefix);
+            if (lane == 0) sums[wave] = (uint32_t)__popcll(gt) << 16 | (uint32_t)__popcll(eq);
+            __syncthreads();
+            uint32_t here = 0, all = 0;
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k) {
+                here += k < wave ? sums[k] : 0u;
+                all += sums[k];
+            }
+            place(j, key, gt, eq, up + (here >> 16), same + (here & 0xffffu));
+            up += all >> 16;
+            same += all & 0xffffu;
+            __syncthreads();
+        }
     }
 }
 
@@ -135,84 +197,77 @@ struct CompactArgs {
     int H, L, Lp, keep, in_place;
 };
 
-// One pass takes kRowsPass tokens of a K column or the side words, or
-// kOctetsPass octets of a V column.
-constexpr int kCompactThreads = 512;
+constexpr int kStretch = 1024;   // tokens read before any is written
 
 template <int D>
-__global__ __launch_bounds__(kCompactThreads)
+__global__ __launch_bounds__(kThreads)
 void kv4_compact(CompactArgs a) {
     constexpr int NG = Kv4Dim<D>::kGroups;
-    constexpr int KC = D / 32, VC = D / 16;   // 16-byte K columns, 64-byte V columns
-    const int bh = blockIdx.x / (KC + VC + 1), col = blockIdx.x - bh * (KC + VC + 1);
+    constexpr int VC = D / 32, COLS = VC + 2;   // V's columns, K, the rest
+    const int bh = blockIdx.x / COLS, col = blockIdx.x - bh * COLS;
     const int b = bh / a.H, tid = threadIdx.x;
     const int n = min(optional_len(a.key_len, b, a.L), a.keep);
     const int32_t *index = a.index + (size_t)bh * a.keep;
-    if (a.new_len != nullptr && bh % a.H == 0 && col == 0 && blockIdx.y == 0 && tid == 0)
-        a.new_len[b] = n;
+    if (bh % a.H == 0 && col == 0 && blockIdx.y == 0 && tid == 0) a.new_len[b] = n;
     const size_t head = (size_t)bh * a.Lp;
 
-    if (col < KC) {
-        const u32x4 *in = reinterpret_cast<const u32x4 *>(a.in.k + head * (D / 8)) + col;
-        u32x4 *out = reinterpret_cast<u32x4 *>(a.out.k + head * (D / 8)) + col;
-        for (int p0 = blockIdx.y * kCompactThreads; p0 < n; p0 += gridDim.y * kCompactThreads) {
-            const int p = p0 + tid;
-            u32x4 v;
-            if (p < n) v = in[(size_t)index[p] * KC];
-            if (a.in_place) __syncthreads();
-            if (p < n) out[(size_t)p * KC] = v;
-        }
-    } else if (col < KC + VC) {
-        // a thread makes four words of an octet: eight nibbles from eight rows
-        const int q = 4 * (col - KC) + (tid & 3);   // of D / 4
-        const u32x4 *in = reinterpret_cast<const u32x4 *>(a.in.v + head / 8 * D) + q;
-        u32x4 *out = reinterpret_cast<u32x4 *>(a.out.v + head / 8 * D) + q;
-        const int octets = (n + 7) / 8;
-        constexpr int PASS = kCompactThreads / 4;
-        for (int o0 = blockIdx.y * PASS; o0 < octets; o0 += gridDim.y * PASS) {
-            const int o = o0 + (tid >> 2);
+    for (int p0 = blockIdx.y * kStretch; p0 < n; p0 += gridDim.y * kStretch) {
+        if (col < VC) {
+            // a thread makes four words of an octet: eight nibbles from eight rows
+            const int q = 8 * col + (tid & 7);   // of D / 4
+            const u32x4 *in = reinterpret_cast<const u32x4 *>(a.in.v + head / 8 * D) + q;
+            u32x4 *out = reinterpret_cast<u32x4 *>(a.out.v + head / 8 * D) + q;
+            const int o = p0 / 8 + (tid >> 3);
             u32x4 v = {0u, 0u, 0u, 0u};
-            if (o < octets) {
+            if (8 * o < n) {
                 uint32_t mask = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (8 * o + e < n) {
-                        const int j = index[8 * o + e];
-                        v |= ((in[(size_t)(j >> 3) * (D / 4)] >> (uint32_t)(4 * (j & 7))) & 15u)
-                             << (uint32_t)(4 * e);
-                        mask |= 15u << (4 * e);
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    const bool there = 8 * o + e < n;
+                    const int j = index[there ? 8 * o + e : 8 * o];
+                    const u32x4 x = in[(size_t)(j >> 3) * (D / 4)] >> (uint32_t)(4 * (j & 7));
+                    mask |= there ? 15u << (4 * e) : 0u;
+                    v |= (x & (there ? 15u : 0u)) << (uint32_t)(4 * e);
+                }
                 if (mask != 0xffffffffu) v |= out[(size_t)o * (D / 4)] & ~mask;
             }
             if (a.in_place) __syncthreads();
-            if (o < octets) out[(size_t)o * (D / 4)] = v;
-        }
-    } else {
-        const uint32_t *ik = a.in.kp + head * NG, *iv = a.in.vp + head * NG;
-        uint32_t *ok = a.out.kp + head * NG, *ov = a.out.vp + head * NG;
-        const float *iw = a.weight + (size_t)bh * a.L;
-        float *ow = a.out_weight + (size_t)bh * a.L;
-        for (int p0 = blockIdx.y * kCompactThreads; p0 < n; p0 += gridDim.y * kCompactThreads) {
-            const int p = p0 + tid;
-            uint32_t k[NG], v[NG];
-            float w = 0.f;
-            if (p < n) {
-                const int j = index[p];
+            if (8 * o < n) out[(size_t)o * (D / 4)] = v;
+        } else if (col == VC) {
+            // D / 2 bytes a token, 16 a thread
+            constexpr int T = D / 32, TURNS = kStretch * T / kThreads;
+            const u32x4 *in = reinterpret_cast<const u32x4 *>(a.in.k + head * (D / 8));
+            u32x4 *out = reinterpret_cast<u32x4 *>(a.out.k + head * (D / 8));
+            u32x4 v[TURNS];
 #pragma unroll
-                for (int i = 0; i < NG; ++i) {
-                    k[i] = ik[(size_t)j * NG + i];
-                    v[i] = iv[(size_t)j * NG + i];
-                }
-                w = iw[j];
+            for (int u = 0; u < TURNS; ++u) {
+                const int p = p0 + (u * kThreads + tid) / T;
+                v[u] = in[(size_t)index[min(p, n - 1)] * T + tid % T];
             }
+            if (a.in_place) __syncthreads();
+#pragma unroll
+            for (int u = 0; u < TURNS; ++u) {
+                const int p = p0 + (u * kThreads + tid) / T;
+                if (p < n) out[(size_t)p * T + tid % T] = v[u];
+            }
+        } else {
+            const int p = p0 + tid, j = index[min(p, n - 1)];
+            const uint32_t *ik = a.in.kp + (head + j) * NG, *iv = a.in.vp + (head + j) * NG;
+            uint32_t k[NG], v[NG];
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                k[i] = ik[i];
+                v[i] = iv[i];
+            }
+            const float w = a.weight[(size_t)bh * a.L + j];
             if (a.in_place) __syncthreads();
             if (p < n) {
 #pragma unroll
                 for (int i = 0; i < NG; ++i) {
-                    ok[(size_t)p * NG + i] = k[i];
-                    ov[(size_t)p * NG + i] = v[i];
+                    a.out.kp[(head + p) * NG + i] = k[i];
+                    a.out.vp[(head + p) * NG + i] = v[i];
                 }
-                ow[p] = w;
+                a.out_weight[(size_t)bh * a.L + p] = w;
             }
         }
     }
@@ -220,10 +275,16 @@ void kv4_compact(CompactArgs a) {
 
 template <int D>
 hipError_t compact(const Kv4Evict &p, const CompactArgs &a, hipStream_t s) {
-    const int cols = D / 32 + D / 16 + 1;
-    const dim3 grid((unsigned)(p.B * p.H * cols),
-                    a.in_place ? 1u : (unsigned)cdiv(p.keep, kCompactThreads));
-    kv4_compact<D><<<grid, kCompactThreads, 0, s>>>(a);
+    const dim3 grid((unsigned)(p.B * p.H * (D / 32 + 2)),
+                    a.in_place ? 1u : (unsigned)cdiv(p.keep, kStretch));
+    kv4_compact<D><<<grid, kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <int SLABS>
+hipError_t select(const Kv4Evict &p, const float *weight, int32_t *index, hipStream_t s) {
+    kv4_select<SLABS><<<(unsigned)(p.B * p.H), kThreads, 0, s>>>(weight, index, p.key_len, p.H,
+                                                                 p.L, p.keep, p.recent);
     return hipGetLastError();
 }
 
@@ -231,9 +292,9 @@ hipError_t compact(const Kv4Evict &p, const CompactArgs &a, hipStream_t s) {
 
 hipError_t launch_kv4_select(const Kv4Evict &p, const float *weight, int32_t *index,
                              hipStream_t s) {
-    kv4_select<<<(unsigned)(p.B * p.H), kThreads, 0, s>>>(weight, index, p.key_len, p.H, p.L,
-                                                          p.keep, p.recent);
-    return hipGetLastError();
+    const int slabs = cdiv(p.L, kThreads);
+    return slabs <= 4 ? select<4>(p, weight, index, s) : slabs <= 12 ? select<12>(p, weight, index, s)
+         : slabs <= 32 ? select<32>(p, weight, index, s) : select<0>(p, weight, index, s);
 }
 
 hipError_t launch_kv4_compact(const Kv4Evict &p, const Kv4Cache<const uint32_t> &c,

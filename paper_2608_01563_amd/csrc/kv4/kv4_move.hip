@@ -53,52 +53,69 @@ __device__ __forceinline__ uint32_t join16(uint32_t x, uint32_t y) {
     return r[0] | r[1];
 }
 
-// The code of t = x - mn for scale sc > 0 and inv = 1 / sc: the quotient in
-// f32, and next to a border between two codes (ties are common among bf16
-// values) the side it falls on in 64 bits, ties to the even code.
-__device__ __forceinline__ uint32_t code_of(float x, float mn, float sc, float inv) {
-    const float q = (x - mn) * inv;
-    const float k = floorf(q), f = q - k;
-    float code = k + (f > 0.5f ? 1.f : 0.f);
-    if (fabsf(f - 0.5f) < 0x1p-16f) {
-        const double over = __builtin_fma(-(double)sc, (double)k + 0.5, (double)x - (double)mn);
-        code = k + (over > 0.0 || (over == 0.0 && ((int)k & 1)) ? 1.f : 0.f);
-    }
-    return (uint32_t)fminf(fmaxf(code, 0.f), 15.f);
-}
+// A lane holds PIECES pieces of PIECE consecutive channels of its token, piece i at
+// channel (8 i + c) PIECE: the eight lanes of a token read and write 128 (d = 32
+// bf16: 64) consecutive bytes at a time.
+template <typename T, int D>
+struct Pieces {
+    static constexpr int PIECE = 16 / (int)sizeof(T) < D / 8 ? 16 / (int)sizeof(T) : D / 8;
+    static constexpr int PIECES = D / 8 / PIECE, NG = Kv4Dim<D>::kGroups;
+    static_assert(PIECES % NG == 0, "a piece index belongs to one group");
+    static constexpr int PER = PIECES / NG;   // pieces a group
 
-// A lane's CH channels of one row: codes (0 where the lane holds no row) and,
-// in the first lane of a group, the group's word.
-template <int CH, int LANES>
-__device__ __forceinline__ uint32_t quantise(const float (&x)[CH], uint32_t (&code)[CH]) {
-    float lo = x[0], hi = x[0];
-    uint32_t top = 0;
+    static __device__ __forceinline__ int channel(int i, int c) { return (8 * i + c) * PIECE; }
+};
+
+// Codes of a lane's pieces of one row (as f32), and the groups' words.
+//
+// code = round((x - min) / scale), from a product with 1 / scale.  Next to a border
+// between two codes (ties are common among bf16 values) the side is settled
+// exactly, with the difference's rounding error, ties to the even code.
+template <typename T, int D>
+__device__ __forceinline__ void quantise(const float (&x)[Pieces<T, D>::PIECES][Pieces<T, D>::PIECE],
+                                         float (&code)[Pieces<T, D>::PIECES][Pieces<T, D>::PIECE],
+                                         uint32_t (&word)[Kv4Dim<D>::kGroups]) {
+    using P = Pieces<T, D>;
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-        lo = fminf(lo, x[i]);
-        hi = fmaxf(hi, x[i]);
-        top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);   // fmin and fmax skip NaN
+    for (int g = 0; g < P::NG; ++g) {
+        float lo = x[g * P::PER][0], hi = lo, odd = 0.f;   // odd: NaN where one is not finite
+#pragma unroll
+        for (int i = g * P::PER; i < (g + 1) * P::PER; ++i)
+#pragma unroll
+            for (int k = 0; k < P::PIECE; ++k) {
+                lo = fminf(lo, x[i][k]);
+                hi = fmaxf(hi, x[i][k]);
+                odd = fmaf(x[i][k], 0.f, odd);
+            }
+#pragma unroll
+        for (int m = 1; m < 8; m *= 2) {
+            lo = fminf(lo, __shfl_xor(lo, m, 64));
+            hi = fmaxf(hi, __shfl_xor(hi, m, 64));
+            odd += __shfl_xor(odd, m, 64);
+        }
+        const uint32_t mb = f32_to_bf16_rne(lo);
+        uint32_t sb = f32_to_bf16_rne((hi - lo) / 15.f);
+        if (sb < 0x0080u) sb = 0;   // below the smallest normal
+        const float mn = bf16_to_f32((uint16_t)mb), sc = bf16_to_f32((uint16_t)sb);
+        const bool good = odd == 0.f && fabsf(mn) < INFINITY && sc < INFINITY;
+        const bool flat = !good || sb == 0;
+        const float inv = flat ? 0.f : 1.f / sc, from = flat ? 0.f : mn;
+        word[g] = good ? sb << 16 | mb : 0x7fc07fc0u;
+#pragma unroll
+        for (int i = g * P::PER; i < (g + 1) * P::PER; ++i)
+#pragma unroll
+            for (int k = 0; k < P::PIECE; ++k) {
+                const float t = x[i][k] - from, q = t * inv;
+                float y = rintf(q);
+                if (fabsf(q - y) > 0.5f - 0x1p-16f) {
+                    const float f = floorf(q), b = t - x[i][k];
+                    const float lost = (x[i][k] - (t - b)) - (from + b);   // t + lost = x - min
+                    const float over = (t - sc * (f + 0.5f)) + lost;       // both exact
+                    y = f + (over > 0.f || (over == 0.f && ((int)f & 1)) ? 1.f : 0.f);
+                }
+                code[i][k] = __builtin_amdgcn_fmed3f(y, 0.f, 15.f);   // (NaN: 0)
+            }
     }
-#pragma unroll
-    for (int m = 1; m < LANES; m *= 2) {
-        lo = fminf(lo, __shfl_xor(lo, m, 64));
-        hi = fmaxf(hi, __shfl_xor(hi, m, 64));
-        top = max(top, (uint32_t)__shfl_xor((int)top, m, 64));
-    }
-    const uint32_t mb = f32_to_bf16_rne(lo);
-    uint32_t sb = f32_to_bf16_rne((hi - lo) / 15.f);
-    if (sb < 0x0080u) sb = 0;   // below the smallest normal
-    const float mn = bf16_to_f32((uint16_t)mb), sc = bf16_to_f32((uint16_t)sb);
-    const bool good = top < 0x7f800000u && fabsf(mn) < INFINITY && sc < INFINITY;
-    if (!good || sb == 0) {
-#pragma unroll
-        for (int i = 0; i < CH; ++i) code[i] = 0;
-        return good ? mb : 0x7fc07fc0u;
-    }
-    const float inv = 1.f / sc;
-#pragma unroll
-    for (int i = 0; i < CH; ++i) code[i] = code_of(x[i], mn, sc, inv);
-    return sb << 16 | mb;
 }
 
 template <typename T, int D>
@@ -108,47 +125,58 @@ void kv4_append(const T *__restrict__ K, const T *__restrict__ V, uint32_t *__re
                 float *__restrict__ weight, const int32_t *__restrict__ start,
                 const int32_t *__restrict__ count, int B, int H, int n, int L, int Lp,
                 int octets) {
-    constexpr int CH = D / 8, NG = Kv4Dim<D>::kGroups, LANES = 8 / NG;
+    using P = Pieces<T, D>;
+    constexpr int CH = D / 8, NG = P::NG, PIECE = P::PIECE;
     Octet o;
     if (!take_octet(&o, B, H, n, L, octets, start, count)) return;
     const int lane = threadIdx.x & 63, e = lane >> 3, c = lane & 7;
     const int p = o.pos + e, j = p - o.at;
     const bool there = j >= 0 && j < o.rows;   // rows are clamped to positions below L
-    const size_t row = ((size_t)o.bh * n + (there ? j : 0)) * D + c * CH;
-    float x[CH];
-    uint32_t code[CH];
-
-    // K: the lane's own words
-    load_row(x, K + row);
-    uint32_t word = quantise<CH, LANES>(x, code);
-    const size_t tok = (size_t)o.bh * Lp + p;
-    uint32_t w[2] = {0, 0};
+    const size_t row = ((size_t)o.bh * n + (there ? j : 0)) * D;
+    float x[P::PIECES][PIECE], y[P::PIECES][PIECE], code[P::PIECES][PIECE];
+    uint32_t word[NG];
 #pragma unroll
-    for (int i = 0; i < CH; ++i) w[i >> 3] |= code[i] << (4 * (i & 7));
-    if (CH == 4) w[0] |= (uint32_t)__shfl_xor((int)w[0], 1, 64) << 16;   // even lanes: both halves
-    if (there) {
-        if (CH >= 8 || (c & 1) == 0) kw[tok * (D / 8) + k_word<D>(c * CH / 8)] = w[0];
-        if (CH == 16) kw[tok * (D / 8) + k_word<D>(2 * c + 1)] = w[1];
-        if (c % LANES == 0) kp[tok * NG + c / LANES] = word;
-        if (weight != nullptr && c == 0) weight[(size_t)o.bh * L + p] = 0.f;
+    for (int i = 0; i < P::PIECES; ++i) load_row(x[i], K + row + P::channel(i, c));
+#pragma unroll
+    for (int i = 0; i < P::PIECES; ++i) load_row(y[i], V + row + P::channel(i, c));
+
+    // K: words of 8 channels, a lane's own or, of 4 each, with its neighbour
+    quantise<T, D>(x, code, word);
+    const size_t tok = (size_t)o.bh * Lp + p;
+#pragma unroll
+    for (int i = 0; i < P::PIECES; ++i) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int k = 0; k < PIECE; ++k) w |= (uint32_t)code[i][k] << (4 * k);
+        if (PIECE == 4) w |= (uint32_t)__shfl_xor((int)w, 1, 64) << 16;   // in even lanes
+        if (there && (PIECE == 8 || (c & 1) == 0))
+            kw[tok * (D / 8) + k_word<D>(P::channel(i, c) / 8)] = w;
+    }
+    if (there && c == 0) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) kp[tok * NG + g] = word[g];
+        if (weight != nullptr) weight[(size_t)o.bh * L + p] = 0.f;
     }
 
     // V: a channel's eight tokens in one word
-    load_row(x, V + row);
-    word = quantise<CH, LANES>(x, code);
-    if (there && c % LANES == 0) vp[tok * NG + c / LANES] = word;
-    const uint32_t mask = there ? 0xfu << (4 * e) : 0u;
+    quantise<T, D>(y, code, word);
+    if (there && c == 0) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) vp[tok * NG + g] = word[g];
+    }
+    const float place = there ? __uint_as_float((127u + 4u * e) << 23) : 0.f;   // 16^e
     uint32_t v[CH];
 #pragma unroll
-    for (int i = 0; i < CH; ++i) v[i] = (code[i] << (4 * e)) & mask;
+    for (int i = 0; i < CH; ++i) v[i] = (uint32_t)(code[i / PIECE][i % PIECE] * place);
 #pragma unroll
     for (int i = 0; i < CH / 2; ++i) v[i] = join32(v[i], v[i + CH / 2]);
 #pragma unroll
     for (int i = 0; i < CH / 4; ++i) v[i] = join16(v[i], v[i + CH / 4]);
-    uint32_t all = join32(mask, mask);
-    all = join16(all, all);
-    all |= other8(all);
-    int ch = c * CH + (e >> 2) * (CH / 2) + ((e >> 1) & 1) * (CH / 4);
+    const uint64_t rows = __ballot(there);
+    uint32_t all = 0;   // nibbles written
+#pragma unroll
+    for (int k = 0; k < 8; ++k) all |= (rows >> (8 * k) & 1) ? 0xfu << (4 * k) : 0u;
+    int at = (e >> 2) * (CH / 2) + ((e >> 1) & 1) * (CH / 4);   // the first word's place of CH
     constexpr int LEFT = CH / 4 > 1 ? CH / 8 : 1;
     if (CH / 4 > 1) {
         const bool up = e & 1;
@@ -157,7 +185,7 @@ void kv4_append(const T *__restrict__ K, const T *__restrict__ V, uint32_t *__re
             const uint32_t keep = up ? v[i + LEFT] : v[i], give = up ? v[i] : v[i + LEFT];
             v[i] = keep | other8(give);
         }
-        ch += up ? LEFT : 0;
+        at += up ? LEFT : 0;
     } else {
         v[0] |= other8(v[0]);
     }
@@ -165,8 +193,9 @@ void kv4_append(const T *__restrict__ K, const T *__restrict__ V, uint32_t *__re
     if (CH / 4 > 1 || (e & 1) == 0) {
 #pragma unroll
         for (int i = 0; i < LEFT; ++i) {
-            uint32_t *at = out + v_word<D>(ch + i);
-            *at = all == 0xffffffffu ? v[i] : (*at & ~all) | v[i];
+            const int ch = P::channel((at + i) / PIECE, c) + (at + i) % PIECE;
+            uint32_t *to = out + v_word<D>(ch);
+            *to = all == 0xffffffffu ? v[i] : (*to & ~all) | v[i];
         }
     }
 }
@@ -177,30 +206,36 @@ void kv4_read(const uint32_t *__restrict__ kw, const uint32_t *__restrict__ vw,
               const uint32_t *__restrict__ kp, const uint32_t *__restrict__ vp,
               T *__restrict__ K, T *__restrict__ V, const int32_t *__restrict__ start,
               const int32_t *__restrict__ count, int B, int H, int n, int L, int Lp, int octets) {
-    constexpr int CH = D / 8, NG = Kv4Dim<D>::kGroups, LANES = 8 / NG;
+    using P = Pieces<T, D>;
+    constexpr int NG = P::NG, PIECE = P::PIECE;
     Octet o;
     if (!take_octet(&o, B, H, n, L, octets, start, count)) return;
     const int lane = threadIdx.x & 63, e = lane >> 3, c = lane & 7;
     const int p = o.pos + e, j = p - o.at;
     if (j < 0 || j >= o.rows) return;
-    const size_t row = ((size_t)o.bh * n + j) * D + c * CH;
+    const size_t row = ((size_t)o.bh * n + j) * D;
     const size_t tok = (size_t)o.bh * Lp + p;
-    const uint32_t kg = kp[tok * NG + c / LANES], vg = vp[tok * NG + c / LANES];
-    uint32_t w[2];
-    w[0] = kw[tok * (D / 8) + k_word<D>(c * CH / 8)];
-    if (CH == 16) w[1] = kw[tok * (D / 8) + k_word<D>(2 * c + 1)];
-    if (CH == 4) w[0] >>= 16 * (c & 1);
-    float x[CH];
-#pragma unroll
-    for (int i = 0; i < CH; ++i)
-        x[i] = fmaf(group_scale(kg), (float)(w[i >> 3] >> (4 * (i & 7)) & 15u), group_min(kg));
-    store_row(K + row, x);
     const uint32_t *in = vw + ((size_t)o.bh * (Lp / 8) + p / 8) * D;
+    uint32_t kg[NG], vg[NG];
 #pragma unroll
-    for (int i = 0; i < CH; ++i)
-        x[i] = fmaf(group_scale(vg), (float)(in[v_word<D>(c * CH + i)] >> (4 * e) & 15u),
-                    group_min(vg));
-    store_row(V + row, x);
+    for (int g = 0; g < NG; ++g) {
+        kg[g] = kp[tok * NG + g];
+        vg[g] = vp[tok * NG + g];
+    }
+#pragma unroll
+    for (int i = 0; i < P::PIECES; ++i) {
+        const int ch = P::channel(i, c), g = i / P::PER;
+        const uint32_t w = kw[tok * (D / 8) + k_word<D>(ch / 8)] >> (4 * (ch & 7));
+        float x[PIECE], y[PIECE];
+#pragma unroll
+        for (int k = 0; k < PIECE; ++k) {
+            x[k] = fmaf(group_scale(kg[g]), (float)(w >> (4 * k) & 15u), group_min(kg[g]));
+            y[k] = fmaf(group_scale(vg[g]), (float)(in[v_word<D>(ch + k)] >> (4 * e) & 15u),
+                        group_min(vg[g]));
+        }
+        store_row(K + row + ch, x);
+        store_row(V + row + ch, y);
+    }
 }
 
 // Octets that n rows from any start can touch.

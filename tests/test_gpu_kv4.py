@@ -281,6 +281,8 @@ EVICT = [
     (1, 2, 333, 128, 7, 0, [300]),
     (2, 2, 3000, 64, 1500, 100, [2999, 1501]),
     (1, 2, 5000, 128, 2300, 31, None),
+    (1, 1, 20001, 32, 9000, 3000, [19999]),
+    (1, 1, 40000, 32, 20011, 7, None),       # more than a workgroup keeps in registers
 ]
 
 
