@@ -9,7 +9,8 @@
  *   min   = bf16(min x)                         (nearest even)
  *   scale = bf16((max x - min x) / 15)          (f32 difference and quotient)
  *   code  = clamp(round((x - min) / scale), 0, 15)   (nearest even; 0 where
- *                                                     the scale is 0)
+ *                                                     the scale is 0; bf16 x:
+ *                                                     the difference in f32)
  *   value = scale * code + min                  (what the cache stands for)
  *
  * A scale below 2^-126 is taken as 0.  A group that holds an infinity or NaN,

@@ -66,54 +66,74 @@ struct Pieces {
     static __device__ __forceinline__ int channel(int i, int c) { return (8 * i + c) * PIECE; }
 };
 
-// Codes of a lane's pieces of one row (as f32), and the groups' words.
+// The value of another of a token's eight lanes, one step of a reduction over them.
+template <int STEP>
+__device__ __forceinline__ float other_lane(float v) {
+    // neighbour, other pair of the four, mirror image in the eight
+    constexpr int CONTROL = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : 0x141;
+    return __int_as_float(
+        __builtin_amdgcn_update_dpp(0, __float_as_int(v), CONTROL, 0xf, 0xf, true));
+}
+
+// Codes of a lane's pieces of one row, each plus the bits of kRound, and the groups'
+// words; all codes 0 where the lane holds no row.
 //
-// code = round((x - min) / scale), from a product with 1 / scale.  Next to a border
-// between two codes (ties are common among bf16 values) the side is settled
-// exactly, with the difference's rounding error, ties to the even code.
+// code = round((x - min) / scale): the quotient of the f32 difference, correctly
+// rounded (a product with 1 / scale and one exact residual), so that ties, which
+// are common among bf16 values, go to the even code when kRound is added.  A bf16
+// difference is exact unless x and min are 2^16 apart.  f32 values within 2^-20 of a
+// border are settled exactly, with the rounding error of the difference.
+constexpr float kRound = 0x1p23f;   // ulp 1: adding it rounds, the code is in the low bits
+constexpr uint32_t kRoundBits = 0x4b000000u;
+
 template <typename T, int D>
 __device__ __forceinline__ void quantise(const float (&x)[Pieces<T, D>::PIECES][Pieces<T, D>::PIECE],
-                                         float (&code)[Pieces<T, D>::PIECES][Pieces<T, D>::PIECE],
-                                         uint32_t (&word)[Kv4Dim<D>::kGroups]) {
+                                         uint32_t (&code)[Pieces<T, D>::PIECES][Pieces<T, D>::PIECE],
+                                         uint32_t (&word)[Kv4Dim<D>::kGroups], bool there) {
     using P = Pieces<T, D>;
+    // minimum and maximum of numbers, NaN where one is NaN
+    const auto least = [](float a, float b) { return __builtin_elementwise_minimum(a, b); };
+    const auto most = [](float a, float b) { return __builtin_elementwise_maximum(a, b); };
 #pragma unroll
     for (int g = 0; g < P::NG; ++g) {
-        float lo = x[g * P::PER][0], hi = lo, odd = 0.f;   // odd: NaN where one is not finite
+        float lo = x[g * P::PER][0], hi = lo;
 #pragma unroll
         for (int i = g * P::PER; i < (g + 1) * P::PER; ++i)
 #pragma unroll
-            for (int k = 0; k < P::PIECE; ++k) {
-                lo = fminf(lo, x[i][k]);
-                hi = fmaxf(hi, x[i][k]);
-                odd = fmaf(x[i][k], 0.f, odd);
+            for (int k = 0; k < P::PIECE; k += 2) {
+                lo = least(least(lo, x[i][k]), x[i][k + 1]);
+                hi = most(most(hi, x[i][k]), x[i][k + 1]);
             }
-#pragma unroll
-        for (int m = 1; m < 8; m *= 2) {
-            lo = fminf(lo, __shfl_xor(lo, m, 64));
-            hi = fmaxf(hi, __shfl_xor(hi, m, 64));
-            odd += __shfl_xor(odd, m, 64);
-        }
-        const uint32_t mb = f32_to_bf16_rne(lo);
-        uint32_t sb = f32_to_bf16_rne((hi - lo) / 15.f);
+        lo = least(lo, other_lane<0>(lo));
+        hi = most(hi, other_lane<0>(hi));
+        lo = least(lo, other_lane<1>(lo));
+        hi = most(hi, other_lane<1>(hi));
+        lo = least(lo, other_lane<2>(lo));
+        hi = most(hi, other_lane<2>(hi));
+        const uint32_t mb = to_bf16(lo);
+        uint32_t sb = to_bf16((hi - lo) / 15.f);   // NaN or infinite where a value is
         if (sb < 0x0080u) sb = 0;   // below the smallest normal
         const float mn = bf16_to_f32((uint16_t)mb), sc = bf16_to_f32((uint16_t)sb);
-        const bool good = odd == 0.f && fabsf(mn) < INFINITY && sc < INFINITY;
-        const bool flat = !good || sb == 0;
+        const bool good = fabsf(mn) < INFINITY && sc < INFINITY;
+        const bool flat = !good || sb == 0 || !there;
         const float inv = flat ? 0.f : 1.f / sc, from = flat ? 0.f : mn;
         word[g] = good ? sb << 16 | mb : 0x7fc07fc0u;
 #pragma unroll
         for (int i = g * P::PER; i < (g + 1) * P::PER; ++i)
 #pragma unroll
             for (int k = 0; k < P::PIECE; ++k) {
-                const float t = x[i][k] - from, q = t * inv;
-                float y = rintf(q);
-                if (fabsf(q - y) > 0.5f - 0x1p-16f) {
-                    const float f = floorf(q), b = t - x[i][k];
-                    const float lost = (x[i][k] - (t - b)) - (from + b);   // t + lost = x - min
-                    const float over = (t - sc * (f + 0.5f)) + lost;       // both exact
-                    y = f + (over > 0.f || (over == 0.f && ((int)f & 1)) ? 1.f : 0.f);
+                const float t = x[i][k] - from, q0 = t * inv;
+                float q = fmaf(fmaf(-sc, q0, t), inv, q0);
+                if (sizeof(T) == 4) {
+                    if (fabsf(q - rintf(q)) > 0.5f - 0x1p-20f) {
+                        const float f = floorf(q), b = t - x[i][k];
+                        const float lost = (x[i][k] - (t - b)) - (from + b);   // t + lost = x - min
+                        const float over = (t - sc * (f + 0.5f)) + lost;       // both exact
+                        q = f + (over > 0.f || (over == 0.f && ((int)f & 1)) ? 1.f : 0.f);
+                    }
                 }
-                code[i][k] = __builtin_amdgcn_fmed3f(y, 0.f, 15.f);   // (NaN: 0)
+                // (NaN: 0)
+                code[i][k] = __float_as_uint(__builtin_amdgcn_fmed3f(q, 0.f, 15.f) + kRound);
             }
     }
 }
@@ -133,21 +153,22 @@ void kv4_append(const T *__restrict__ K, const T *__restrict__ V, uint32_t *__re
     const int p = o.pos + e, j = p - o.at;
     const bool there = j >= 0 && j < o.rows;   // rows are clamped to positions below L
     const size_t row = ((size_t)o.bh * n + (there ? j : 0)) * D;
-    float x[P::PIECES][PIECE], y[P::PIECES][PIECE], code[P::PIECES][PIECE];
-    uint32_t word[NG];
+    float x[P::PIECES][PIECE], y[P::PIECES][PIECE];
+    uint32_t code[P::PIECES][PIECE], word[NG];
 #pragma unroll
     for (int i = 0; i < P::PIECES; ++i) load_row(x[i], K + row + P::channel(i, c));
 #pragma unroll
     for (int i = 0; i < P::PIECES; ++i) load_row(y[i], V + row + P::channel(i, c));
 
     // K: words of 8 channels, a lane's own or, of 4 each, with its neighbour
-    quantise<T, D>(x, code, word);
+    quantise<T, D>(x, code, word, there);
     const size_t tok = (size_t)o.bh * Lp + p;
 #pragma unroll
     for (int i = 0; i < P::PIECES; ++i) {
-        uint32_t w = 0;
+        // sums of codes at their places; kRoundBits' own sum is taken off first
+        uint32_t w = 0u - kRoundBits - (kRoundBits << 4);
 #pragma unroll
-        for (int k = 0; k < PIECE; ++k) w |= (uint32_t)code[i][k] << (4 * k);
+        for (int k = 0; k < PIECE; ++k) w += code[i][k] << (4 * k);
         if (PIECE == 4) w |= (uint32_t)__shfl_xor((int)w, 1, 64) << 16;   // in even lanes
         if (there && (PIECE == 8 || (c & 1) == 0))
             kw[tok * (D / 8) + k_word<D>(P::channel(i, c) / 8)] = w;
@@ -159,15 +180,15 @@ void kv4_append(const T *__restrict__ K, const T *__restrict__ V, uint32_t *__re
     }
 
     // V: a channel's eight tokens in one word
-    quantise<T, D>(y, code, word);
+    quantise<T, D>(y, code, word, there);
     if (there && c == 0) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) vp[tok * NG + g] = word[g];
     }
-    const float place = there ? __uint_as_float((127u + 4u * e) << 23) : 0.f;   // 16^e
+    const uint32_t place = 4u * e, off = 0u - (kRoundBits << place);
     uint32_t v[CH];
 #pragma unroll
-    for (int i = 0; i < CH; ++i) v[i] = (uint32_t)(code[i / PIECE][i % PIECE] * place);
+    for (int i = 0; i < CH; ++i) v[i] = (code[i / PIECE][i % PIECE] << place) + off;
 #pragma unroll
     for (int i = 0; i < CH / 2; ++i) v[i] = join32(v[i], v[i + CH / 2]);
 #pragma unroll
