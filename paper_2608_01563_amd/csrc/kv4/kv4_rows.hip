@@ -10,7 +10,7 @@
 //
 // Scores: kv4_tile.h.  The second product is O^T = V^T P^T on V's codes:
 //   O = sum_j (p_j scale_j) code_j + sum_j p_j min_j
-// with p scale rounded to f16 (within 2^-12; strict: two parts, 2^-23) and the
+// (strict: code - 8, with min + 8 scale) with p scale rounded to f16 (within 2^-12; strict: two parts, 2^-23) and the
 // second sum in f32 from the unrounded p.  f16 holds p scale because both
 // factors are taken relative to a running bound: p to 2^kSlack above 1, and the
 // scales to a power of two of the row's own, moved up (and the sums rescaled,
@@ -72,7 +72,7 @@ struct Kv4Values {
 
 template <int NG>
 struct BlockGroups {   // a block's groups in LDS, token k's at k * NG
-    float scale[2][32 * NG], min[2][32 * NG];   // of K, V
+    float scale[2][32 * NG], base[2][32 * NG];   // of K, V
 };
 
 // A block's group words, brought in by the wave's lanes (a word of K and one of V
@@ -93,14 +93,15 @@ struct Kv4GroupWords {
         }
     }
     // 0 for tokens at or behind n
+    template <int NP>
     __device__ __forceinline__ void put(BlockGroups<NG> &to, int block, int n, int lane) {
         const bool in = 32 * block + (NG == 2 ? lane >> 1 : lane & 31) < n;
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
             w[i] = in ? w[i] : 0u;
-            float *scale = &to.scale[0][0], *min = &to.min[0][0];
+            float *scale = &to.scale[0][0], *base = &to.base[0][0];
             scale[64 * i + lane] = group_scale(w[i]);
-            min[64 * i + lane] = group_min(w[i]);
+            base[64 * i + lane] = base_of<NP>(w[i]);
         }
     }
     // the lane's V word, or 0
@@ -158,7 +159,7 @@ void kv4_rows(RowsArgs a) {
     int e = -kExpMax;                  // V's scales are below 2^e
     uint32_t most = 0;                 // ... as a bound on their group words
     float l = 0.f;                     // sum of p 2^(kRaise - e)
-    float low[NG];                     // sums of p min in the same units
+    float low[NG];                     // sums of p base in the same units
     f32x4 o[NB];                       // O^T[16 b + 4g + r][row c], over kCodeUnit
 #pragma unroll
     for (int i = 0; i < NG; ++i) low[i] = 0.f;
@@ -167,15 +168,15 @@ void kv4_rows(RowsArgs a) {
 
     auto step = [&](int block, const Kv4Keys<D> &key, const Kv4Values<D> &val,
                     Kv4GroupWords<NG> &words, BlockGroups<NG> &groups) {
-        words.put(groups, block, mask.n, lane);
+        words.template put<NP>(groups, block, mask.n, lane);
         __builtin_amdgcn_wave_barrier();   // one wave's LDS accesses stay in order
         f32x4 s[2];
-        key.scores(s, q, groups.scale[0], groups.min[0], c, g);
+        key.scores(s, q, groups.scale[0], groups.base[0], c, g);
         float vs[8 * NG], vm[8 * NG];   // of the lane's octet
 #pragma unroll
         for (int i = 0; i < 2 * NG; ++i) {
             const f32x4 x = *reinterpret_cast<const f32x4 *>(&groups.scale[1][8 * g * NG + 4 * i]);
-            const f32x4 y = *reinterpret_cast<const f32x4 *>(&groups.min[1][8 * g * NG + 4 * i]);
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(&groups.base[1][8 * g * NG + 4 * i]);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 vs[4 * i + k] = x[k];
@@ -239,7 +240,7 @@ void kv4_rows(RowsArgs a) {
             split_operand<NP>(part, x);
 #pragma unroll
             for (int cb = i * (NB / NG); cb < (i + 1) * (NB / NG); ++cb) {
-                const f16x8 v = code_operand(val.w[cb]);
+                const f16x8 v = operand_of<NP>(val.w[cb]);
 #pragma unroll
                 for (int n = NP - 1; n >= 0; --n) o[cb] = mfma16x16x32f16(v, part[n], o[cb]);
             }

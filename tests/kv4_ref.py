@@ -153,12 +153,22 @@ def attention(q, code, group, n, rows, causal, scale, strict, many=False):
     is rounded once to f16 (strict: within 2^-23), n terms are summed in f32
     and the result is rounded to its type.  With many bf16 rows a head p and v
     are rounded to f16 each, v in units that leave an error of 2^-34 of the
-    largest v at worst."""
+    largest v at worst.
+
+    Roundings are relative to the parts that a value is summed from: scale code
+    and min, or, strict, scale (code - 8) and min + 8 scale (which f32 rounds
+    once more: a half step of it).  p * scale is held as f16 in units of
+    2^(e - 11), 2^e at most twice the largest scale: below f16's normal numbers it
+    is off by up to 2^-25 units, times a code of 15 (strict: 8) for each token."""
     Lq, d = q.shape
     (kc, vc), ((ks, km), (vs, vm)) = code, group
     f32 = HALF_STEP["f32"]
     k, v = values(kc[:n], ks[:n], km[:n]), values(vc[:n], vs[:n], vm[:n])
-    size = lambda c, s, m: values(c, np.abs(s), np.abs(m))
+    def size(c, s, m):
+        if not strict:
+            return values(c, np.abs(s), np.abs(m))
+        return values(np.abs(c.astype(np.int16) - 8), np.abs(s), np.abs(m + 8 * s))
+
     kk, vv = size(kc[:n], ks[:n], km[:n]), size(vc[:n], vs[:n], vm[:n])
     i = np.arange(Lq)[:, None]
     j = np.arange(n)[None, :]
@@ -185,7 +195,8 @@ def attention(q, code, group, n, rows, causal, scale, strict, many=False):
         out = f32 if strict else HALF_STEP["bf16"]
         part = 2.0 ** -22 if strict else HALF_STEP["f16"] * (2 if many else 1)
         tO[r] = out * np.abs(O[r]) + (part + rel + (len(at) + 8) * f32) * (p @ vv[at]) \
-            + (2.0 ** -34 * vv.max() if many else 0)
+            + (2.0 ** -34 * vv.max() if many else
+               len(at) * (8 if strict else 15) * 2.0 ** -35 * vs[at].max())
         tL[r] = rel + 4 * f32 * abs(LSE[r])
         tP[r, at] = 2 * rel * p + 1e-30
     return O, LSE, P, tO, tL, tP
