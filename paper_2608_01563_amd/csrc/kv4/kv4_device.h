@@ -44,6 +44,31 @@ __device__ __forceinline__ uint16_t to_bf16(float x) {
     return __builtin_bit_cast(uint16_t, (__bf16)x);
 }
 
+// The value of another lane, one step of a reduction over aligned lanes: neighbour,
+// other pair of four, mirror image in eight, mirror image in sixteen.
+template <int STEP>
+__device__ __forceinline__ float other_lane(float v) {
+    constexpr int CONTROL = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : STEP == 2 ? 0x141 : 0x140;
+    return __int_as_float(
+        __builtin_amdgcn_update_dpp(0, __float_as_int(v), CONTROL, 0xf, 0xf, true));
+}
+template <int LANES>
+__device__ __forceinline__ float max_of(float v) {
+    if (LANES >= 2) v = fmaxf(v, other_lane<0>(v));
+    if (LANES >= 4) v = fmaxf(v, other_lane<1>(v));
+    if (LANES >= 8) v = fmaxf(v, other_lane<2>(v));
+    if (LANES >= 16) v = fmaxf(v, other_lane<3>(v));
+    return v;
+}
+template <int LANES>
+__device__ __forceinline__ float sum_of(float v) {
+    if (LANES >= 2) v += other_lane<0>(v);
+    if (LANES >= 4) v += other_lane<1>(v);
+    if (LANES >= 8) v += other_lane<2>(v);
+    if (LANES >= 16) v += other_lane<3>(v);
+    return v;
+}
+
 // N consecutive elements as f32, N * sizeof(T) a multiple of 8 bytes.
 template <int N>
 __device__ __forceinline__ void load_row(float (&x)[N], const float *p) {

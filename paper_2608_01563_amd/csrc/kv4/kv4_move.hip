@@ -66,15 +66,6 @@ struct Pieces {
     static __device__ __forceinline__ int channel(int i, int c) { return (8 * i + c) * PIECE; }
 };
 
-// The value of another of a token's eight lanes, one step of a reduction over them.
-template <int STEP>
-__device__ __forceinline__ float other_lane(float v) {
-    // neighbour, other pair of the four, mirror image in the eight
-    constexpr int CONTROL = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : 0x141;
-    return __int_as_float(
-        __builtin_amdgcn_update_dpp(0, __float_as_int(v), CONTROL, 0xf, 0xf, true));
-}
-
 // Codes of a lane's pieces of one row, each plus the bits of kRound, and the groups'
 // words; all codes 0 where the lane holds no row.
 //

@@ -221,25 +221,12 @@ __device__ __forceinline__ int piece(int row, int p) {
     return row * (N + 1) + p;
 }
 
-// Maximum and sum over the wave (rotations within its rows of 16, then swaps).
-template <int ROTATE>
-__device__ __forceinline__ float max_rotated(float v) {
-    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(
-                        0, __float_as_int(v), 0x120 + ROTATE, 0xf, 0xf, false)));
-}
+// Maximum and sum over the wave.
 __device__ __forceinline__ float max_of_wave(float v) {
-    v = max_rotated<1>(max_rotated<2>(max_rotated<4>(max_rotated<8>(v))));
-    return max_xor32(max_xor16(v));
-}
-
-template <int ROTATE>
-__device__ __forceinline__ float sum_rotated(float v) {
-    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + ROTATE,
-                                                          0xf, 0xf, false));
+    return max_xor32(max_xor16(max_of<16>(v)));
 }
 __device__ __forceinline__ float sum_of_wave(float v) {
-    v = sum_rotated<1>(sum_rotated<2>(sum_rotated<4>(sum_rotated<8>(v))));
-    return sum_xor32(sum_xor16(v));
+    return sum_xor32(sum_xor16(sum_of<16>(v)));
 }
 
 // Token (of 32) in row i of a score product.

@@ -93,16 +93,14 @@ void kv4_weights(WeightArgs a) {
         float top = 0.f, sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
-#pragma unroll
-        for (int m = 1; m < PER; m *= 2) top = fmaxf(top, xor_lanes(top, m));
+        top = max_of<PER>(top);
         const int exponent = __builtin_amdgcn_frexp_expf(top);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             sum += ldexpf(x[e], -exponent);
             x[e] = ldexpf(x[e], 15 - exponent);
         }
-#pragma unroll
-        for (int m = 1; m < PER / NG; m *= 2) sum += xor_lanes(sum, m);
+        sum = sum_of<PER / NG>(sum);
         f16x8 part[NP];
         split_operand<NP>(part, x);
 #pragma unroll
