@@ -45,8 +45,11 @@
  * are 16-byte aligned device memory except int32 and weight arrays (4-byte).
  * Lengths in device arrays are clamped on the device.  Outputs must not alias
  * inputs except where said.  No atomics on results: they are bitwise
- * reproducible.  d in {32, 64, 128}.  Calls on one cache must be ordered by
- * the caller (one stream, or events).
+ * reproducible.  Calls on one cache must be ordered by the caller (one stream,
+ * or events).
+ *
+ * Sizes: d in {32, 64, 128}; L and n at most 2^24, B*H at most 2^19, B*H*L (L
+ * rounded up to 32) at most 2^30, B*H*n at most 2^28, B*Hq*Lq*d below 2^31.
  */
 #ifndef MG_KV4_H
 #define MG_KV4_H
@@ -60,8 +63,7 @@
 extern "C" {
 #endif
 
-/* Bytes of a cache; 0 when the arguments are invalid: sizes < 1, B*H > 2^20,
- * L > 2^24, or d not supported. */
+/* Bytes of a cache; 0 for sizes below 1 or that no cache has (above). */
 size_t mg_kv4_cache_bytes(int B, int H, int L, int d);
 
 /*

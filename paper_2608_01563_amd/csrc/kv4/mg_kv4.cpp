@@ -61,7 +61,11 @@ using mg::host::fail;
 using mg::host::ok;
 using mg::host::run_kernel;
 
-constexpr int kMaxTokens = 1 << 24, kMaxHeads = 1 << 20;
+// These keep every grid below 2^32 threads (six workgroups of 1,024 a head where
+// sequences are cut, 64 threads an octet of tokens written, two threads a token
+// where weights are gathered) and a head's regions below 4 GiB.
+constexpr int kMaxTokens = 1 << 24, kMaxHeads = 1 << 19;
+constexpr int64_t kMaxCache = 1 << 30, kMaxMoved = 1 << 28;
 
 mg_status_t check_contract(mg_contract_t c) {
     if (c != MG_CONTRACT_STRICT_F32 && c != MG_CONTRACT_FAST_BF16 && c != MG_CONTRACT_ACCELERATED)
@@ -75,10 +79,10 @@ mg_status_t check_cache(int B, int H, int L, int d) {
         return fail(MG_ERR_INVALID_ARGUMENT, "sizes must be >= 1 (B=%d H=%d L=%d d=%d)", B, H, L,
                     d);
     if ((int64_t)B * H > kMaxHeads || L > kMaxTokens ||
-        (int64_t)B * H * mg::kv4_padded(L) > INT32_MAX)
+        (int64_t)B * H * mg::kv4_padded(L) > kMaxCache)
         return fail(MG_ERR_INVALID_ARGUMENT,
-                    "the cache is too large (B=%d H=%d L=%d): B*H at most 2^20, L at most 2^24, "
-                    "B*H*L below 2^31", B, H, L);
+                    "the cache is too large (B=%d H=%d L=%d): B*H at most 2^19, L at most 2^24, "
+                    "B*H*L (L rounded up to 32) at most 2^30", B, H, L);
     if (d != 32 && d != 64 && d != 128)
         return fail(MG_ERR_UNSUPPORTED, "head dimension %d is not 32, 64 or 128", d);
     return MG_OK;
@@ -88,9 +92,9 @@ mg_status_t check_move(int B, int H, int n, int L, int d, mg_contract_t contract
     MG_TRY(check_contract(contract));
     MG_TRY(check_cache(B, H, L, d));
     if (n < 1) return fail(MG_ERR_INVALID_ARGUMENT, "n must be >= 1 (got %d)", n);
-    if (n > kMaxTokens || (int64_t)B * H * n >= (1 << 29))
+    if (n > kMaxTokens || (int64_t)B * H * n > kMaxMoved)
         return fail(MG_ERR_INVALID_ARGUMENT,
-                    "too many rows (B=%d H=%d n=%d): n at most 2^24, B*H*n below 2^29", B, H, n);
+                    "too many rows (B=%d H=%d n=%d): n at most 2^24, B*H*n at most 2^28", B, H, n);
     return MG_OK;
 }
 

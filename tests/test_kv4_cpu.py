@@ -49,6 +49,19 @@ def test_no_cache_of_bad_sizes(B, H, L, d):
         mg.kv4_cache(B, H, L, d)
 
 
+def test_largest_sizes(lib):
+    """Grids of 2^32 threads and more are not launched."""
+    for B, H, L, more in ((1 << 19, 1, 32, (1, 0, 0)), (1 << 10, 1 << 9, 1 << 11, (0, 0, 1)),
+                          (1 << 3, 1 << 3, 1 << 24, (0, 0, 1))):
+        assert mg.mg_kv4_cache_bytes(B, H, L, 32) == ref.regions(B, H, L, 32)[1] > 0
+        assert mg.mg_kv4_cache_bytes(B + more[0], H + more[1], L + more[2], 32) == 0
+    for call in (append, read):
+        # n at its limit: the pointers, which are nobody's, are what is refused
+        for n, refused in ((1 << 9, "device"), ((1 << 9) + 1, "rows")):
+            assert call(lib, B=1 << 10, H=1 << 9, n=n, L=64) == 1
+            assert refused in mg.mg_last_error_detail()
+
+
 def test_workspace_query():
     f = mg.mg_attn_fwd_kv4_workspace_bytes
     assert f(1, 4, 4, 1, 256, 64) == 0                      # one share a head, no weights
