@@ -1,7 +1,7 @@
 // kv4_many.hip -- attention over the 4-bit cache for many query rows (bf16).
 //
 // Where kv4_rows.hip has every wave unpack the codes it multiplies, here a
-// workgroup of WAVES x 32 rows unpacks a tile of 64 tokens once into LDS and
+// workgroup of 256 rows unpacks a tile of 64 tokens once into LDS and
 // all of its waves read it there (32x32x16 products, 32 rows a wave):
 //
 //   K   codes as f16, exact; scores are scaled and shifted a group at a time as
@@ -23,7 +23,7 @@
 namespace mg {
 namespace {
 
-constexpr int kTokens = 64;
+constexpr int kTokens = 64, kManyWaves = 8, kRows = 32 * kManyWaves;
 constexpr float kManySlack = 4.f;
 constexpr int kLift = 11;      // P is at most 2^(slack + kLift) = 2^15
 constexpr int kManyExp = 100;  // bound on E
@@ -84,11 +84,11 @@ struct Query32 {
     }
 };
 
-template <int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, 8)))
+template <int D>
+__global__ __launch_bounds__(64 * kManyWaves) __attribute__((amdgpu_waves_per_eu(2, 8)))
 void kv4_many(ManyArgs a) {
     constexpr int NG = Kv4Dim<D>::kGroups, NS = D / 16, NB = D / 32, KR = D / 8;
-    constexpr int T = 64 * WAVES, WORDS = kTokens * D / 8;
+    constexpr int T = 64 * kManyWaves, WORDS = kTokens * D / 8;
     constexpr int N = WORDS / T < 1 ? 1 : WORDS / T;   // words a thread unpacks
     __shared__ __attribute__((aligned(16))) f16x8 Ks[2][kTokens * (KR + 1)];
     __shared__ __attribute__((aligned(16))) f16x8 Vs[3][D * 9];
@@ -108,16 +108,16 @@ void kv4_many(ManyArgs a) {
     const int rows = a.G * a.Lq;
     const Kv4Mask mask = sequence_mask(a.key_len, a.q_len, bh / a.H, a.L, a.Lq, a.causal);
 
-    const int r0 = 32 * (WAVES * tile + w), r = r0 + c;
+    const int r0 = kRows * tile + 32 * w, r = r0 + c;
     const bool in = r < rows;
     const int rr = in ? r : rows - 1, i = rr / a.G;
     const size_t at = ((size_t)bh * a.G + (rr - i * a.G)) * a.Lq + i;
     const int limit = mask.limit(i);
     // tokens that some row of the workgroup, some row of the wave, every row
     // of the wave sees
-    const int wg0 = 32 * WAVES * tile;
+    const int wg0 = kRows * tile;
     const int end = wg0 / a.G < mask.rows
-        ? max(mask.limit(min((min(rows, wg0 + 32 * WAVES) - 1) / a.G, mask.rows - 1)), 0) : 0;
+        ? max(mask.limit(min((min(rows, wg0 + kRows) - 1) / a.G, mask.rows - 1)), 0) : 0;
     const int wave_end = r0 < rows && r0 / a.G < mask.rows
         ? max(mask.limit(min((min(rows, r0 + 32) - 1) / a.G, mask.rows - 1)), 0) : 0;
     const int wave_all = r0 < rows ? mask.limit(r0 / a.G) : 0;
@@ -435,16 +435,15 @@ void kv4_many(ManyArgs a) {
     if (h == 0) a.LSE[at] = l != l ? l : row_lse(m, ldexpf(l, -kLift));
 }
 
-template <int D, int WAVES>
+template <int D>
 hipError_t many(const Kv4Attn &p, const Kv4Plan &plan, const void *Q,
                 const Kv4Cache<const uint32_t> &c, void *O, float *LSE, char *ws, hipStream_t s) {
-    const int tiles = (int)((kv4_rows(p) + 32 * WAVES - 1) / (32 * WAVES));
+    const int tiles = (int)((kv4_rows(p) + kRows - 1) / kRows);
     const ManyArgs a = {static_cast<const uint16_t *>(Q), c.k, c.v, c.kp, c.vp,
                         static_cast<uint16_t *>(O), LSE, (float *)(ws + plan.part),
                         (float *)(ws + plan.stat), p.key_len, p.q_len, p.H, p.G, p.Lq, p.L,
                         kv4_padded(p.L), p.causal, p.scale * kLog2e, plan.splits, tiles};
-    kv4_many<D, WAVES><<<(unsigned)((int64_t)p.B * p.H * plan.splits * tiles), 64 * WAVES, 0, s>>>(
-        a);
+    kv4_many<D><<<(unsigned)((int64_t)p.B * p.H * plan.splits * tiles), 64 * kManyWaves, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -454,13 +453,9 @@ hipError_t launch_kv4_many(const Kv4Attn &p, const Kv4Plan &plan, const void *Q,
                            const Kv4Cache<const uint32_t> &c, void *O, float *LSE, void *ws,
                            hipStream_t s) {
     char *w = static_cast<char *>(ws);
-    if (plan.rows == 256)
-        return p.d == 32 ? many<32, 8>(p, plan, Q, c, O, LSE, w, s)
-             : p.d == 64 ? many<64, 8>(p, plan, Q, c, O, LSE, w, s)
-                         : many<128, 8>(p, plan, Q, c, O, LSE, w, s);
-    return p.d == 32 ? many<32, 4>(p, plan, Q, c, O, LSE, w, s)
-         : p.d == 64 ? many<64, 4>(p, plan, Q, c, O, LSE, w, s)
-                     : many<128, 4>(p, plan, Q, c, O, LSE, w, s);
+    return p.d == 32 ? many<32>(p, plan, Q, c, O, LSE, w, s)
+         : p.d == 64 ? many<64>(p, plan, Q, c, O, LSE, w, s)
+                     : many<128>(p, plan, Q, c, O, LSE, w, s);
 }
 
 }  // namespace mg

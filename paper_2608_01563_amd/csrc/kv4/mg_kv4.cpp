@@ -12,18 +12,25 @@
 
 namespace mg {
 
-// How a call runs.  kv4_many from 64 rows a cache head on, with 256 rows a
-// workgroup where that gives every compute unit one, its tokens split over
-// workgroups where there are fewer.  Else kv4_rows, its tokens cut into chunks for
-// two workgroups on every compute unit (with 1,280 workgroups drafted rows took
-// 22.9 instead of 19.9 us, a long batch 51 either way: each workgroup prepares
-// its query rows and joins its waves).  A split has at least 256 tokens.
+// How a call runs.  kv4_many reads a tile of tokens once for 256 rows, kv4_rows
+// for 16, with a simpler start and end.  At 256 heads of 8,192 tokens, kv4_many /
+// kv4_rows in us: d = 128: 211/92 with 32 rows a head, 246/266 with 96, 251/361
+// with 128, 656/1034 with 512; d = 64: 200/181 with 128, 227/329 with 256.  It
+// needs the work too: 43/47 at 8 heads x 512 rows x 8,192 tokens (2^25) and 41/53
+// at 256 x 128 x 1,024 (the same), but 35/28 with 8 x 256 x 8,192, where its split
+// form hardly fills the GPU.  (128-row workgroups were slower at d = 128: their
+// unpacked tiles fill the LDS all the same.)  Tokens are split over workgroups
+// where there are fewer than the GPU holds at once: one of kv4_many or two of
+// kv4_rows a compute unit (with 1,280 drafted rows took 22.9 instead of 19.9 us, a
+// long batch 51 either way: each workgroup prepares its query rows and joins its
+// waves).  A split has at least 256 tokens.
 Kv4Plan kv4_plan(const Kv4Attn &p, bool weights, bool bf16) {
     const int64_t heads = (int64_t)p.B * p.H, rows = kv4_rows(p);
     Kv4Plan plan = {};
-    plan.rows = !bf16 || rows < 64 ? 16 : heads * ((rows + 255) / 256) >= 256 ? 256 : 128;
+    const bool many = bf16 && rows >= 128 && heads * rows * p.L >= (1 << 25);
+    plan.rows = many ? 256 : 16;
     const int64_t tiles = heads * ((rows + plan.rows - 1) / plan.rows);
-    const int64_t want = plan.rows == 256 ? 256 : 512;
+    const int64_t want = many ? 256 : 512;
     const int blocks = kv4_padded(p.L) / 32;
     plan.splits = (int)std::max<int64_t>(
         1, std::min({(want + tiles - 1) / tiles, (int64_t)64, (int64_t)blocks / 8}));

@@ -153,7 +153,8 @@ def attention(q, code, group, n, rows, causal, scale, strict, many=False):
     is rounded once to f16 (strict: within 2^-23), n terms are summed in f32
     and the result is rounded to its type.  With many bf16 rows a head p and v
     are rounded to f16 each, v in units that leave an error of 2^-34 of the
-    largest v at worst.
+    largest v at worst, and the largest p is held as 2^10 or more: p below f16's
+    normal numbers are off by up to 2^-25, so by 2^-35 of the sum of p.
 
     Roundings are relative to the parts that a value is summed from: scale code
     and min, or, strict, scale (code - 8) and min + 8 scale (which f32 rounds
@@ -195,7 +196,7 @@ def attention(q, code, group, n, rows, causal, scale, strict, many=False):
         out = f32 if strict else HALF_STEP["bf16"]
         part = 2.0 ** -22 if strict else HALF_STEP["f16"] * (2 if many else 1)
         tO[r] = out * np.abs(O[r]) + (part + rel + (len(at) + 8) * f32) * (p @ vv[at]) \
-            + (2.0 ** -34 * vv.max() if many else
+            + ((2.0 ** -34 + len(at) * 2.0 ** -35) * vv.max() if many else
                len(at) * (8 if strict else 15) * 2.0 ** -35 * vs[at].max())
         tL[r] = rel + 4 * f32 * abs(LSE[r])
         tP[r, at] = 2 * rel * p + 1e-30

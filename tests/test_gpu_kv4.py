@@ -146,8 +146,25 @@ ATTN = [
     (2, 3, 1, 100, 1000, 32, [1000, 65], [100, 1], True),
     (1, 4, 2, 300, 640, 128, [639], [299], True),
     (1, 1, 1, 64, 6000, 64, [5990], None, True),        # split over workgroups
-    (32, 8, 8, 257, 257, 32, None, None, True),         # the larger workgroups
+    (32, 8, 8, 257, 257, 32, None, None, True),
     (32, 8, 8, 300, 64, 128, None, None, False),
+]
+
+
+def many_rows(heads, rows, L):
+    """Whether a bf16 call runs in the form for many rows and much work."""
+    return rows >= 128 and heads * rows * L >= 1 << 25
+
+
+MANY = [
+    (2, 8, 2, 301, 7001, 128, [7001, 65], [301, 100], True),
+    (1, 16, 16, 2100, 1001, 32, None, None, False),
+    (32, 8, 8, 257, 511, 64, [511, 1, 0, 64, 65, 300, 2, 511] * 4,
+     [257, 257, 3, 1, 200, 0, 257, 256] * 4, True),
+    (1, 8, 1, 129, 32600, 64, [32577], None, True),
+    (1, 2, 1, 65, 1 << 18, 32, [250001], None, False),
+    (3, 3, 3, 4000, 2800, 128, [2800, 0, 5], [4000, 17, 0], True),
+    (1, 1, 1, 128, 1 << 18, 128, [63], [127], True),
 ]
 
 
@@ -164,7 +181,7 @@ def reference(c, Q, kl, ql, G, causal, scale, strict):
             h = hq // G
             out = ref.attention(Q[b, hq].astype(np.float64), [x[b, h] for x in c.code],
                                 [(s[b, h], m[b, h]) for s, m in grp], n, r, causal, scale, strict,
-                                not strict and G * Lq >= 64)
+                                not strict and many_rows(B * H, G * Lq, L))
             O[b, hq], LSE[b, hq], P, tO[b, hq], tL[b, hq], tP = out
             W[b, h, :n] += P.sum(0)
             tW[b, h, :n] += tP.sum(0)
@@ -219,19 +236,27 @@ def test_attention(gpu_lib, B, Hq, H, Lq, L, d, key_len, q_len, causal, contract
                     (-0.5 if L == 333 else 1.0) / math.sqrt(d), contract, weights)
 
 
-@pytest.mark.parametrize("contract", ["fast_bf16", "strict_f32"])
-def test_attention_over_a_wide_range(gpu_lib, contract):
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("B,Hq,H,Lq,L,d,key_len,q_len,causal", MANY)
+def test_attention_of_many_rows(gpu_lib, B, Hq, H, Lq, L, d, key_len, q_len, causal, weights):
+    assert many_rows(B * H, Hq // H * Lq, L)
+    test_attention(gpu_lib, B, Hq, H, Lq, L, d, key_len, q_len, causal, "fast_bf16", weights)
+
+
+@pytest.mark.parametrize("contract,Lq,L", [("fast_bf16", 9, 900), ("strict_f32", 9, 900),
+                                           ("fast_bf16", 130, 65000)])
+def test_attention_over_a_wide_range(gpu_lib, contract, Lq, L):
     """Token scales and query rows of very different size, growing and falling
     along the sequence (the running units move both ways)."""
-    say("kv4 attention, wide range %s" % contract)
+    say("kv4 attention, wide range %s Lq%d" % (contract, Lq))
     rng = np.random.default_rng(5)
-    B, H, L, d = 1, 2, 900, 64
+    B, H, d = 1, 2, 64
     c = ref.Cache(B, H, L, d)
     size = np.exp(3.0 * np.sin(np.arange(L) / 40.0))[None, :, None]
     size[:, 500:520] = 1e4
     c.put(0, 0, np.arange(L), rows(rng, (H, L, d), "strict_f32"))
     c.put(1, 0, np.arange(L), (rows(rng, (H, L, d), "strict_f32") * size).astype(np.float32))
-    Q = rows(rng, (B, 4, 9, d), contract)
+    Q = rows(rng, (B, 4, Lq, d), contract)
     Q[0, :, 3] *= 2.0 ** -40
     Q[0, :, 4] *= 2.0 ** 4
     Q[0, :, 5] = 0
@@ -239,16 +264,16 @@ def test_attention_over_a_wide_range(gpu_lib, contract):
 
 
 @pytest.mark.parametrize("contract", ["fast_bf16", "strict_f32"])
-@pytest.mark.parametrize("Lq", [1, 20, 40])
-def test_attention_not_a_number(gpu_lib, contract, Lq):
+@pytest.mark.parametrize("Lq,L", [(1, 100), (20, 100), (40, 100), (512, 32768)])
+def test_attention_not_a_number(gpu_lib, contract, Lq, L):
     """A NaN token reaches the rows that see it, and its own group's channels of
     O if only its V is NaN; rows that do not see it are as without it."""
     import torch
     mg = gpu_lib
     say("kv4 attention with NaN %s Lq%d" % (contract, Lq))
     rng = np.random.default_rng(6)
-    B, H, L, d = 1, 1, 100, 128
-    n = 90
+    B, H, d = 1, 1, 128
+    n = L - 10
     c = filled(rng, B, H, L, d)
     dt = dtype_of(contract)
     Q = dev(rows(rng, (B, 2, Lq, d), contract), dt)

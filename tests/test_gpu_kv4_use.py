@@ -69,7 +69,8 @@ class Session:
 
 # few rows with kept scores; rows whose weights are recomputed; many rows
 SESSIONS = [dict(seed=1), dict(seed=2, Lq=5, d=128, contract="strict_f32"),
-            dict(seed=3, Lq=90, d=128), dict(seed=4, L=5000, n=4500, Lq=1, keep=900, d=32)]
+            dict(seed=3, Lq=90, d=128), dict(seed=4, L=5000, n=4500, Lq=1, keep=900, d=32),
+            dict(seed=8, B=1, Hq=16, H=4, L=9000, n=8500, Lq=241, keep=5000, d=128)]
 
 
 def expected(s):
@@ -162,14 +163,14 @@ def test_nothing_outside_the_buffers_is_written(gpu_lib, kwargs):
         assert bool((whole[:GUARD] == 0xA5).all()) and bool((whole[-GUARD:] == 0xA5).all()), name
 
 
-@pytest.mark.parametrize("Lq", [1, 40])
-def test_lengths_are_clamped(gpu_lib, Lq):
+@pytest.mark.parametrize("Lq,L", [(1, 90), (40, 90), (1400, 6100)])
+def test_lengths_are_clamped(gpu_lib, Lq, L):
     """Lengths above what there is, and below 0, mean all of it and nothing."""
     import torch
     mg = gpu_lib
     say("kv4: lengths out of range, Lq%d" % Lq)
     rng = np.random.default_rng(8)
-    B, Hq, H, L, d = 3, 4, 2, 90, 64
+    B, Hq, H, d = 3, 4, 2, 64
     cache = mg.kv4_cache(B, H, L, d)
     K, V = bf16(rng, B, H, L, d), bf16(rng, B, H, L, d)
     mg.mg_kv4_append(K, V, cache, None, ints(1 << 30, L, L), L=L)
@@ -209,7 +210,7 @@ def test_a_cache_beyond_32_bit_offsets(gpu_lib):
     mg.mg_kv4_read(small, outs[2], outs[3], ints(L - n), L=L)
     for b, s in ((outs[0], outs[2]), (outs[1], outs[3])):
         assert torch.equal(b, s.expand_as(b))
-    for Lq in (1, 64):
+    for Lq in (1, 64, 128):
         q = bf16(rng, 1, 1, Lq, d)
         wb, ws = torch.zeros(1, H, L, device="cuda"), torch.zeros(1, 1, L, device="cuda")
         kw = dict(L=L, causal=True, scale=0.2)
