@@ -101,25 +101,28 @@ void kv4_many(ManyArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int share = blockIdx.x / a.row_tiles;
-    // causal: the tiles of the last rows, which see the most, first
-    const int tile_at = blockIdx.x - share * a.row_tiles;
-    const int tile = a.causal ? a.row_tiles - 1 - tile_at : tile_at;
+    const int tile = blockIdx.x - share * a.row_tiles;
     const int bh = share / a.splits, split = share - bh * a.splits;
     const int rows = a.G * a.Lq;
     const Kv4Mask mask = sequence_mask(a.key_len, a.q_len, bh / a.H, a.L, a.Lq, a.causal);
 
-    const int r0 = kRows * tile + 32 * w, r = r0 + c;
+    // Four waves take rows from the front and four from the back: causal
+    // workgroups differ less in work, the first ones having the most.
+    const int front = kRows / 2 * tile, back = kRows / 2 * (2 * a.row_tiles - 1 - tile);
+    const int r0 = w < kManyWaves / 2 ? front + 32 * w : back + 32 * (w - kManyWaves / 2);
+    const int r = r0 + c;
     const bool in = r < rows;
     const int rr = in ? r : rows - 1, i = rr / a.G;
     const size_t at = ((size_t)bh * a.G + (rr - i * a.G)) * a.Lq + i;
     const int limit = mask.limit(i);
     // tokens that some row of the workgroup, some row of the wave, every row
     // of the wave sees
-    const int wg0 = kRows * tile;
-    const int end = wg0 / a.G < mask.rows
-        ? max(mask.limit(min((min(rows, wg0 + kRows) - 1) / a.G, mask.rows - 1)), 0) : 0;
-    const int wave_end = r0 < rows && r0 / a.G < mask.rows
-        ? max(mask.limit(min((min(rows, r0 + 32) - 1) / a.G, mask.rows - 1)), 0) : 0;
+    const auto end_of = [&](int from, int n) {
+        return from < rows && from / a.G < mask.rows
+            ? max(mask.limit(min((min(rows, from + n) - 1) / a.G, mask.rows - 1)), 0) : 0;
+    };
+    const int end = max(end_of(front, kRows / 2), end_of(back, kRows / 2));
+    const int wave_end = end_of(r0, 32);
     const int wave_all = r0 < rows ? mask.limit(r0 / a.G) : 0;
 
     const int tiles = (end + kTokens - 1) / kTokens, each = (tiles + a.splits - 1) / a.splits;
