@@ -17,6 +17,7 @@ namespace {
 
 constexpr int kWaves = 8;
 constexpr int kThreads = 64 * kWaves;
+constexpr int kUnits = 256;          // compute units
 constexpr int kTile = 32 * kWaves;   // tokens of a workgroup
 
 struct WeightArgs {
@@ -30,19 +31,24 @@ struct WeightArgs {
 };
 
 template <typename T, int D, int NP>
-__global__ __launch_bounds__(kThreads)
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 8)))
 void kv4_weights(WeightArgs a) {
     constexpr int NG = Kv4Dim<D>::kGroups, NS = D / 16, KR = D / 8;
     constexpr int PER = KR;   // threads that prepare a row, 8 channels each
     __shared__ __attribute__((aligned(16))) f16x8 Qs[2][NP][32 * (KR + 1)];
     __shared__ float Sum[2][2][32], Factor[2][32], Lse[2][32];
     __shared__ int Limit[2][32];
+    __shared__ __attribute__((aligned(16))) float Scale[kWaves][NG][32];
 
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int bh = blockIdx.x / (a.tiles * a.shares);
-    const int rest = blockIdx.x - bh * a.tiles * a.shares;
-    const int tile = rest / a.shares, share = rest - tile * a.shares;
+    // the first tiles, which causal rows see the most, first; where a compute unit
+    // gets two workgroups and no more, its second is the lighter the heavier the
+    // first is
+    const int all = gridDim.x, order = blockIdx.x;
+    const int item = all <= 2 * kUnits && order >= kUnits ? all - 1 - (order - kUnits) : order;
+    const int tile = item / (a.heads * a.shares), rest = item - tile * a.heads * a.shares;
+    const int bh = rest / a.shares, share = rest - bh * a.shares;
     const Kv4Mask mask = sequence_mask(a.key_len, a.q_len, bh / a.H, a.L, a.Lq, a.causal);
     const int j0 = kTile * tile;
     if (j0 >= mask.n) return;
@@ -63,12 +69,7 @@ void kv4_weights(WeightArgs a) {
 #pragma unroll
     for (int s = 0; s < NS; ++s)   // channels 16s + 8h + e: word 2s + h of the row
         code[s] = code_operand(kw[tok * KR + k_word<D>(2 * s + h)]);
-    float scale[NG][16];
-#pragma unroll
-    for (int v = 0; v < 16; ++v)
-#pragma unroll
-        for (int g = 0; g < NG; ++g)
-            scale[g][v] = group_scale(kp[(16 * (v >> 3) + 8 * h + (v & 7)) * NG + g]);
+    if (h < NG) Scale[w][h][c] = group_scale(kp[c * NG + h]);   // read by the wave itself
     const float low = NG == 2 || h == 0 ? group_min(kp[tok * NG + (NG == 2 ? h : 0)]) : 0.f;
 
     // preparing rows: thread r * PER + k takes channels 8k..8k+7 of row r
@@ -77,16 +78,22 @@ void kv4_weights(WeightArgs a) {
     float x[8];
     float lse = 0.f;
     int limit = 0;
-    auto fetch = [&](int block) {
+    // its query row i and head g in the next block, a block's step of both
+    int i = (32 * begin + pr) / a.G, g = 32 * begin + pr - i * a.G;
+    const int step_i = 32 / a.G, step_g = 32 - step_i * a.G;
+    const T *qs = static_cast<const T *>(a.Q) + (size_t)bh * a.G * a.Lq * D + 8 * pk;
+    const float *lses = a.LSE + (size_t)bh * a.G * a.Lq;
+    auto fetch = [&](int block) {   // called for one block after the other
         if (!prepares) return;
-        const int r = 32 * block + pr;
-        const bool in = r < rows && block < stop;
-        const int i = in ? r / a.G : 0, g = in ? r - i * a.G : 0;
-        const size_t at = ((size_t)bh * a.G + g) * a.Lq + i;
-        load_row(x, static_cast<const T *>(a.Q) + at * D + 8 * pk);
-        lse = a.LSE[at];
+        const bool in = i < mask.rows && block < stop;
+        const int at = in ? g * a.Lq + i : 0;
+        load_row(x, qs + (size_t)at * D);
+        lse = lses[at];
         // nothing from rows without sight (LSE -inf)
         limit = in && lse != -INFINITY ? mask.limit(i) : 0;
+        g += step_g;
+        i += step_i + (g >= a.G ? 1 : 0);
+        g -= g >= a.G ? a.G : 0;
     };
     auto put = [&](int buf) {
         if (!prepares) return;
@@ -97,15 +104,15 @@ void kv4_weights(WeightArgs a) {
         const int exponent = __builtin_amdgcn_frexp_expf(top);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            sum += ldexpf(x[e], -exponent);
             x[e] = ldexpf(x[e], 15 - exponent);
+            sum += x[e];
         }
         sum = sum_of<PER / NG>(sum);
         f16x8 part[NP];
         split_operand<NP>(part, x);
 #pragma unroll
         for (int p = 0; p < NP; ++p) Qs[buf][p][piece<KR>(pr, pk)] = part[p];
-        if (pk % (PER / NG) == 0) Sum[buf][pk / (PER / NG)][pr] = sum * 0x1p6f;
+        if (pk % (PER / NG) == 0) Sum[buf][pk / (PER / NG)][pr] = sum * 0x1p-9f;
         if (pk == 0) {
             if (NG == 1) Sum[buf][1][pr] = 0.f;
             Factor[buf][pr] = row_factor(a.scale_log2, exponent);
@@ -124,27 +131,35 @@ void kv4_weights(WeightArgs a) {
         __syncthreads();
         for (int block = begin; block < stop; ++block) {
             const int buf = (block - begin) & 1;
-            f32x16 part[NG];
+            f32x16 s = mfma32x32x2(low, Sum[buf][h][c], zero16());
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                part[g] = zero16();
+                f32x16 part = zero16();
 #pragma unroll
-                for (int s = g * (NS / NG); s < (g + 1) * (NS / NG); ++s)
+                for (int k = g * (NS / NG); k < (g + 1) * (NS / NG); ++k)
 #pragma unroll
                     for (int p = NP - 1; p >= 0; --p)
-                        part[g] = mfma32x32x16f16(code[s], Qs[buf][p][piece<KR>(c, 2 * s + h)],
-                                                  part[g]);
+                        part = mfma32x32x16f16(code[k], Qs[buf][p][piece<KR>(c, 2 * k + h)], part);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const f32x4 scale = *reinterpret_cast<const f32x4 *>(
+                        &Scale[w][g][16 * (u >> 1) + 8 * h + 4 * (u & 1)]);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        s[4 * u + v] = fmaf(part[4 * u + v], scale[v], s[4 * u + v]);
+                }
             }
-            f32x16 s = mfma32x32x2(low, Sum[buf][h][c], zero16());
             const float factor = Factor[buf][c], off = Lse[buf][c];
             const int left = Limit[buf][c] - mine - 8 * h;
+            if (__all(left > 23)) {   // every row sees every token
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                float y = s[v];
+                for (int v = 0; v < 16; ++v) sum[v] += exp2_fast(fmaf(s[v], factor, -off));
+            } else {
 #pragma unroll
-                for (int g = 0; g < NG; ++g) y = fmaf(part[g][v], scale[g][v], y);
-                const float p = exp2_fast(fmaf(y, factor, -off));
-                sum[v] += 16 * (v >> 3) + (v & 7) < left ? p : 0.f;
+                for (int v = 0; v < 16; ++v) {
+                    const float p = exp2_fast(fmaf(s[v], factor, -off));
+                    sum[v] += 16 * (v >> 3) + (v & 7) < left ? p : 0.f;
+                }
             }
             put(buf ^ 1);
             fetch(block + 2);

@@ -47,11 +47,13 @@ Kv4Plan kv4_plan(const Kv4Attn &p, bool weights, bool bf16) {
         plan.bytes += host::round256((size_t)(heads * rows) * kv4_padded(p.L) * 4);
     }
     if (weights && !plan.scores) {
-        // enough workgroups of 256 tokens for two on every compute unit, with at
-        // least eight blocks of 32 rows each
+        // four workgroups of 256 tokens a compute unit, which even out how much
+        // causal rows see of them, each with 15 blocks of 32 rows or more (4 x 4
+        // heads, 4,000 rows, 1,000 tokens of 64: 27 us with 8 shares, 34 with 16;
+        // 16 heads, 16,384 rows, 4,096 tokens of 128: 419 with 2, 286 with 4 or 8)
         const int64_t groups = heads * cdiv(p.L, 256);
-        plan.shares = (int)std::min<int64_t>((512 + groups - 1) / groups,
-                                             std::max<int64_t>(1, rows / 256));
+        plan.shares = (int)std::min<int64_t>((1024 + groups - 1) / groups,
+                                             std::max<int64_t>(1, rows / 480));
         if (plan.shares > 1) {
             plan.sums = plan.bytes;
             plan.bytes += host::round256((size_t)plan.shares * heads * kv4_padded(p.L) * 4);
