@@ -24,10 +24,11 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 2048;
+constexpr int kList = 8192;   // keys
 
-// Order-preserving whole number of a weight; NaN lowest, -0 as 0.
+// Order-preserving whole number of a weight; NaN lowest, -0 as 0.  No weight has 0.
 __device__ __forceinline__ uint32_t weight_key(float w) {
-    if (w != w) return 0;
+    if (w != w) return 1;
     const uint32_t u = __float_as_uint(w == 0.f ? 0.f : w);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
@@ -61,8 +62,10 @@ void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
                 const int32_t *key_len, int H, int L, int keep, int recent) {
     __shared__ uint32_t hist[kBins];
     __shared__ uint32_t sums[kWaves];
-    __shared__ uint32_t found[2];   // digit, and how many of its bin stay
+    __shared__ uint32_t found[3];   // digit, how many of its bin stay, how many it has
     __shared__ uint32_t counts[SLABS > 0 ? SLABS * kWaves : 1];
+    constexpr bool LISTS = SLABS > 4;   // (4,096 tokens: 9.7 us with a list, 8.9 without)
+    __shared__ uint32_t list[LISTS ? kList : 1];
     const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const float *w = weight + (size_t)bh * L;
@@ -82,34 +85,36 @@ void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
     uint32_t want = keep - recent;   // of the old tokens; old > want
     for (int p = tid; p < recent; p += kThreads) to[want + p] = old + p;
     if (want == 0) return;
+    // the keys of the thread's turns; 0 behind the old tokens
+    const int turns = (old + kThreads - 1) / kThreads;
+    auto key_of = [&](int i, float x) {
+        return kThreads * i + tid < old ? weight_key(x) : 0u;
+    };
     uint32_t kept[KEYS];
 #pragma unroll
-    for (int i = 0; i < KEYS; ++i) kept[i] = SLABS > 0 ? weight_key(raw[i]) : 0u;
-    // token and key of the thread's i-th turn
-    const int turns = SLABS > 0 ? KEYS : (old + kThreads - 1) / kThreads;
+    for (int i = 0; i < KEYS; ++i) kept[i] = SLABS > 0 ? key_of(i, raw[i]) : 0u;
     auto each = [&](auto &&f) {
         if (SLABS > 0) {
 #pragma unroll
-            for (int i = 0; i < KEYS; ++i) f(i, kThreads * i + tid, kept[i]);
+            for (int i = 0; i < KEYS; ++i) f(kept[i]);
         } else {
-            for (int i = 0; i < turns; ++i) {
-                const int j = kThreads * i + tid;
-                f(i, j, weight_key(w[min(j, L - 1)]));
-            }
+            for (int i = 0; i < turns; ++i) f(key_of(i, w[min(kThreads * i + tid, L - 1)]));
         }
     };
 
-    // the key of rank `want` from the top, digit by digit
+    // The key of rank `want` from the top, digit by digit.  The first digit of most
+    // weights is one of few; the keys that share the one found go to a list, if they
+    // fit, for the other two passes.
     uint32_t prefix = 0;
-    int shift = 32;
+    int shift = 32, listed = -1;
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
         const int bits = pass == 2 ? 10 : 11, below = shift - bits;
         const uint32_t mask = (1u << bits) - 1;
         for (int k = tid; k < kBins; k += kThreads) hist[k] = 0;
         __syncthreads();
-        each([&](int, int j, uint32_t key) {
-            const bool in = j < old && (pass == 0 || (key ^ prefix) >> shift == 0);
+        auto count = [&](uint32_t key) {
+            const bool in = pass == 0 || (key ^ prefix) >> shift == 0;
             const uint64_t votes = __ballot(in);
             if (votes == 0) return;
             const uint32_t digit = (key >> below) & mask;
@@ -117,7 +122,14 @@ void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
             const uint64_t same = __ballot(in && digit == first);
             if (in && digit != first) atomicAdd(&hist[digit], 1u);
             if (lane == 0) atomicAdd(&hist[first], (uint32_t)__popcll(same));
-        });
+        };
+        if (listed < 0)
+            each(count);
+        else   // (0, which is behind the list, shares no digit with what is sought but 0)
+            for (int k = 0; k < listed; k += kThreads) {
+                const bool there = k + tid < listed;
+                count(there ? list[k + tid] : 0u);
+            }
         __syncthreads();
         // threads take bins from the top, two each
         const int bin = kBins - 1 - 2 * tid;
@@ -127,26 +139,36 @@ void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
             const bool second = before + h0 < want;
             found[0] = second ? bin - 1 : bin;
             found[1] = want - before - (second ? h0 : 0u);
+            found[2] = second ? h1 : h0;
         }
         __syncthreads();
         prefix |= found[0] << below;
         want = found[1];
         shift = below;
+        if (LISTS && pass == 0 && found[2] <= kList) {
+            uint32_t n_in = 0;
+            each([&](uint32_t key) { n_in += key >> 21 == prefix >> 21 ? 1u : 0u; });
+            uint32_t at = scan_group(n_in, sums, lane, wave) - n_in;
+            each([&](uint32_t key) {
+                if (key >> 21 == prefix >> 21) list[at++] = key;
+            });
+            listed = (int)found[2];   // all of them; the next barrier is before they are read
+        }
     }
 
     // every key above prefix stays, and the first `want` that equal it
     const uint64_t lower = (1ull << lane) - 1;
-    auto place = [&](int j, uint32_t key, uint64_t gt, uint64_t eq, uint32_t up, uint32_t same) {
+    auto place = [&](int i, uint32_t key, uint64_t gt, uint64_t eq, uint32_t up, uint32_t same) {
         const uint32_t u = up + __popcll(gt & lower), s = same + __popcll(eq & lower);
-        if (j < old && (key > prefix || (key == prefix && s < want))) to[u + min(s, want)] = j;
+        if (key > prefix || (key == prefix && s < want))
+            to[u + min(s, want)] = kThreads * i + tid;
     };
     if constexpr (SLABS > 0) {
         // counts of each 64 tokens: above in the upper half, equal in the lower
 #pragma unroll
         for (int i = 0; i < KEYS; ++i) {
-            const int j = kThreads * i + tid;
-            const uint32_t gt = __popcll(__ballot(j < old && kept[i] > prefix));
-            const uint32_t eq = __popcll(__ballot(j < old && kept[i] == prefix));
+            const uint32_t gt = __popcll(__ballot(kept[i] > prefix));
+            const uint32_t eq = __popcll(__ballot(kept[i] == prefix));
             if (lane == 0) counts[kWaves * i + wave] = gt << 16 | eq;
         }
         __syncthreads();
@@ -156,21 +178,17 @@ void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < KEYS; ++i) {
-            const int j = kThreads * i + tid;
-            const uint64_t gt = __ballot(j < old && kept[i] > prefix);
-            const uint64_t eq = __ballot(j < old && kept[i] == prefix);
+            const uint64_t gt = __ballot(kept[i] > prefix), eq = __ballot(kept[i] == prefix);
             const uint32_t at = counts[kWaves * i + wave];
-            place(j, kept[i], gt, eq, at >> 16, at & 0xffffu);
+            if ((gt | eq) != 0) place(i, kept[i], gt, eq, at >> 16, at & 0xffffu);
         }
     } else {
         // the same, a slab at a time
         uint32_t up = 0, same = 0;
 #pragma unroll 1
         for (int i = 0; i < turns; ++i) {
-            const int j = kThreads * i + tid;
-            const uint32_t key = weight_key(w[min(j, L - 1)]);
-            const uint64_t gt = __ballot(j < old && key > prefix);
-            const uint64_t eq = __ballot(j < old && key == prefix);
+            const uint32_t key = key_of(i, w[min(kThreads * i + tid, L - 1)]);
+            const uint64_t gt = __ballot(key > prefix), eq = __ballot(key == prefix);
             if (lane == 0) sums[wave] = (uint32_t)__popcll(gt) << 16 | (uint32_t)__popcll(eq);
             __syncthreads();
             uint32_t here = 0, all = 0;
@@ -179,7 +197,7 @@ void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
                 here += k < wave ? sums[k] : 0u;
                 all += sums[k];
             }
-            place(j, key, gt, eq, up + (here >> 16), same + (here & 0xffffu));
+            place(i, key, gt, eq, up + (here >> 16), same + (here & 0xffffu));
             up += all >> 16;
             same += all & 0xffffu;
             __syncthreads();

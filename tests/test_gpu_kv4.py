@@ -362,6 +362,26 @@ def test_evict(gpu_lib, B, H, L, d, keep, recent, key_len, in_place):
         assert np.array_equal(host(raw), c.to_bytes())
 
 
+@pytest.mark.parametrize("L,keep,recent", [(9000, 4000, 10), (30000, 12000, 0), (33000, 100, 50)])
+def test_evict_by_weights_of_every_kind(gpu_lib, L, keep, recent):
+    """All weights equal, all NaN, spread over the whole range, negative, and
+    few above many."""
+    import torch
+    mg = gpu_lib
+    say("kv4 evict L%d, weights of every kind" % L)
+    rng = np.random.default_rng(L)
+    bits = rng.integers(0, 1 << 32, L, dtype=np.uint32).view(np.float32)   # NaN and inf too
+    w = np.stack([np.full(L, 0.125), np.full(L, np.nan), bits,
+                  -np.exp(rng.standard_normal(L)),
+                  np.where(rng.random(L) < 0.01, 2.0, 1e-30 * rng.random(L))]).astype(np.float32)
+    H = len(w)
+    cache = mg.kv4_cache(1, H, L, 32)
+    index = torch.empty(1, H, keep, dtype=torch.int32, device="cuda")
+    mg.mg_kv4_evict(cache, dev(w[None]), index, dev(np.zeros(1, np.int32)), d=32, recent=recent)
+    for h in range(H):
+        assert np.array_equal(host(index)[0, h], ref.evict(w[h], L, keep, recent)), h
+
+
 @pytest.mark.parametrize("contract", ["fast_bf16", "strict_f32"])
 def test_a_served_sequence(gpu_lib, contract):
     """Prompt, decode steps, eviction, more steps: after each, attention and
