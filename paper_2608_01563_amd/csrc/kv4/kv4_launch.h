@@ -29,7 +29,7 @@ inline int64_t kv4_rows(const Kv4Attn &p) { return (int64_t)p.G * p.Lq; }
 
 // How one call runs.
 struct Kv4Plan {
-    int rows;          // of a workgroup: 16 (kv4_rows), 128 or 256 (kv4_many)
+    int rows;          // of a workgroup: 16 (kv4_rows) or 256 (kv4_many)
     int splits;        // workgroups that share a row tile's tokens
     int chunk;         // kv4_rows: blocks of 32 tokens of each
     bool scores;       // weights come from scores the forward keeps
