@@ -29,8 +29,10 @@ struct Octet {
 };
 __device__ __forceinline__ bool take_octet(Octet *o, int B, int H, int n, int L, int octets,
                                            const int32_t *start, const int32_t *count) {
-    const int64_t id = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-    const int bh = (int)(id / octets), k = (int)(id - (int64_t)bh * octets);
+    // (fewer than 2^28 octets)
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t id = blockIdx.x * (kThreads / 64) + wave;
+    const int bh = (int)(id / (uint32_t)octets), k = (int)(id - (uint32_t)bh * octets);
     if (bh >= B * H) return false;
     const int b = bh / H;
     // clamped so that at + j cannot overflow; beyond these no row lands in [0, L)
@@ -73,12 +75,14 @@ struct Pieces {
 // words; all codes 0 where the lane holds no row.
 //
 // code = round((x - min) / scale): the quotient of the f32 difference, correctly
-// rounded (a product with 1 / scale and one exact residual), so that ties, which
-// are common among bf16 values, go to the even code when kRound is added.  A bf16
+// rounded (a product with 1 / scale, at most 2^125 and normal, to an ulp or so, and
+// one exact residual), so that ties, which are common among bf16 values, go to the
+// even code when kRound is added.  A bf16
 // difference is exact unless x and min are 2^16 apart.  f32 values within 2^-20 of a
 // border are settled exactly, with the rounding error of the difference.
 constexpr float kRound = 0x1p23f;   // ulp 1: adding it rounds, the code is in the low bits
 constexpr uint32_t kRoundBits = 0x4b000000u;
+constexpr float kFifteenth = 1.f / 15.f;
 
 template <typename T, int D>
 __device__ __forceinline__ void quantise(const float (&x)[Pieces<T, D>::PIECES][Pieces<T, D>::PIECE],
@@ -105,12 +109,15 @@ __device__ __forceinline__ void quantise(const float (&x)[Pieces<T, D>::PIECES][
         lo = least(lo, other_lane<2>(lo));
         hi = most(hi, other_lane<2>(hi));
         const uint32_t mb = to_bf16(lo);
-        uint32_t sb = to_bf16((hi - lo) / 15.f);   // NaN or infinite where a value is
+        // a fifteenth, correctly rounded as above; NaN or infinite where a value is
+        const float wide = hi - lo, part = wide * kFifteenth;
+        uint32_t sb = to_bf16(wide < INFINITY ? fmaf(fmaf(-15.f, part, wide), kFifteenth, part)
+                                              : wide);
         if (sb < 0x0080u) sb = 0;   // below the smallest normal
         const float mn = bf16_to_f32((uint16_t)mb), sc = bf16_to_f32((uint16_t)sb);
         const bool good = fabsf(mn) < INFINITY && sc < INFINITY;
         const bool flat = !good || sb == 0 || !there;
-        const float inv = flat ? 0.f : 1.f / sc, from = flat ? 0.f : mn;
+        const float inv = flat ? 0.f : __builtin_amdgcn_rcpf(sc), from = flat ? 0.f : mn;
         word[g] = good ? sb << 16 | mb : 0x7fc07fc0u;
 #pragma unroll
         for (int i = g * P::PER; i < (g + 1) * P::PER; ++i)
