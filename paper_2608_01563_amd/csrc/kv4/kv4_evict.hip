@@ -161,7 +161,12 @@ void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
         }
     }
 
-    // every key above prefix stays, and the first `want` that equal it
+    // Every key above prefix stays, and the first `want` that equal it: all of them,
+    // most often, and then one comparison does.
+    if (found[2] == want) {
+        prefix -= 1;
+        want = 0;
+    }
     const uint64_t lower = (1ull << lane) - 1;
     auto place = [&](int i, uint32_t key, uint64_t gt, uint64_t eq, uint32_t up, uint32_t same) {
         const uint32_t u = up + __popcll(gt & lower), s = same + __popcll(eq & lower);
@@ -172,9 +177,9 @@ void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
         // counts of each 64 tokens: above in the upper half, equal in the lower
 #pragma unroll
         for (int i = 0; i < KEYS; ++i) {
-            const uint32_t gt = __popcll(__ballot(kept[i] > prefix));
-            const uint32_t eq = __popcll(__ballot(kept[i] == prefix));
-            if (lane == 0) counts[kWaves * i + wave] = gt << 16 | eq;
+            uint32_t n_in = __popcll(__ballot(kept[i] > prefix)) << 16;
+            if (want > 0) n_in |= __popcll(__ballot(kept[i] == prefix));
+            if (lane == 0) counts[kWaves * i + wave] = n_in;
         }
         __syncthreads();
         const uint32_t mine = tid < SLABS * kWaves ? counts[tid] : 0u;
@@ -183,9 +188,13 @@ void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < KEYS; ++i) {
-            const uint64_t gt = __ballot(kept[i] > prefix), eq = __ballot(kept[i] == prefix);
             const uint32_t at = counts[kWaves * i + wave];
-            if ((gt | eq) != 0) place(i, kept[i], gt, eq, at >> 16, at & 0xffffu);
+            const uint64_t gt = __ballot(kept[i] > prefix);
+            if (want == 0) {
+                if (kept[i] > prefix) to[(at >> 16) + __popcll(gt & lower)] = kThreads * i + tid;
+            } else {
+                place(i, kept[i], gt, __ballot(kept[i] == prefix), at >> 16, at & 0xffffu);
+            }
         }
     } else {
         // the same, a slab at a time
