@@ -29,7 +29,7 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 2048;
-constexpr int kList = 8192;   // keys
+constexpr int kList = 4 * kBins;   // keys
 
 // Order-preserving whole number of a weight; NaN lowest, -0 as 0.  No weight has 0.
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -116,7 +116,10 @@ void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
     for (int pass = 0; pass < 3; ++pass) {
         const int bits = pass == 2 ? 10 : 11, below = shift - bits;
         const uint32_t mask = (1u << bits) - 1;
+        const bool apart = LISTS && pass == 0;   // counted in four places, lane by lane
         for (int k = tid; k < kBins; k += kThreads) hist[k] = 0;
+        if (apart)
+            for (int k = tid; k < 4 * kBins; k += kThreads) list[k] = 0;
         __syncthreads();
         auto count = [&](uint32_t key) {
             const bool in = pass == 0 || (key ^ prefix) >> shift == 0;
@@ -128,7 +131,9 @@ void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
             if (in && digit != first) atomicAdd(&hist[digit], 1u);
             if (lane == 0) atomicAdd(&hist[first], (uint32_t)__popcll(same));
         };
-        if (listed < 0)
+        if (apart)
+            each([&](uint32_t key) { atomicAdd(&list[(key >> 21) * 4 + (lane & 3)], 1u); });
+        else if (listed < 0)
             each(count);
         else   // (0, which is behind the list, shares no digit with what is sought but 0)
             for (int k = 0; k < listed; k += kThreads) {
@@ -138,7 +143,12 @@ void kv4_select(const float *__restrict__ weight, int32_t *__restrict__ index,
         __syncthreads();
         // threads take bins from the top, two each
         const int bin = kBins - 1 - 2 * tid;
-        const uint32_t h0 = hist[bin], h1 = hist[bin - 1];
+        uint32_t h0 = hist[bin], h1 = hist[bin - 1];
+        if (apart)
+            for (int k = 0; k < 4; ++k) {
+                h0 += list[4 * bin + k];
+                h1 += list[4 * (bin - 1) + k];
+            }
         const uint32_t upto = scan_group(h0 + h1, sums, lane, wave), before = upto - h0 - h1;
         if (before < want && upto >= want) {
             const bool second = before + h0 < want;
