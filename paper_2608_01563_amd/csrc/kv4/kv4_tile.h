@@ -64,7 +64,10 @@ template <int NP>
 __device__ __forceinline__ void split_operand(f16x8 (&out)[NP], const float (&x)[8]) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const float v = x[slot_value(k)];
+        float v = x[slot_value(k)];
+        // Rounded to f32 here: where v is a product, a conversion fused with it rounds
+        // once and, next to a tie, to another h than the one taken off below.
+        if constexpr (NP > 1) asm("" : "+v"(v));
         const _Float16 h = (_Float16)v;
         out[0][k] = h;
         if constexpr (NP > 1) out[1][k] = (_Float16)(v - (float)h);

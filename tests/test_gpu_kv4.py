@@ -236,6 +236,19 @@ def test_attention(gpu_lib, B, Hq, H, Lq, L, d, key_len, q_len, causal, contract
                     (-0.5 if L == 333 else 1.0) / math.sqrt(d), contract, weights)
 
 
+@pytest.mark.parametrize("d", [32, 128])
+def test_strict_parts_belong_together(gpu_lib, d):
+    """Few tokens of nearly equal probability leave bounds of some 1e-5; of 10^5
+    probabilities some lie next to a tie of f16, where the first part must be the
+    one that the second was taken from (else O is off by up to 1e-4)."""
+    say("kv4 strict, parts of probabilities d%d" % d)
+    rng = np.random.default_rng(12)
+    c = filled(rng, 1, 1, 8, d)
+    Q = rows(rng, (1, 8, 2000, d), "strict_f32")
+    check_attention(gpu_lib, rng, c, dev(c.to_bytes()), Q, None, None, False, 1e-2, "strict_f32",
+                    False)
+
+
 @pytest.mark.parametrize("weights", [False, True])
 @pytest.mark.parametrize("B,Hq,H,Lq,L,d,key_len,q_len,causal", MANY)
 def test_attention_of_many_rows(gpu_lib, B, Hq, H, Lq, L, d, key_len, q_len, causal, weights):
