@@ -6,8 +6,10 @@
 // depend on the order of the counting), then writes the indices of what stays
 // in order: counts of every 64 tokens, one scan over them, places.  Of the tokens
 // that equal the last weight, the first ones stay.  Weights are read once and kept
-// in registers for sequences up to 32,768 tokens; counting takes a wave's most
-// common first digit in one addition (many tokens share a small weight).
+// in registers for sequences up to 32,768 tokens.  Many tokens share a digit, so
+// LDS additions meet: from 4,097 tokens on first digits are counted in four places
+// (16 heads of 32,768: 24 us, 26 without), else a wave adds its first lane's digit
+// once for all that share it (37 us with plain additions, 27 so).
 //
 // kv4_compact: moves rows to where select's indices put them.  A workgroup owns
 // whole 128-byte columns of the cache (the K rows, 128 bytes of the V octets, or the
@@ -16,7 +18,7 @@
 // another cache, stretches are shared out over workgroups.
 //
 // 64 heads cut from 4,096 to 1,024 tokens of 128 channels: 9 us to select, 11 to
-// move; 16 heads from up to 32,768 to 8,192: 27 and 18.  Selection is bound by the
+// move; 16 heads from up to 32,768 to 8,192: 24 and 18.  Selection is bound by the
 // vector and LDS work of the one compute unit a head has (5 us to load and turn
 // into keys), moving by the latency of rows that follow their index.
 #include "cdiv.h"

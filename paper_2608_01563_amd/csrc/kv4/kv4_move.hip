@@ -10,8 +10,8 @@
 //
 // Both directions are bound by HBM: 2 D elements and D + 8 max(1, D/64) cache
 // bytes a token and head.  4 x 8 heads of up to 8,192 bf16 tokens of 128 channels
-// (96 MB each way, less where sequences are shorter): 30 us written and 23 read
-// back, 3.6 TB/s; of the f32 reads of 134 MB 25 us, 5.9 TB/s.  A wave an octet,
+// (96 MB each way): 29 us written and 22 read back, 3.6 TB/s with both launches;
+// reading 134 MB of f32 25 us, 5.9 TB/s.  A wave an octet,
 // because V's words then have one writer and rows are read whole.
 #include "kv4_device.h"
 #include "kv4_launch.h"
