@@ -17,7 +17,7 @@
 // A tile's words are loaded an iteration before they are unpacked, and its
 // group words one before that, because unpacking V needs them from LDS.
 //
-// 2 x 32 heads, 2,048 rows over 8,192 tokens of 128 channels, causal: 582 us, 826
+// 2 x 32 heads, 2,048 rows over 8,192 tokens of 128 channels, causal: 571 us, 842
 // TFLOP/s where a large bf16 product reaches 1,206.  The matrix units are busy 40 %
 // of the time; operand reads from LDS cost the most of the rest (without them 475
 // of then 603 us; without unpacking 570, without the exponentials 590).  32x32

@@ -9,10 +9,10 @@
 // lanes until the end.  Where token tiles are too few for the GPU, the rows are
 // shared out too, and shares of a weight are added in order by a second kernel.
 //
-// 16 heads of 16,384 causal rows over 4,096 tokens of 128 channels: 286 us, half of
+// 16 heads of 16,384 causal rows over 4,096 tokens of 128 channels: 273 us, half of
 // it vector instructions (about 200 for 32 x 32 probabilities, 16 of them
 // exponentials), a quarter matrix products.  Two workgroups a compute unit need at
-// most 128 registers, so scales come from LDS (with them in registers: 416 us).
+// most 128 registers, so scales come from LDS (with them in registers: 416 us where this made 286).
 #include "cdiv.h"
 #include "kv4_launch.h"
 #include "kv4_tile.h"
