@@ -234,6 +234,33 @@ def test_a_cache_beyond_32_bit_offsets(gpu_lib):
                                                   outs[2][0, 0][at.clamp(min=0)], 0.0))
 
 
+def test_the_most_heads(gpu_lib):
+    """2^19 heads, whose grids come near 2^32 threads: every one as a single one."""
+    import torch
+    mg = gpu_lib
+    say("kv4: 2^19 heads")
+    rng = np.random.default_rng(13)
+    B, H, L, d, n, keep = 1 << 10, 1 << 9, 32, 128, 21, 7
+
+    def session(b, h, K, V, Q):
+        cache, w = mg.kv4_cache(b, h, L, d), torch.zeros(b, h, L, device="cuda")
+        k, v, q = (t.expand(b, h, -1, d).contiguous() for t in (K, V, Q))
+        length = ints(*([n] * b))
+        mg.mg_kv4_append(k, v, cache, L=L, weight=w)
+        O, LSE = mg.attention_forward_kv4(q, cache, H=h, L=L, causal=True, scale=0.1,
+                                          key_len=length, weight=w)
+        index = torch.empty(b, h, keep, dtype=torch.int32, device="cuda")
+        mg.mg_kv4_evict(cache, w, index, length, length, d=d, recent=2)
+        out = torch.zeros(b, h, keep, d, dtype=torch.bfloat16, device="cuda")
+        mg.mg_kv4_read(cache, out, torch.empty_like(out), L=L)
+        return O, LSE, w[:, :, :n], index, out, length
+
+    data = [bf16(rng, 1, 1, m, d) for m in (n, n, 1)]
+    few, many = session(1, 1, *data), session(B, H, *data)
+    for a, b in zip(few, many):
+        assert bool((b == a).all())
+
+
 def test_refusals(gpu_lib):
     import torch
     mg = gpu_lib
