@@ -32,7 +32,7 @@ namespace {
 constexpr int kTokens = 64, kManyWaves = 8, kRows = 32 * kManyWaves;
 constexpr float kManySlack = 4.f;
 constexpr int kLift = 11;      // P is at most 2^(slack + kLift) = 2^15
-constexpr int kManyExp = 100;  // bound on E
+constexpr int kManyExp = -100; // least E
 
 struct ManyArgs {
     const uint16_t *Q;
@@ -160,7 +160,7 @@ void kv4_many(ManyArgs a) {
         for (int g = 0; g < NG; ++g)
             params[g] = w < 2 && k < mask.n ? p[(size_t)k * NG + g] : 0u;
     };
-    int bound = -kManyExp;   // E, in wave 1
+    int bound = kManyExp;   // E, in wave 1
     auto put_params = [&](int t) {
         const int b = t & 3;
         if (w == 0) {
@@ -183,7 +183,7 @@ void kv4_many(ManyArgs a) {
                 if (lane == 0) Bad[b][g] = bad;
             }
             most = max_of_wave(most);
-            bound = max(bound, min(kManyExp, __builtin_amdgcn_frexp_expf(most)));
+            if (most > 0.f) bound = max(bound, __builtin_amdgcn_frexp_expf(most));
             if (lane == 0) Es[b] = bound;
             // in the octet's slot order
             const int slot = (lane & 0x38) | (lane & 1) << 2 | (lane & 6) >> 1;
@@ -222,7 +222,7 @@ void kv4_many(ManyArgs a) {
     q.load(a.Q + at * D, in, h, a.scale_log2 < 0.f);
     const float factor = positive_factor(a.scale_log2, q.exponent);
     float m = -INFINITY, l = 0.f;
-    int E = -kManyExp;
+    int E = kManyExp;
     f32x16 o[NB];   // O^T[32 b + 8 (v/4) + 4h + v%4][row c] 2^(kLift + 15 - E)
 #pragma unroll
     for (int b = 0; b < NB; ++b) o[b] = zero16();

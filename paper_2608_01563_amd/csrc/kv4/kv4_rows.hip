@@ -40,6 +40,9 @@ constexpr int kRows = 16;
 constexpr float kRowSlack = 4.f;
 constexpr int kRaise = 11;    // 2^(slack + 11) = 2^15 at most
 constexpr int kExpMax = 100;  // bound on the scales' exponent (|V| about 2^104)
+// Least e, and how far a minimum may lie above 2^e: sums of 2^24 p and p min in
+// units of 2^(e - kRaise) stay below 2^(4 + 11 + 80 + 24).
+constexpr int kExpMin = -80;
 
 struct RowsArgs {
     const void *Q;
@@ -166,7 +169,7 @@ void kv4_rows(RowsArgs a) {
     const int stop = min((end + 31) / 32, begin + a.chunk);
 
     float m = -INFINITY;               // running maximum (base 2) rounded up, of the row
-    int e = -kExpMax;                  // V's scales are below 2^e
+    int e = kExpMin;                   // V's scales are below 2^e, its minima below 2^(e + 80)
     uint32_t most = 0;                 // ... as a bound on their group words
     float l = 0.f;                     // sum of p 2^(kRaise - e)
     float low[NG];                     // sums of p base in the same units
@@ -214,7 +217,9 @@ void kv4_rows(RowsArgs a) {
         mx = max_over_groups(mx) * factor;
         // NaN scales (a token that is not finite) move nothing
         const uint32_t mine = words.value(lane);
-        const uint32_t top = mine < 0x7f800000u ? mine : 0u;
+        constexpr uint32_t kBelow = (uint32_t)-kExpMin << 23;
+        const uint32_t low_bound = max((mine & 0x7fffu) << 16, kBelow) - kBelow;
+        const uint32_t top = mine < 0x7f800000u ? max(mine, low_bound) : 0u;
         if (__any(mx > m + kRowSlack || top > most)) {
             const float m_new = fmaxf(m, ceilf(mx));
             // finite words order as the scales in their upper halves do

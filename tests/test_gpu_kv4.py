@@ -276,6 +276,46 @@ def test_attention_over_a_wide_range(gpu_lib, contract, Lq, L):
     check_attention(gpu_lib, rng, c, dev(c.to_bytes()), Q, None, None, True, 0.3, contract, True)
 
 
+@pytest.mark.parametrize("contract,Lq,L", [("fast_bf16", 3, 70), ("strict_f32", 3, 70),
+                                           ("fast_bf16", 256, 65600)])
+@pytest.mark.parametrize("size", [0.0, 1e-30, 1.0, 1e6, 2.0 ** 100])
+def test_attention_of_flat_values(gpu_lib, contract, Lq, L, size):
+    """V rows whose channels are all the same have scale 0: only minima."""
+    say("kv4 attention, flat values of %g, %s Lq%d" % (size, contract, Lq))
+    rng = np.random.default_rng(14)
+    H, d = 1, 32
+    c = ref.Cache(1, H, L, d)
+    c.put(0, 0, np.arange(L), rows(rng, (H, L, d), "strict_f32"))
+    flat = ref.bf16_round((size * rng.standard_normal((H, L, 1))).astype(np.float32))
+    flat[:, :L // 3] = 0
+    c.put(1, 0, np.arange(L), np.broadcast_to(flat, (H, L, d)).astype(np.float32))
+    assert not c.group(1)[0].any()
+    Q = rows(rng, (1, 2, Lq, d), contract)
+    check_attention(gpu_lib, rng, c, dev(c.to_bytes()), Q, None, None, True, 0.2, contract, False)
+
+
+@pytest.mark.parametrize("contract,value", [("fast_bf16", 0.0), ("strict_f32", 3.0)])
+def test_the_longest_sequence(gpu_lib, contract, value):
+    """2^24 tokens of equal score: O is their value, LSE the logarithm of their
+    number, and each gathers 2^-24."""
+    import torch
+    mg = gpu_lib
+    say("kv4 attention over 2^24 tokens %s" % contract)
+    L, d, n = 1 << 24, 32, 1 << 22
+    dt = dtype_of(contract)
+    cache, w = mg.kv4_cache(1, 1, L, d), torch.zeros(1, 1, L, device="cuda")
+    V = torch.full((1, 1, n, d), value, dtype=dt, device="cuda")
+    for at in range(0, L, n):
+        mg.mg_kv4_append(V, V, cache, dev(np.array([at], np.int32)), L=L, contract=contract)
+    Q = torch.zeros(1, 2, 1, d, dtype=dt, device="cuda")
+    O, LSE = mg.attention_forward_kv4(Q, cache, H=1, L=L, causal=True, scale=1.0, weight=w,
+                                      contract=contract)
+    # equal addends, in partial sums of fewer than 2^18 of them: 2^-7 at the very worst
+    assert np.all(np.abs(host(O) - value) <= 2.0 ** -7 * value)
+    assert np.all(np.abs(host(LSE) - 24 * math.log(2)) <= 2.0 ** -7)
+    assert np.all(np.abs(host(w) * 2.0 ** 23 - 1) <= 2.0 ** -7)
+
+
 @pytest.mark.parametrize("contract", ["fast_bf16", "strict_f32"])
 @pytest.mark.parametrize("Lq,L", [(1, 100), (20, 100), (40, 100), (512, 32768)])
 def test_attention_not_a_number(gpu_lib, contract, Lq, L):
