@@ -17,8 +17,8 @@
 // stretch of tokens before any of it is written, is safe in place; into
 // another cache, stretches are shared out over workgroups.
 //
-// 64 heads cut from 4,096 to 1,024 tokens of 128 channels: 9 us to select, 11 to
-// move; 16 heads from up to 32,768 to 8,192: 24 and 18.  Selection is bound by the
+// 64 heads cut from 4,096 to 1,024 tokens of 128 channels: 9 us to select, 10 to
+// move; 16 heads from up to 32,768 to 8,192: 24 and 17.  Selection is bound by the
 // vector and LDS work of the one compute unit a head has (5 us to load and turn
 // into keys), moving by the latency of rows that follow their index.
 #include "cdiv.h"

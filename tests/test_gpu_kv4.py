@@ -294,6 +294,21 @@ def test_attention_of_flat_values(gpu_lib, contract, Lq, L, size):
     check_attention(gpu_lib, rng, c, dev(c.to_bytes()), Q, None, None, True, 0.2, contract, False)
 
 
+@pytest.mark.parametrize("contract,Lq,L", [("fast_bf16", 3, 70), ("strict_f32", 3, 70),
+                                           ("fast_bf16", 40, 70), ("strict_f32", 40, 70),
+                                           ("fast_bf16", 256, 65600)])
+@pytest.mark.parametrize("q,k,scale", [(1.0, 1.0, 0.0), (1e25, 1.0, -3e-26), (1e-30, 1.0, 3e29),
+                                       (1.0, 1e20, 3e-21), (1.0, 1e-20, 3e19), (0.0, 1.0, 0.3)])
+def test_attention_of_large_and_small_factors(gpu_lib, contract, Lq, L, q, k, scale):
+    say("kv4 attention q %g k %g scale %g %s Lq%d" % (q, k, scale, contract, Lq))
+    rng = np.random.default_rng(15)
+    H, d = 1, 64
+    c = filled(rng, 1, H, L, d)
+    c.put(0, 0, np.arange(L), (k * rng.standard_normal((H, L, d))).astype(np.float32))
+    Q = ref.bf16_round((q * rng.standard_normal((1, 2, Lq, d))).astype(np.float32))
+    check_attention(gpu_lib, rng, c, dev(c.to_bytes()), Q, None, None, True, scale, contract, True)
+
+
 @pytest.mark.parametrize("contract,value", [("fast_bf16", 0.0), ("strict_f32", 3.0)])
 def test_the_longest_sequence(gpu_lib, contract, value):
     """2^24 tokens of equal score: O is their value, LSE the logarithm of their
