@@ -13,11 +13,11 @@
 // (strict: code - 8, with min + 8 scale) with p scale rounded to f16 (half a step
 // 2^-11, where a bf16 result has 2^-8; strict: two parts, 2^-23) and the second
 // sum in f32 from the unrounded p.  f16 holds p scale because both
-// factors are taken relative to a running bound: p to 2^kSlack above 1, and the
-// scales to a power of two of the row's own, moved up (and the sums rescaled,
-// as for a new maximum) when a block has a larger one.  kRaise lifts the
-// products to the top of f16's range, so that values 2^-25 below the largest
-// keep all their bits.
+// factors are taken relative to a running bound of the row: p to 2^kRowSlack
+// above 1, and the scales to a power of two, moved up (and the sums rescaled, as
+// for a new maximum) when a block has a larger one that the row sees.  kRaise
+// lifts the products to the top of f16's range, so that products 2^-25 below the
+// largest keep all their bits (of the two strict parts: 2^-13).
 //
 // 16 rows are the least a matrix product takes, and enough: one pass over the
 // cache is what a decode step costs.  64 heads of up to 32,768 tokens of 128
@@ -83,6 +83,14 @@ struct Kv4Values {
     }
 };
 
+// The f32 bits of a V scale, or of what stands for its minimum if that is more; 0
+// for a token that is not finite, which moves nothing.  (Words order as the scales
+// in their upper halves do.)
+__device__ __forceinline__ uint32_t value_bound(uint32_t scale, uint32_t size) {
+    constexpr uint32_t kBelow = (uint32_t)-kExpMin << 23;
+    return scale < 0x7f800000u ? max(scale, max(size, kBelow) - kBelow) : 0u;
+}
+
 template <int NG>
 struct BlockGroups {   // a block's groups in LDS, token k's at k * NG
     float scale[2][32 * NG], base[2][32 * NG];   // of K, V
@@ -105,7 +113,7 @@ struct Kv4GroupWords {
             w[0] = (lane < 32 ? kp : vp)[32 * block + (lane & 31)];
         }
     }
-    // 0 for tokens at or behind n
+    // taken apart; 0 for tokens at or behind n
     template <int NP>
     __device__ __forceinline__ void put(BlockGroups<NG> &to, int block, int n, int lane) {
         const bool in = 32 * block + (NG == 2 ? lane >> 1 : lane & 31) < n;
@@ -117,9 +125,10 @@ struct Kv4GroupWords {
             base[64 * i + lane] = base_of<NP>(w[i]);
         }
     }
-    // the lane's V word, or 0
-    __device__ __forceinline__ uint32_t value(int lane) const {
-        return NG == 2 || lane >= 32 ? w[NG - 1] : 0u;
+    // the lane's V word as a bound of its token, or 0
+    __device__ __forceinline__ uint32_t bound(int lane) const {
+        const uint32_t v = NG == 2 || lane >= 32 ? w[NG - 1] : 0u;
+        return value_bound(v, (v & 0x7fffu) << 16);
     }
 };
 
@@ -169,8 +178,10 @@ void kv4_rows(RowsArgs a) {
     const int stop = min((end + 31) / 32, begin + a.chunk);
 
     float m = -INFINITY;               // running maximum (base 2) rounded up, of the row
-    int e = kExpMin;                   // V's scales are below 2^e, its minima below 2^(e + 80)
-    uint32_t most = 0;                 // ... as a bound on their group words
+    int e = kExpMin;                   // V's scales that the row sees are below 2^e, its
+                                       // minima (strict: bases) below 2^(e + 80)
+    uint32_t most = 0;                 // ... as a value_bound
+    float off = kRaise - kExpMin;      // of exponents: kRaise - e - m
     float l = 0.f;                     // sum of p 2^(kRaise - e)
     float low[NG];                     // sums of p base in the same units
     f32x4 o[NB];                       // O^T[16 b + 4g + r][row c], over kCodeUnit
@@ -196,9 +207,12 @@ void kv4_rows(RowsArgs a) {
                 vm[4 * i + k] = y[k];
             }
         }
-        if (32 * (block + 1) > all) {
-            // tokens out of sight: no score, and groups that add nothing (a token
-            // that is not finite must not reach rows that do not see it)
+        uint32_t top = words.bound(lane);
+        const bool partly = 32 * (block + 1) > all;
+        if (partly) {
+            // tokens out of sight: no score, and groups that add nothing and bound
+            // nothing (a token that is not finite, or far above the others, must not
+            // reach rows that do not see it)
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 if (32 * block + 8 * g + k >= limit) {
@@ -206,6 +220,14 @@ void kv4_rows(RowsArgs a) {
 #pragma unroll
                     for (int i = 0; i < NG; ++i) vs[k * NG + i] = vm[k * NG + i] = 0.f;
                 }
+            float scale = 0.f, base = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8 * NG; ++i) {
+                scale = fmaxf(scale, vs[i]);
+                base = fmaxf(base, fabsf(vm[i]));
+            }
+            top = value_bound(__float_as_uint(max_over_groups(scale)),
+                              __float_as_uint(max_over_groups(base)));
         }
         if (a.score != nullptr && in) {
             float *to = a.score + ((size_t)bh * rows + r) * a.Lp + 32 * block + 8 * g;
@@ -215,15 +237,12 @@ void kv4_rows(RowsArgs a) {
         float mx = max3_f32(max3_f32(s[0][0], s[0][1], s[0][2]),
                             max3_f32(s[0][3], s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]));
         mx = max_over_groups(mx) * factor;
-        // NaN scales (a token that is not finite) move nothing
-        const uint32_t mine = words.value(lane);
-        constexpr uint32_t kBelow = (uint32_t)-kExpMin << 23;
-        const uint32_t low_bound = max((mine & 0x7fffu) << 16, kBelow) - kBelow;
-        const uint32_t top = mine < 0x7f800000u ? max(mine, low_bound) : 0u;
+        // (blocks that rows see part of come last, so `most` is the same in all lanes
+        // up to the first of them)
         if (__any(mx > m + kRowSlack || top > most)) {
             const float m_new = fmaxf(m, ceilf(mx));
-            // finite words order as the scales in their upper halves do
-            const uint32_t high = __float_as_uint(max_of_wave(__uint_as_float(top)));
+            const uint32_t high =
+                partly ? top : __float_as_uint(max_of_wave(__uint_as_float(top)));
             const int e_new = max(e, min(kExpMax, (int)(high >> 23) - 126));
             const float alpha =
                 m_new == -INFINITY ? 1.f : ldexpf(exp2_fast(m - m_new), e - e_new);
@@ -235,8 +254,8 @@ void kv4_rows(RowsArgs a) {
             m = m_new;
             e = e_new;
             most = e == kExpMax ? 0xffffffffu : ((uint32_t)(e + 127) << 23) - 1;
+            off = (float)(kRaise - e) - (m == -INFINITY ? 0.f : m);
         }
-        const float off = (float)(kRaise - e) - (m == -INFINITY ? 0.f : m);
         float p[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {

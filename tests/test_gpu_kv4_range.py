@@ -1,0 +1,68 @@
+"""Attention over the 4-bit cache at the ends of its range: values far above
+the others behind what a row sees."""
+import numpy as np
+import pytest
+
+import kv4_ref as ref
+from gpu_util import say
+from test_gpu_kv4 import dev, dtype_of, filled, host, many_rows, rows
+
+pytestmark = pytest.mark.gpu
+
+# kv4_many holds values in units of up to 2^12 of what a row itself sees, beside
+# the 2^-34 of them that the reference's bound has for those units
+MANY_UNITS = 2.0 ** (12 - 34)
+
+
+def check_rows_before(c, Q, O, LSE, n, cuts, causal_scale, strict):
+    """Rows between the tokens `cuts`, which are out of the ordinary, against the
+    reference over the tokens that they can see: a token that a row does not see
+    must not widen its bound."""
+    B, Hq, Lq, d = Q.shape
+    H = c.dims[1]
+    many = not strict and many_rows(B * H, Hq // H * Lq, c.dims[2])
+    O, LSE = host(O).astype(np.float64), host(LSE).astype(np.float64)
+    done = 0
+    for cut in list(cuts) + [n]:
+        m = cut - (n - Lq)      # rows that do not see token `cut`
+        for hq in range(Hq):
+            h = hq // (Hq // H)
+            rO, rL, _, tO, tL, _ = ref.attention(
+                Q[0, hq, :m].astype(np.float64), [x[0, h] for x in c.code],
+                [tuple(p[0, h] for p in c.group(i)) for i in range(2)], cut, m, True,
+                causal_scale, strict, many)
+            if many:
+                tO = tO + MANY_UNITS * np.abs(c.rows(1)[0, h, :cut]).max()
+            off = np.abs(O[0, hq, done:m] - rO[done:])
+            assert np.all(off <= tO[done:]), (cut, hq, (off / tO[done:]).max())
+            assert np.all(np.abs(LSE[0, hq, done:m] - rL[done:]) <= tL[done:]), (cut, hq)
+        done = m
+
+
+def run(mg, c, Q, n, scale, contract):
+    return mg.attention_forward_kv4(dev(Q, dtype_of(contract)), dev(c.to_bytes()), H=c.dims[1],
+                                    L=c.dims[2], causal=True, scale=scale,
+                                    key_len=dev(np.array([n], np.int32)), contract=contract)
+
+
+@pytest.mark.parametrize("contract", ["fast_bf16", "strict_f32"])
+@pytest.mark.parametrize("grow", [20, 60])
+@pytest.mark.parametrize("Hq,H,Lq,L,d,cuts", [
+    (2, 1, 5, 70, 64, [68]),                  # the last of few rows sees it alone
+    (4, 2, 7, 400, 128, [394, 398]),          # two, one above the other
+    (3, 1, 50, 333, 32, [300, 301, 331]),
+    (1, 1, 40, 40, 64, [1, 17, 39]),          # the first row sees one token
+    (2, 2, 3, 5000, 128, [4998])])            # split over workgroups
+def test_values_that_rows_do_not_see(gpu_lib, contract, grow, Hq, H, Lq, L, d, cuts):
+    """Tokens whose V is 2^20 or 2^60 times the others (and the next one that
+    again) must not cost the rows before them anything."""
+    say("kv4 attention, unseen values 2^%d, %s Hq%d Lq%d L%d d%d" % (grow, contract, Hq, Lq, L, d))
+    rng = np.random.default_rng(grow + L + d)
+    c = filled(rng, 1, H, L, d)
+    for k, cut in enumerate(cuts):
+        big = rows(rng, (H, 1, d), "strict_f32") * 2.0 ** (grow * (k + 1) / len(cuts))
+        c.put(1, 0, np.array([cut]), big.astype(np.float32))
+    n = L - 1 if L - 1 not in cuts else L
+    Q = rows(rng, (1, Hq, Lq, d), contract)
+    O, LSE = run(gpu_lib, c, Q, n, 0.1, contract)
+    check_rows_before(c, Q, O, LSE, n, cuts, 0.1, contract != "fast_bf16")
