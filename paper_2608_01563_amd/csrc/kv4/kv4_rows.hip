@@ -244,9 +244,9 @@ void kv4_rows(RowsArgs a) {
             const uint32_t high =
                 partly ? top : __float_as_uint(max_of_wave(__uint_as_float(top)));
             const int e_new = max(e, min(kExpMax, (int)(high >> 23) - 126));
-            const float alpha =
-                m_new == -INFINITY ? 1.f : ldexpf(exp2_fast(m - m_new), e - e_new);
-            l *= alpha;
+            const float lower = m_new == -INFINITY ? 1.f : exp2_fast(m - m_new);
+            l = ldexpf(l * lower, e - e_new);   // (where the factor alone would be 0)
+            const float alpha = ldexpf(lower, e - e_new);
 #pragma unroll
             for (int i = 0; i < NG; ++i) low[i] *= alpha;
 #pragma unroll

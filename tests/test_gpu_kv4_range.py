@@ -5,7 +5,7 @@ import pytest
 
 import kv4_ref as ref
 from gpu_util import say
-from test_gpu_kv4 import dev, dtype_of, filled, host, many_rows, rows
+from test_gpu_kv4 import check_attention, dev, dtype_of, filled, host, many_rows, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -66,3 +66,19 @@ def test_values_that_rows_do_not_see(gpu_lib, contract, grow, Hq, H, Lq, L, d, c
     Q = rows(rng, (1, Hq, Lq, d), contract)
     O, LSE = run(gpu_lib, c, Q, n, 0.1, contract)
     check_rows_before(c, Q, O, LSE, n, cuts, 0.1, contract != "fast_bf16")
+
+
+@pytest.mark.parametrize("contract", ["fast_bf16", "strict_f32"])
+@pytest.mark.parametrize("first,at", [(-70, 650), (-70, 400), (-30, 130), (0, 699)])
+def test_a_leap_of_values(gpu_lib, contract, first, at):
+    """One V 2^150 (or as far as values may go) above those before it must leave LSE,
+    which V has no part in, and the probabilities as they are."""
+    say("kv4 attention, a leap of values at %d from 2^%d, %s" % (at, first, contract))
+    rng = np.random.default_rng(at)
+    H, L, d = 2, 700, 64
+    c = filled(rng, 1, H, L, d)
+    x = (rows(rng, (H, L, d), "strict_f32") * 2.0 ** first).astype(np.float32)
+    x[:, at] = rows(rng, (H, d), "strict_f32") * np.float32(2.0 ** min(80, first + 150))
+    c.put(1, 0, np.arange(L), x)
+    Q = rows(rng, (1, 4, 2, d), contract)
+    check_attention(gpu_lib, rng, c, dev(c.to_bytes()), Q, None, None, False, 0.1, contract, True)
