@@ -7,7 +7,10 @@
 //   K   codes as f16, exact; scores are scaled and shifted a group at a time as
 //       in kv4_tile.h, the minima's part by one f32 product over the groups
 //   V   values v 2^(15-E) rounded to f16 (within 2^-11), E bounding all values
-//       so far, so that one product per 16 tokens covers scale and minimum
+//       so far, so that one product per 16 tokens covers scale and minimum;
+//       rows that see a tile in part, and of its values only some that are
+//       2^kFar below its E, are computed anew in kv4_sweep.h's form, whose
+//       bounds are a row's own
 //   P   f16, at most 2^15
 //
 // The row order of the score product swaps bits 2 and 3 of the token, which
@@ -24,7 +27,7 @@
 // products, because they read half as much of LDS for their work as 16x16 ones.
 #include "cdiv.h"
 #include "kv4_launch.h"
-#include "kv4_tile.h"
+#include "kv4_sweep.h"
 
 namespace mg {
 namespace {
@@ -33,6 +36,10 @@ constexpr int kTokens = 64, kManyWaves = 8, kRows = 32 * kManyWaves;
 constexpr float kManySlack = 4.f;
 constexpr int kLift = 11;      // P is at most 2^(slack + kLift) = 2^15
 constexpr int kManyExp = -100; // least E
+constexpr int kFar = 12;       // V's f16 parts are then off by 2^-22 of the largest at most
+constexpr int kNone = -1000;   // exponent of nothing but zeros
+constexpr int kLeap = 60;      // E may move by this in one tile before f32 sums lose bits
+constexpr int kFarTiles = 8;   // tiles in or just before which 128 rows can end, twice
 
 struct ManyArgs {
     const uint16_t *Q;
@@ -90,6 +97,60 @@ struct Query32 {
     }
 };
 
+// Rows first .. first + 15 of a head over blocks begin .. stop - 1 of 32 tokens, in the
+// form of few rows, by one wave.
+template <int D>
+__device__ __forceinline__ void anew(const ManyArgs &a, int bh, int split, int first, int begin,
+                                     int stop, const Kv4Mask &mask,
+                                     BlockGroups<Kv4Dim<D>::kGroups> &groups, int lane) {
+    constexpr int NG = Kv4Dim<D>::kGroups, NB = Kv4Dim<D>::kBlocks;
+    const int c = lane & 15, g = lane >> 4, rows = a.G * a.Lq;
+    const int r = first + c;
+    const bool in = r < rows;
+    const RowAt at = row_at(in ? r : rows - 1, bh, a.G, a.Lq);
+    const size_t head = (size_t)bh * a.Lp;
+    Kv4Query<D, 1> q;
+    q.load(a.Q + at.at * D, in, g, a.scale_log2 < 0.f);
+    const float factor = positive_factor(a.scale_log2, q.exponent);
+    const int limit = mask.limit(at.i), all = mask.limit(first / a.G);
+    Kv4Sweep<D, 1> sweep;
+#pragma unroll 1
+    for (int block = begin; block < stop; ++block) {
+        Kv4Keys<D> key;
+        Kv4Values<D> val;
+        Kv4GroupWords<NG> words;
+        key.load(a.kw + head * (D / 8), block, c, g);
+        val.load(a.vw + head / 8 * D, block, c, g);
+        words.load(a.kp + head * NG, a.vp + head * NG, block, lane);
+        sweep.step(block, q, factor, limit, all, mask.n, key, val, words, groups, lane,
+                   [](const f32x4(&)[2]) {});
+    }
+    sweep.finish();
+    if (!in) return;
+    const bool valid = at.i < mask.rows;
+    if (a.splits > 1) {
+        const size_t slot = ((size_t)bh * a.splits + split) * rows + r;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+            *reinterpret_cast<f32x4 *>(a.part + slot * D + 16 * b + 4 * g) =
+                valid ? sweep.o[b] : zero4();
+        if (g == 0) {
+            a.stat[2 * slot] = valid ? sweep.m : -INFINITY;
+            a.stat[2 * slot + 1] = valid ? sweep.l : 0.f;
+        }
+        return;
+    }
+    const float l = valid ? sweep.l : 0.f, inv = 1.f / l;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        float x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = l == 0.f ? 0.f : sweep.o[b][k] * inv;
+        store_row(a.O + at.at * D + 16 * b + 4 * g, x);
+    }
+    if (g == 0) a.LSE[at.at] = l != l ? l : row_lse(sweep.m, l);
+}
+
 template <int D>
 __global__ __launch_bounds__(64 * kManyWaves) __attribute__((amdgpu_waves_per_eu(2, 8)))
 void kv4_many(ManyArgs a) {
@@ -103,6 +164,7 @@ void kv4_many(ManyArgs a) {
     __shared__ __attribute__((aligned(16))) _Float16 Vsc[4][NG][kTokens], Vmn[4][NG][kTokens];
     __shared__ uint64_t Bad[4][NG];   // tokens whose V is not finite
     __shared__ int Es[4];
+    __shared__ int FarCount, Far[kFarTiles][2];   // rows with limits in (first, second]
 
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -127,7 +189,8 @@ void kv4_many(ManyArgs a) {
         return from < rows && from / a.G < mask.rows
             ? max(mask.limit(min((min(rows, from + n) - 1) / a.G, mask.rows - 1)), 0) : 0;
     };
-    const int end = max(end_of(front, kRows / 2), end_of(back, kRows / 2));
+    const int front_end = end_of(front, kRows / 2), back_end = end_of(back, kRows / 2);
+    const int end = max(front_end, back_end);
     const int wave_end = end_of(r0, 32);
     const int wave_all = r0 < rows ? mask.limit(r0 / a.G) : 0;
 
@@ -160,7 +223,13 @@ void kv4_many(ManyArgs a) {
         for (int g = 0; g < NG; ++g)
             params[g] = w < 2 && k < mask.n ? p[(size_t)k * NG + g] : 0u;
     };
-    int bound = kManyExp;   // E, in wave 1
+    // in wave 1: E, the same of what was not 0, and how many Far tiles there are
+    int bound = kManyExp, known = kNone, far_tiles = 0;
+    // whether [from, to] holds the limit of a row of the workgroup
+    auto limits_in = [&](int from, int to) {
+        return (front < rows && max(mask.limit(front / a.G), from) <= min(front_end, to)) ||
+               (back < rows && max(mask.limit(back / a.G), from) <= min(back_end, to));
+    };
     auto put_params = [&](int t) {
         const int b = t & 3;
         if (w == 0) {
@@ -171,20 +240,43 @@ void kv4_many(ManyArgs a) {
             }
             if (NG == 1) Kmn[b][1][lane] = 0.f;
         } else if (w == 1) {
-            float most = 0.f;
+            float size = 0.f;
             bool good[NG];
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
                 const float sc = group_scale(params[g]), mn = group_min(params[g]);
                 const float v = fmaxf(fabsf(mn), fabsf(fmaf(15.f, sc, mn)));
                 good[g] = v < INFINITY;
-                most = fmaxf(most, good[g] ? v : 0.f);
+                size = fmaxf(size, good[g] ? v : 0.f);
                 const uint64_t bad = __ballot(!good[g]);
                 if (lane == 0) Bad[b][g] = bad;
             }
-            most = max_of_wave(most);
-            if (most > 0.f) bound = max(bound, __builtin_amdgcn_frexp_expf(most));
+            const float most = max_of_wave(size);
+            const int moved = __builtin_amdgcn_readfirstlane(
+                most > 0.f ? max(bound, __builtin_amdgcn_frexp_expf(most)) : kNone);
+            bound = max(bound, moved);
             if (lane == 0) Es[b] = bound;
+            if (bound > known + kFar) {
+                // Rows that see nothing of the tile from its first value near E on, if they
+                // see a value other than 0; after a leap also what a wave that works on
+                // the tile has of rows that end before it.
+                const int at = kTokens * t;
+                const bool some = known != kNone, leap = some && bound > known + kLeap;
+                const int own = max(__builtin_amdgcn_frexp_expf(size), kManyExp);
+                const int from = leap ? at - 32 : at;
+                const int near = __builtin_ctzll(__ballot(size > 0.f && own + kFar >= bound) |
+                                                 1ull << 63);
+                const bool seen = some || (__ballot(size > 0.f) & ((1ull << near) - 1)) != 0;
+                if (seen && t < stop && limits_in(from + 1, at + near) && far_tiles < kFarTiles) {
+                    if (lane == 0) {
+                        Far[far_tiles][0] = from;
+                        Far[far_tiles][1] = at + near;
+                        FarCount = far_tiles + 1;
+                    }
+                    ++far_tiles;
+                }
+            }
+            known = moved != kNone ? bound : known;
             // in the octet's slot order
             const int slot = (lane & 0x38) | (lane & 1) << 2 | (lane & 6) >> 1;
 #pragma unroll
@@ -362,6 +454,7 @@ void kv4_many(ManyArgs a) {
     };
 
     if (begin < stop) {
+        if (tid == 64) FarCount = 0;
         load_params(begin);
         load_words(begin);
         put_params(begin);
@@ -408,9 +501,23 @@ void kv4_many(ManyArgs a) {
         }
     }
 
+    const bool valid = i < mask.rows;
+    if (begin < stop && FarCount > 0) {
+        __syncthreads();   // Ks is free
+        bool far = false;
+        for (int k = 0; k < FarCount; ++k) far |= limit > Far[k][0] && limit <= Far[k][1];
+        const uint32_t which = (uint32_t)__ballot(in && valid && far);   // lanes l and l + 32 agree
+        auto &groups = reinterpret_cast<BlockGroups<NG> *>(&Ks[0][0])[w];
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half)
+            if (which >> (16 * half) & 0xffffu)
+                anew<D>(a, bh, split, r0 + 16 * half, 2 * begin,
+                        min(2 * stop, (end_of(r0 + 16 * half, 16) + 31) / 32), mask, groups, lane);
+        if (which >> (c & 16) & 0xffffu) return;
+    }
+
     l = sum_xor32(l);
     if (!in) return;
-    const bool valid = i < mask.rows;
     if (a.splits > 1) {
         const size_t slot = ((size_t)bh * a.splits + split) * rows + r;
         float *to = a.part + slot * D;

@@ -14,7 +14,7 @@ pytestmark = pytest.mark.gpu
 MANY_UNITS = 2.0 ** (12 - 34)
 
 
-def check_rows_before(c, Q, O, LSE, n, cuts, causal_scale, strict):
+def check_rows_before(c, Q, O, LSE, n, cuts, causal_scale, strict, heads=None):
     """Rows between the tokens `cuts`, which are out of the ordinary, against the
     reference over the tokens that they can see: a token that a row does not see
     must not widen its bound."""
@@ -25,7 +25,7 @@ def check_rows_before(c, Q, O, LSE, n, cuts, causal_scale, strict):
     done = 0
     for cut in list(cuts) + [n]:
         m = cut - (n - Lq)      # rows that do not see token `cut`
-        for hq in range(Hq):
+        for hq in heads or range(Hq):
             h = hq // (Hq // H)
             rO, rL, _, tO, tL, _ = ref.attention(
                 Q[0, hq, :m].astype(np.float64), [x[0, h] for x in c.code],
@@ -82,3 +82,56 @@ def test_a_leap_of_values(gpu_lib, contract, first, at):
     c.put(1, 0, np.arange(L), x)
     Q = rows(rng, (1, 4, 2, d), contract)
     check_attention(gpu_lib, rng, c, dev(c.to_bytes()), Q, None, None, False, 0.1, contract, True)
+
+
+@pytest.mark.parametrize("grow", [11, 30, 100])
+@pytest.mark.parametrize("Hq,H,Lq,L,d,cuts", [
+    (32, 32, 1024, 1030, 64, [10, 70, 500, 503, 900, 1025]),
+    (8, 4, 2200, 2200, 128, [1, 2, 64, 1000, 1001, 2100]),   # the first rows see little
+    (1, 1, 256, 131072, 32, [130817, 130900, 131071])])      # split over workgroups
+def test_values_that_many_rows_do_not_see(gpu_lib, grow, Hq, H, Lq, L, d, cuts):
+    """The same where a tile of values is shared by rows that see it in part."""
+    say("kv4 attention of many rows, unseen values 2^%d, Hq%d Lq%d L%d d%d" % (grow, Hq, Lq, L, d))
+    assert many_rows(H, Hq // H * Lq, L)
+    rng = np.random.default_rng(grow + L + d)
+    c = filled(rng, 1, H, L, d)
+    for k, cut in enumerate(cuts):
+        big = rows(rng, (H, 1, d), "strict_f32") * 2.0 ** (grow * (k + 1) / len(cuts))
+        c.put(1, 0, np.array([cut]), big.astype(np.float32))
+    Q = rows(rng, (1, Hq, Lq, d), "fast_bf16")
+    O, LSE = run(gpu_lib, c, Q, L, 0.1, "fast_bf16")
+    check_rows_before(c, Q, O, LSE, L, cuts, 0.1, False, sorted({0, Hq - 1}))
+
+
+def test_many_rows_before_values_and_zeros(gpu_lib):
+    """Rows that see nothing but V = 0 get 0, and rows whose values are tiny theirs,
+    whatever comes behind them."""
+    say("kv4 attention of many rows, zeros and tiny values first")
+    rng = np.random.default_rng(21)
+    H, L, d = 32, 1024, 32
+    c = filled(rng, 1, H, L, d)
+    x = rows(rng, (H, L, d), "strict_f32")
+    x[:, :5] = 0
+    x[:, 5:30] *= 2.0 ** -60
+    c.put(1, 0, np.arange(L), x)
+    Q = rows(rng, (1, H, L, d), "fast_bf16")
+    O, LSE = run(gpu_lib, c, Q, L, 0.1, "fast_bf16")
+    assert not host(O)[0, :, :5].any()
+    check_rows_before(c, Q, O, LSE, L, [30], 0.1, False, [0, H - 1])
+
+
+@pytest.mark.parametrize("cut", [640, 645, 703])
+def test_many_rows_before_a_leap(gpu_lib, cut):
+    """Values of 2^-70, then one of 2^80, at the start of a tile, within one and at its
+    end, where some rows of a wave see the tile and others end before it."""
+    say("kv4 attention of many rows before a leap at %d" % cut)
+    rng = np.random.default_rng(cut)
+    H, Lq, L, d = 32, 1024, 1030, 64
+    c = filled(rng, 1, H, L, d)
+    x = rows(rng, (H, L, d), "strict_f32") * np.float32(2.0 ** -70)
+    for _ in range(2):   # (2^150 is no f32)
+        x[:, cut] *= np.float32(2.0 ** 75)
+    c.put(1, 0, np.arange(L), x)
+    Q = rows(rng, (1, H, Lq, d), "fast_bf16")
+    O, LSE = run(gpu_lib, c, Q, L, 0.1, "fast_bf16")
+    check_rows_before(c, Q, O, LSE, L, [cut], 0.1, False, [0, H - 1])
