@@ -58,7 +58,7 @@ template <int D>
 struct Query32 {
     f16x8 q[D / 16];
     float sum;      // of group l/32 (0 where there is no second)
-    int exponent;
+    int exponent, size;   // as in Kv4Query
 
     __device__ __forceinline__ void load(const uint16_t *row, bool valid, int h, bool negate) {
         constexpr int NS = D / 16, NG = Kv4Dim<D>::kGroups;
@@ -74,7 +74,7 @@ struct Query32 {
                 top = fmaxf(top, fabsf(x[s][e]));
                 if (negate) x[s][e] = -x[s][e];
             }
-        exponent = __builtin_amdgcn_frexp_expf(max_xor32(top));
+        exponent = query_exponent(max_xor32(top), &size);
         float each[2] = {0.f, 0.f};
 #pragma unroll
         for (int gr = 0; gr < NG; ++gr) {
@@ -111,7 +111,7 @@ __device__ __forceinline__ void anew(const ManyArgs &a, int bh, int split, int f
     const size_t head = (size_t)bh * a.Lp;
     Kv4Query<D, 1> q;
     q.load(a.Q + at.at * D, in, g, a.scale_log2 < 0.f);
-    const float factor = positive_factor(a.scale_log2, q.exponent);
+    const auto factors = Kv4Sweep<D, 1>::factors(q, a.scale_log2, lane);
     const int limit = mask.limit(at.i), all = mask.limit(first / a.G);
     Kv4Sweep<D, 1> sweep;
 #pragma unroll 1
@@ -122,7 +122,7 @@ __device__ __forceinline__ void anew(const ManyArgs &a, int bh, int split, int f
         key.load(a.kw + head * (D / 8), block, c, g);
         val.load(a.vw + head / 8 * D, block, c, g);
         words.load(a.kp + head * NG, a.vp + head * NG, block, lane);
-        sweep.step(block, q, factor, limit, all, mask.n, key, val, words, groups, lane,
+        sweep.step(block, q, factors, limit, all, mask.n, key, val, words, groups, lane,
                    [](const f32x4(&)[2]) {});
     }
     sweep.finish();
@@ -163,7 +163,7 @@ void kv4_many(ManyArgs a) {
     __shared__ float Kmn[4][2][kTokens];
     __shared__ __attribute__((aligned(16))) _Float16 Vsc[4][NG][kTokens], Vmn[4][NG][kTokens];
     __shared__ uint64_t Bad[4][NG];   // tokens whose V is not finite
-    __shared__ int Es[4];
+    __shared__ int Es[4], Sizes[kManyWaves];
     __shared__ int FarCount, Far[kFarTiles][2];   // rows with limits in (first, second]
 
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h = lane >> 5;
@@ -223,6 +223,7 @@ void kv4_many(ManyArgs a) {
         for (int g = 0; g < NG; ++g)
             params[g] = w < 2 && k < mask.n ? p[(size_t)k * NG + g] : 0u;
     };
+    float unit = 1.f;   // of K's groups, in wave 0
     // in wave 1: E, the same of what was not 0, and how many Far tiles there are
     int bound = kManyExp, known = kNone, far_tiles = 0;
     // whether [from, to] holds the limit of a row of the workgroup
@@ -235,8 +236,8 @@ void kv4_many(ManyArgs a) {
         if (w == 0) {
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                Ksc[b][g][lane] = group_scale(params[g]);
-                Kmn[b][g][lane] = group_min(params[g]);
+                Ksc[b][g][lane] = group_scale(params[g]) * unit;
+                Kmn[b][g][lane] = group_min(params[g]) * unit;
             }
             if (NG == 1) Kmn[b][1][lane] = 0.f;
         } else if (w == 1) {
@@ -312,7 +313,7 @@ void kv4_many(ManyArgs a) {
 
     Query32<D> q;
     q.load(a.Q + at * D, in, h, a.scale_log2 < 0.f);
-    const float factor = positive_factor(a.scale_log2, q.exponent);
+    float factor = 0.f;
     float m = -INFINITY, l = 0.f;
     int E = kManyExp;
     f32x16 o[NB];   // O^T[32 b + 8 (v/4) + 4h + v%4][row c] 2^(kLift + 15 - E)
@@ -457,9 +458,25 @@ void kv4_many(ManyArgs a) {
         if (tid == 64) FarCount = 0;
         load_params(begin);
         load_words(begin);
+        const float wave_size = max_of<16>(max_xor16((float)q.size));
+        if (lane == 0) Sizes[w] = (int)wave_size;
         put_params(begin);
         load_params(begin + 1);
         __syncthreads();
+        // one unit of K for the workgroup's rows (the first tile's groups are there)
+        int size = Sizes[0];
+#pragma unroll
+        for (int k = 1; k < kManyWaves; ++k) size = max(size, Sizes[k]);
+        const int exponent = __builtin_amdgcn_readfirstlane(key_unit(a.scale_log2, size));
+        factor = positive_factor(a.scale_log2, q.exponent, exponent);
+        unit = power_of_two(exponent);
+        if (w == 0) {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                Ksc[begin & 3][g][lane] *= unit;
+                Kmn[begin & 3][g][lane] *= unit;
+            }
+        }
         put_words(begin, 0);
         put_params(begin + 1);
         load_words(begin + 1);

@@ -74,7 +74,7 @@ void kv4_rows(RowsArgs a) {
     const RowAt at = row_at(in ? r : rows - 1, bh, a.G, a.Lq);
     Kv4Query<D, NP> q;
     q.load(static_cast<const T *>(a.Q) + at.at * D, in, g, a.scale_log2 < 0.f);
-    const float factor = positive_factor(a.scale_log2, q.exponent);
+    const auto factors = Kv4Sweep<D, NP>::factors(q, a.scale_log2, lane);
 
     // the tokens that the tile's last and its first row see
     if (32 * begin >= mask.n && begin > 0) return;   // kv4_join knows
@@ -88,12 +88,12 @@ void kv4_rows(RowsArgs a) {
     Kv4Sweep<D, NP> sweep;
     auto step = [&](int block, const Kv4Keys<D> &key, const Kv4Values<D> &val,
                     Kv4GroupWords<NG> &words, BlockGroups<NG> &groups) {
-        sweep.step(block, q, factor, limit, all, mask.n, key, val, words, groups, lane,
+        sweep.step(block, q, factors, limit, all, mask.n, key, val, words, groups, lane,
                    [&](const f32x4(&s)[2]) {
             if (a.score == nullptr || !in) return;
             float *to = a.score + ((size_t)bh * rows + r) * a.Lp + 32 * block + 8 * g;
-            *reinterpret_cast<f32x4 *>(to) = s[0] * factor;
-            *reinterpret_cast<f32x4 *>(to + 4) = s[1] * factor;
+            *reinterpret_cast<f32x4 *>(to) = s[0] * factors.factor;
+            *reinterpret_cast<f32x4 *>(to + 4) = s[1] * factors.factor;
         });
     };
 

@@ -84,16 +84,19 @@ struct Kv4GroupWords {
             w[0] = (lane < 32 ? kp : vp)[32 * block + (lane & 31)];
         }
     }
-    // taken apart; 0 for tokens at or behind n
+    // taken apart, K's times `unit` (a power of two; in lanes that hold V's alone 1);
+    // 0 for tokens at or behind n
     template <int NP>
-    __device__ __forceinline__ void put(BlockGroups<NG> &to, int block, int n, int lane) {
+    __device__ __forceinline__ void put(BlockGroups<NG> &to, int block, int n, float unit,
+                                        int lane) {
         const bool in = 32 * block + (NG == 2 ? lane >> 1 : lane & 31) < n;
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
             w[i] = in ? w[i] : 0u;
             float *scale = &to.scale[0][0], *base = &to.base[0][0];
-            scale[64 * i + lane] = group_scale(w[i]);
-            base[64 * i + lane] = base_of<NP>(w[i]);
+            const float times = i == 0 ? unit : 1.f;
+            scale[64 * i + lane] = group_scale(w[i]) * times;
+            base[64 * i + lane] = base_of<NP>(w[i]) * times;
         }
     }
     // the lane's V word as a bound of its token, or 0
@@ -125,16 +128,29 @@ struct Kv4Sweep {
         for (int i = 0; i < NB; ++i) o[i] = zero4();
     }
 
+    // The row's products are scores times 1 / factor where K's groups are taken times unit.
+    struct Factors {
+        float factor, unit;
+    };
+    static __device__ __forceinline__ Factors factors(const Kv4Query<D, NP> &q, float scale_log2,
+                                                      int lane) {
+        // (a size is a whole number that f32 holds)
+        const int unit = __builtin_amdgcn_readfirstlane(
+            key_unit(scale_log2, (int)max_of<16>((float)q.size)));
+        return {positive_factor(scale_log2, q.exponent, unit),
+                NG == 2 || lane < 32 ? power_of_two(unit) : 1.f};
+    }
+
     // One block, later ones later.  The row sees tokens below `limit`, every row of the
-    // wave those below `all`; `n`: the sequence's tokens; `factor`: of the row's scores,
-    // which `keep` gets first.
+    // wave those below `all`; `n`: the sequence's tokens; `keep` gets the scores first.
     template <typename Keep>
-    __device__ __forceinline__ void step(int block, const Kv4Query<D, NP> &q, float factor,
+    __device__ __forceinline__ void step(int block, const Kv4Query<D, NP> &q, Factors f,
                                          int limit, int all, int n, const Kv4Keys<D> &key,
                                          const Kv4Values<D> &val, Kv4GroupWords<NG> &words,
                                          BlockGroups<NG> &groups, int lane, Keep &&keep) {
         const int c = lane & 15, g = lane >> 4;
-        words.template put<NP>(groups, block, n, lane);
+        const float factor = f.factor;
+        words.template put<NP>(groups, block, n, f.unit, lane);
         __builtin_amdgcn_wave_barrier();   // one wave's LDS accesses stay in order
         f32x4 s[2];
         key.scores(s, q, groups.scale[0], groups.base[0], c, g);

@@ -74,6 +74,14 @@ __device__ __forceinline__ void split_operand(f16x8 (&out)[NP], const float (&x)
     }
 }
 
+// Exponent of a row's largest value; 0 for zero, infinity and NaN, which have no size.
+constexpr int kNoSize = -1000;
+__device__ __forceinline__ int query_exponent(float top, int *size) {
+    const int e = __builtin_amdgcn_frexp_expf(top);
+    *size = top > 0.f && top < INFINITY ? e : kNoSize;
+    return e;
+}
+
 // A query row as operands: q[p][s] holds channels 32s + 8g + e of part p, times
 // 2^(15 - exponent of the row's largest value); sum is one group's sum in the
 // units of a product with codes.
@@ -82,6 +90,7 @@ struct Kv4Query {
     f16x8 q[NP][D / 32];
     float sum;      // of group g (0 where there is none)
     int exponent;   // scores = products * 2^(exponent - 6)
+    int size;       // the same, kNoSize for a row of zeros or not finite
 
     template <typename T>
     __device__ __forceinline__ void load(const T *row, bool valid, int g, bool negate) {
@@ -99,8 +108,7 @@ struct Kv4Query {
                 if (negate) x[s][e] = -x[s][e];
             }
         top = max_over_groups(top);
-        // 0 for zero, infinity and NaN
-        exponent = __builtin_amdgcn_frexp_expf(top);
+        exponent = query_exponent(top, &size);
         sum = 0.f;
 #pragma unroll
         for (int gr = 0; gr < NG; ++gr) {
@@ -184,15 +192,26 @@ struct Kv4Keys {
     }
 };
 
-// A scale times log2 e and the row's power of two.
-__device__ __forceinline__ float row_factor(float scale_log2, int exponent) {
-    return ldexpf(scale_log2, exponent - 6);
+// K's scales and minima enter scores times 2^key_unit, so that a product with codes is in
+// range whenever the score is, and too small only where the score is nothing: the
+// factor of the largest of the rows that share them (its size; kNoSize if none has one).
+__device__ __forceinline__ int key_unit(float scale_log2, int size) {
+    return scale_log2 == 0.f ? -126
+         : min(max(__builtin_amdgcn_frexp_expf(scale_log2) + size - 6, -126), 126);
 }
 
-// The same for a row whose negative scale went into Q, at least the smallest
-// normal: -inf times it stays -inf where the scale is 0.
-__device__ __forceinline__ float positive_factor(float scale_log2, int exponent) {
-    return fmaxf(row_factor(fabsf(scale_log2), exponent), 0x1p-126f);
+// 2^e of a normal number (in scalar registers where e is).
+__device__ __forceinline__ float power_of_two(int e) {
+    return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+// What a row's products, in units of 2^unit, are multiplied with: the scale times log2 e
+// (its sign went into Q) and the row's power of two; at least the smallest normal (-inf
+// times it stays -inf where the scale is 0, and only nothing is less) and finite (a
+// row of zeros).
+__device__ __forceinline__ float positive_factor(float scale_log2, int exponent, int unit) {
+    const float f = ldexpf(fabsf(scale_log2), max(min(exponent - 6 - unit, 1000), -1000));
+    return fminf(fmaxf(f, 0x1p-126f), 0x1p126f);
 }
 
 // One sequence's lengths and mask: row i sees tokens below limit(i).

@@ -41,8 +41,8 @@ void kv4_weights(WeightArgs a) {
     constexpr int NG = Kv4Dim<D>::kGroups, NS = D / 16, KR = D / 8;
     constexpr int PER = KR;   // threads that prepare a row, 8 channels each
     __shared__ __attribute__((aligned(16))) f16x8 Qs[2][NP][32 * (KR + 1)];
-    __shared__ float Sum[2][2][32], Factor[2][32], Lse[2][32];
-    __shared__ int Limit[2][32];
+    __shared__ float Sum[2][2][32], Lse[2][32];
+    __shared__ int Exponent[2][32], Limit[2][32];
     __shared__ __attribute__((aligned(16))) float Scale[kWaves][NG][32];
 
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h = lane >> 5;
@@ -74,8 +74,15 @@ void kv4_weights(WeightArgs a) {
 #pragma unroll
     for (int s = 0; s < NS; ++s)   // channels 16s + 8h + e: word 2s + h of the row
         code[s] = code_operand(kw[tok * KR + k_word<D>(2 * s + h)]);
-    if (h < NG) Scale[w][h][c] = group_scale(kp[c * NG + h]);   // read by the wave itself
-    const float low = NG == 2 || h == 0 ? group_min(kp[tok * NG + (NG == 2 ? h : 0)]) : 0.f;
+    // Scales and minima are taken over 2^size, the largest of the wave's tokens (those
+    // that are there and finite), and factors times it, so that products stay in range.
+    const uint32_t own = kp[c * NG + (NG == 2 ? h : 0)];
+    const float most = fmaxf(0x1p-4f * fabsf(group_min(own)), group_scale(own));
+    const int size = 4 + __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(
+        max_of_wave(base + c < mask.n && most < INFINITY ? most : 0.f)));
+    if (h < NG) Scale[w][h][c] = ldexpf(group_scale(own), -size);   // read by the wave itself
+    const float low =
+        NG == 2 || h == 0 ? ldexpf(group_min(kp[tok * NG + (NG == 2 ? h : 0)]), -size) : 0.f;
 
     // preparing rows: thread r * PER + k takes channels 8k..8k+7 of row r
     const int pr = tid / PER, pk = tid % PER;
@@ -120,7 +127,7 @@ void kv4_weights(WeightArgs a) {
         if (pk % (PER / NG) == 0) Sum[buf][pk / (PER / NG)][pr] = sum * 0x1p-9f;
         if (pk == 0) {
             if (NG == 1) Sum[buf][1][pr] = 0.f;
-            Factor[buf][pr] = row_factor(a.scale_log2, exponent);
+            Exponent[buf][pr] = top > 0.f ? exponent - 6 : kNoSize;   // (zeros: scores of 0)
             Lse[buf][pr] = lse * kLog2e;
             Limit[buf][pr] = limit;
         }
@@ -154,7 +161,8 @@ void kv4_weights(WeightArgs a) {
                         s[4 * u + v] = fmaf(part[4 * u + v], scale[v], s[4 * u + v]);
                 }
             }
-            const float factor = Factor[buf][c], off = Lse[buf][c];
+            const float factor = ldexpf(a.scale_log2, Exponent[buf][c] + size);
+            const float off = Lse[buf][c];
             const int left = Limit[buf][c] - mine - 8 * h;
             if (__all(left > 23)) {   // every row sees every token
 #pragma unroll

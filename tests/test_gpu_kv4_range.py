@@ -135,3 +135,80 @@ def test_many_rows_before_a_leap(gpu_lib, cut):
     Q = rows(rng, (1, H, Lq, d), "fast_bf16")
     O, LSE = run(gpu_lib, c, Q, L, 0.1, "fast_bf16")
     check_rows_before(c, Q, O, LSE, L, [cut], 0.1, False, [0, H - 1])
+
+
+# few rows; rows whose weights are recomputed; many rows
+FORMS = [("fast_bf16", 1, 3, 70), ("strict_f32", 1, 3, 70), ("fast_bf16", 1, 40, 70),
+         ("strict_f32", 1, 40, 70), ("fast_bf16", 32, 64, 8200)]
+
+
+def one_head(rng, L, d, K=None, V=None):
+    """A cache of one head with these rows, or ordinary ones."""
+    c = filled(rng, 1, 1, L, d)
+    for which, x in ((0, K), (1, V)):
+        if x is not None:
+            c.put(which, 0, np.arange(L), x.astype(np.float32))
+    return c
+
+
+def check_heads(mg, rng, c, Q, H, scale, contract):
+    """Attention with weights over H heads that all hold what c's one does; the first
+    and the last two query heads against the reference."""
+    import torch
+    _, Hq, Lq, d = Q.shape
+    L, G, strict = c.dims[2], Hq // H, contract != "fast_bf16"
+    whole = ref.Cache(1, H, L, d)
+    for which in range(2):
+        whole.code[which] = np.repeat(c.code[which], H, 1)
+        whole.word[which] = np.repeat(c.word[which], H, 1)
+    w0 = rng.random((1, H, L)).astype(np.float32)
+    weight = dev(w0)
+    O, LSE = mg.attention_forward_kv4(dev(Q, dtype_of(contract)), dev(whole.to_bytes()), H=H, L=L,
+                                      causal=True, scale=scale, weight=weight, contract=contract)
+    O, LSE, weight = (host(t).astype(np.float64) for t in (O, LSE, weight))
+    for h in sorted({0, H - 1}):
+        W, tW = np.zeros(L), np.zeros(L)
+        for hq in range(h * G, (h + 1) * G):
+            rO, rL, P, tO, tL, tP = ref.attention(
+                Q[0, hq].astype(np.float64), [x[0, 0] for x in c.code],
+                [tuple(p[0, 0] for p in c.group(i)) for i in range(2)], L, Lq, True, scale, strict,
+                not strict and many_rows(H, G * Lq, L))
+            assert np.all(np.abs(LSE[0, hq] - rL) <= tL), (hq, (np.abs(LSE[0, hq] - rL) / tL).max())
+            assert np.all(np.abs(O[0, hq] - rO) <= tO), (hq, (np.abs(O[0, hq] - rO) / tO).max())
+            W += P.sum(0)
+            tW += tP.sum(0)
+        w = w0[0, h].astype(np.float64)
+        assert np.all(np.abs(weight[0, h] - (w + W)) <= tW + 2.0 ** -22 * (w + W)), h
+
+
+@pytest.mark.parametrize("contract,H,Lq,L", FORMS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("q,k,scale", [
+    (1e-30, 1e37, 1e-7),             # products of K and codes beyond f32, scores of some units
+    (2.0 ** -100, 2.0 ** 123, 2.0 ** -26),   # |scale| max |Q| below the smallest normal
+    (2.0 ** -120, 2.0 ** 120, -0.3),
+    (2.0 ** 120, 2.0 ** -120, 0.3),
+    (1e-5, 1e-35, 1e38),
+    (2.0 ** 100, 2.0 ** 120, 0.0),   # scores of 0 all the same
+    (0.0, 2.0 ** 124, 2.0 ** 100)])
+def test_keys_and_queries_of_any_size(gpu_lib, contract, H, Lq, L, d, q, k, scale):
+    """Only the scores have to be in range, not the parts they are made of."""
+    say("kv4 attention q %g k %g scale %g d%d %s Lq%d" % (q, k, scale, d, contract, Lq))
+    rng = np.random.default_rng(17)
+    c = one_head(rng, L, d, K=k * rng.standard_normal((1, L, d)))
+    Q = ref.bf16_round((q * rng.standard_normal((1, 2 * H, Lq, d))).astype(np.float32))
+    check_heads(gpu_lib, rng, c, Q, H, scale, contract)
+
+
+@pytest.mark.parametrize("contract,H,Lq,L", FORMS)
+def test_queries_of_every_size_over_large_keys(gpu_lib, contract, H, Lq, L):
+    """Rows of 1, 2^-60, 2^-100 and 0 beside one another: the small ones' scores are 0."""
+    say("kv4 attention, rows of every size %s Lq%d" % (contract, Lq))
+    rng = np.random.default_rng(18)
+    d = 64
+    c = one_head(rng, L, d, K=2.0 ** 122 * rng.standard_normal((1, L, d)))
+    Q = ref.bf16_round(rng.standard_normal((1, 2 * H, Lq, d)).astype(np.float32))
+    Q[0, :, 0] *= np.float32(2.0 ** -60)
+    Q[0, 0, 1] *= np.float32(2.0 ** -100)
+    Q[0, 1, 1] = 0
+    check_heads(gpu_lib, rng, c, Q, H, 2.0 ** -122, contract)
