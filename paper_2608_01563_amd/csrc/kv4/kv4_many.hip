@@ -555,7 +555,7 @@ void kv4_many(ManyArgs a) {
         return;
     }
     if (!valid) l = 0.f;
-    const float inv = l == 0.f ? 0.f : ldexpf(1.f / l, E - 15);
+    const float inv = 1.f / l;   // (2^(E - 15) of it may be below f32's normal numbers)
     uint16_t *to = a.O + at * D;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -564,7 +564,7 @@ void kv4_many(ManyArgs a) {
             uint16_t x[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                x[k] = to_bf16(l == 0.f ? 0.f : o[b][4 * u + k] * inv);
+                x[k] = to_bf16(l == 0.f ? 0.f : ldexpf(o[b][4 * u + k] * inv, E - 15));
             *reinterpret_cast<u32x2 *>(to + 32 * b + 8 * u + 4 * h) =
                 u32x2{x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16};
         }

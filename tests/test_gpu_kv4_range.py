@@ -212,3 +212,21 @@ def test_queries_of_every_size_over_large_keys(gpu_lib, contract, H, Lq, L):
     Q[0, 0, 1] *= np.float32(2.0 ** -100)
     Q[0, 1, 1] = 0
     check_heads(gpu_lib, rng, c, Q, H, 2.0 ** -122, contract)
+
+
+def test_tiny_values_of_many_tokens(gpu_lib):
+    """Equal probabilities of 202,135 tokens whose V is 2^-104 throughout: every sum is
+    exact, and O is that value.  (Row tiles enough that tokens are not split.)"""
+    import torch
+    mg = gpu_lib
+    say("kv4 attention of many rows, V of 2^-104")
+    n, d, Lq = 202135, 32, 256 * 256
+    V = torch.full((1, 1, n, d), 2.0 ** -104, dtype=torch.bfloat16, device="cuda")
+    cache = mg.kv4_cache(1, 1, n, d)
+    mg.mg_kv4_append(V, V, cache, L=n)
+    assert mg.mg_attn_fwd_kv4_workspace_bytes(1, 1, 1, Lq, n, d) == 0
+    Q = torch.zeros(1, 1, Lq, d, dtype=torch.bfloat16, device="cuda")
+    O, LSE = mg.attention_forward_kv4(Q, cache, H=1, L=n, causal=False, scale=1.0)
+    assert bool((O == 2.0 ** -104).all())
+    # the logarithm's two ulps and one more for its sum with the maximum
+    assert float((LSE.double() - np.log(n)).abs().max()) <= 3 * 2.0 ** -23 * np.log(n)
