@@ -2,8 +2,8 @@
 // each cached token, from Q, K and LSE: weight_j += sum over rows of
 // exp(S_ij - LSE_i).
 //
-// Tokens stay, rows stream: a wave keeps the codes and scales of 32 tokens in
-// registers and takes rows 32 at a time (32x32x16 products, S^T as in
+// Tokens stay, rows stream: a wave keeps the codes (strict: less 8, as the forward that
+// made LSE does) of 32 tokens in registers and takes rows 32 at a time (32x32x16 products, S^T as in
 // kv4_many.hip) from LDS, where its workgroup's eight waves prepare them once:
 // scaled f16 operands, group sums, factors, LSE and limits.  Sums stay in the
 // lanes until the end.  Where token tiles are too few for the GPU, the rows are
@@ -73,8 +73,8 @@ void kv4_weights(WeightArgs a) {
     const int tok = token_of(c);
 #pragma unroll
     for (int s = 0; s < NS; ++s)   // channels 16s + 8h + e: word 2s + h of the row
-        code[s] = code_operand(kw[tok * KR + k_word<D>(2 * s + h)]);
-    // Scales and minima are taken over 2^size, the largest of the wave's tokens (those
+        code[s] = operand_of<NP>(kw[tok * KR + k_word<D>(2 * s + h)]);
+    // Scales and bases are taken over 2^size, the largest of the wave's tokens (those
     // that are there and finite), and factors times it, so that products stay in range.
     const uint32_t own = kp[c * NG + (NG == 2 ? h : 0)];
     const float most = fmaxf(0x1p-4f * fabsf(group_min(own)), group_scale(own));
@@ -82,7 +82,7 @@ void kv4_weights(WeightArgs a) {
         max_of_wave(base + c < mask.n && most < INFINITY ? most : 0.f)));
     if (h < NG) Scale[w][h][c] = ldexpf(group_scale(own), -size);   // read by the wave itself
     const float low =
-        NG == 2 || h == 0 ? ldexpf(group_min(kp[tok * NG + (NG == 2 ? h : 0)]), -size) : 0.f;
+        NG == 2 || h == 0 ? ldexpf(base_of<NP>(kp[tok * NG + (NG == 2 ? h : 0)]), -size) : 0.f;
 
     // preparing rows: thread r * PER + k takes channels 8k..8k+7 of row r
     const int pr = tid / PER, pk = tid % PER;

@@ -230,3 +230,32 @@ def test_tiny_values_of_many_tokens(gpu_lib):
     assert bool((O == 2.0 ** -104).all())
     # the logarithm's two ulps and one more for its sum with the maximum
     assert float((LSE.double() - np.log(n)).abs().max()) <= 3 * 2.0 ** -23 * np.log(n)
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("Lq", [4, 24, 200])
+def test_strict_weights_of_codes_around_zero(gpu_lib, Lq, d):
+    """Keys of codes 8 but for two channels that no query has: every score is 0 exactly,
+    a sum of parts less 8 that are 0 each; as scale code + min it is a difference of
+    numbers in the thousands, off by a hundredth.  So rows give every token alike."""
+    import torch
+    mg = gpu_lib
+    say("kv4 strict weights, codes around zero Lq%d d%d" % (Lq, d))
+    rng = np.random.default_rng(19)
+    L = 64
+    K = np.zeros((1, 1, L, d), np.float32)
+    g = min(d, 64)
+    K[..., 0::g], K[..., 1::g] = -8, 7          # scale 1, minimum -8
+    c = ref.Cache(1, 1, L, d)
+    c.put(0, 0, np.arange(L), K[0])
+    c.put(1, 0, np.arange(L), rows(rng, (1, L, d), "strict_f32"))
+    assert (c.code[0][..., 2:g] == 8).all() and np.all(c.group(0)[0] == 1)
+    Q = np.abs(rows(rng, (1, 1, Lq, d), "strict_f32")) + 0.5
+    Q[..., 0::g] = Q[..., 1::g] = 0
+    weight = torch.zeros(1, 1, L, device="cuda")
+    O, LSE = mg.attention_forward_kv4(dev(Q), dev(c.to_bytes()), H=1, L=L, causal=False, scale=300.0,
+                                      weight=weight, contract="strict_f32")
+    # a row: LSE's rounding, of a number below 5, twice; sums of Lq probabilities
+    tol = (2 * 5 + 4 + Lq) * 2.0 ** -24
+    assert np.all(np.abs(host(LSE) - np.log(L)) <= 5 * 2.0 ** -23)
+    assert np.all(np.abs(host(weight) * L / Lq - 1) <= tol)
