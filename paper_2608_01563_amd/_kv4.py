@@ -3,7 +3,7 @@ marshalling only, in the manner of _binding.py.
 
 Every function checks the tensors it is given, runs on the tensors' own
 device (which need not be the current one) and raises MgError on a non-MG_OK
-status.  A cache is a uint8 tensor of mg_kv4_cache_bytes(B, H, L, d) bytes.
+status.  A cache is a uint8 tensor of exactly mg_kv4_cache_bytes(B, H, L, d) bytes.
 """
 import functools
 
@@ -37,8 +37,9 @@ def _need(dev, named):
 
 
 def _need_room(cache, B, H, L, d):
+    """The cache must be one of these sizes: in a larger one another layout lies."""
     need = mg_kv4_cache_bytes(B, H, L, d)   # 0 for bad sizes: the library says why
-    if cache.numel() < need:
+    if need and cache.numel() != need:
         raise ValueError("the cache has %d bytes, B=%d H=%d L=%d d=%d needs %d"
                          % (cache.numel(), B, H, L, d, need))
 

@@ -1,0 +1,18 @@
+"""Refusals of the 4-bit cache's entry points that need no GPU: a cache of other sizes
+than those given."""
+import pytest
+
+import paper_2608_01563_amd as mg
+from paper_2608_01563_amd import _kv4
+from test_kv4_cpu import lib  # noqa: F401
+
+
+@pytest.mark.parametrize("other", [(2, 3, 65, 64), (2, 4, 64, 64), (3, 3, 64, 64),
+                                   (2, 3, 64, 128), (2, 3, 64, 32), (1, 3, 64, 64)])
+def test_a_cache_of_other_sizes_is_refused(lib, other):  # noqa: F811
+    """Larger ones too: another layout would be read from them."""
+    import torch
+    sizes = (2, 3, 64, 64)
+    _kv4._need_room(torch.empty(mg.mg_kv4_cache_bytes(*sizes), dtype=torch.uint8), *sizes)
+    with pytest.raises(ValueError, match="bytes"):
+        _kv4._need_room(torch.empty(mg.mg_kv4_cache_bytes(*other), dtype=torch.uint8), *sizes)
