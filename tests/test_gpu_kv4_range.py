@@ -259,3 +259,61 @@ def test_strict_weights_of_codes_around_zero(gpu_lib, Lq, d):
     tol = (2 * 5 + 4 + Lq) * 2.0 ** -24
     assert np.all(np.abs(host(LSE) - np.log(L)) <= 5 * 2.0 ** -23)
     assert np.all(np.abs(host(weight) * L / Lq - 1) <= tol)
+
+
+def long_cache(mg, L, d, contract, K, V):
+    """L tokens in pieces; K, V: functions of a piece's first token and length to f32
+    tensors [n] that all channels have."""
+    import torch
+    cache, n, dt = mg.kv4_cache(1, 1, L, d), 1 << 21, dtype_of(contract)
+    for at in range(0, L, n):
+        m = min(n, L - at)
+        k, v = (f(at, m).to(dt)[None, None, :, None].expand(1, 1, m, d).contiguous()
+                for f in (K, V))
+        mg.mg_kv4_append(k, v, cache, dev(np.array([at], np.int32)), L=L, contract=contract)
+    return cache
+
+
+@pytest.mark.parametrize("contract,Lq", [("fast_bf16", 1), ("strict_f32", 3), ("fast_bf16", 256)])
+def test_every_token_of_the_longest_sequence(gpu_lib, contract, Lq):
+    """2^24 tokens of score 0 whose values are whole numbers below 16: a wave's and a
+    workgroup's sums are exact, so what is left are the roundings of joining 64 of
+    them, and three blocks of 32 tokens dropped or taken twice would show in LSE."""
+    import torch
+    mg = gpu_lib
+    say("kv4: every one of 2^24 tokens, %s Lq%d" % (contract, Lq))
+    L, d = 1 << 24, 32
+    torch.manual_seed(20)
+    total = []
+
+    def whole(at, m):   # larger ones later, so that a piece's place shows
+        v = torch.randint(0, 4, (m,), device="cuda") + 12 * at // L
+        total.append(int(v.sum()))
+        return v.float()
+
+    cache = long_cache(mg, L, d, contract, lambda at, m: torch.ones(m, device="cuda"), whole)
+    Q = torch.zeros(1, 1, Lq, d, dtype=dtype_of(contract), device="cuda")
+    O, LSE = mg.attention_forward_kv4(Q, cache, H=1, L=L, causal=False, scale=1.0,
+                                      contract=contract)
+    mean = sum(total) / L
+    tol = 2.0 ** -8 if contract == "fast_bf16" else 2.0 ** -24
+    # joining: at most 64 sums, products and the quotient
+    assert float((O.double() - mean).abs().max()) <= mean * (tol + 70 * 2.0 ** -24)
+    assert float((LSE.double() - 24 * np.log(2)).abs().max()) <= 2 * 2.0 ** -23 * 24 * np.log(2)
+
+
+def test_sums_of_many_rows_over_many_tokens(gpu_lib):
+    """Equal scores whose probabilities are no power of two round the same way at every
+    addition, so a chain of sums over all tokens drifts (2^23 of them: LSE by 2^-7).
+    Chains have at most 2^18 tokens, of which a lane adds 2^15 sums of four."""
+    import torch
+    mg = gpu_lib
+    say("kv4 attention of many rows, equal scores of 2^23 tokens")
+    L, d, Lq, score = 1 << 23, 32, 256 * 256, 0.6180339
+    cache = long_cache(mg, L, d, "fast_bf16", lambda at, m: torch.ones(m, device="cuda"),
+                       lambda at, m: torch.full((m,), 0.7109375, device="cuda"))
+    Q = torch.ones(1, 1, Lq, d, dtype=torch.bfloat16, device="cuda")
+    O, LSE = mg.attention_forward_kv4(Q, cache, H=1, L=L, causal=False, scale=score / d)
+    sums = 2.0 ** 15 * 2.0 ** -24
+    assert float((LSE.double() - (score + np.log(L))).abs().max()) <= sums + 2.0 ** -20
+    assert float((O.double() / 0.7109375 - 1).abs().max()) <= 2 * sums + 2.0 ** -8
