@@ -80,6 +80,7 @@ using mg::host::run_kernel;
 // where weights are gathered) and a head's regions below 4 GiB.
 constexpr int kMaxTokens = 1 << 24, kMaxHeads = 1 << 19;
 constexpr int64_t kMaxCache = 1 << 30, kMaxMoved = 1 << 28;
+constexpr float kLog2e = 1.4426950408889634f;   // as the kernels take it
 
 mg_status_t check_contract(mg_contract_t c) {
     if (c != MG_CONTRACT_STRICT_F32 && c != MG_CONTRACT_FAST_BF16 && c != MG_CONTRACT_ACCELERATED)
@@ -130,7 +131,8 @@ mg_status_t check_attn(int B, int Hq, int H, int Lq, int L, int d, float scale,
         (int64_t)B * Hq * Lq * d > INT32_MAX)
         return fail(MG_ERR_INVALID_ARGUMENT, "B*Hq*Lq*d exceeds 2^31-1 (B=%d Hq=%d Lq=%d d=%d)",
                     B, Hq, Lq, d);
-    if (!std::isfinite(scale)) return fail(MG_ERR_INVALID_ARGUMENT, "scale is not finite");
+    if (!std::isfinite(scale * kLog2e))
+        return fail(MG_ERR_INVALID_ARGUMENT, "scale log2 e is not finite (scale %g)", scale);
     return MG_OK;
 }
 
