@@ -13,7 +13,6 @@ struct Kv4Dim {
     static constexpr int kGroups = D <= 64 ? 1 : D / 64;
     static constexpr int kBlocks = D / 16;                  // 16-channel blocks
     static constexpr int kWide = kBlocks < 4 ? kBlocks : 4;   // V words a lane reads at once
-    static constexpr int kKWords = D / 8;                   // K words a token
     static constexpr int kSteps = D / 32;                   // 32-channel products
 };
 
@@ -35,9 +34,6 @@ __device__ __forceinline__ float group_min(uint32_t w) { return __uint_as_float(
 __device__ __forceinline__ int optional_len(const int32_t *len, int b, int full) {
     return key_limit(len, b, full);
 }
-
-__device__ __forceinline__ float load_elem(const float *p) { return *p; }
-__device__ __forceinline__ float load_elem(const uint16_t *p) { return bf16_to_f32(*p); }
 
 // bf16 bits, nearest even (one conversion instruction for a pair).
 __device__ __forceinline__ uint16_t to_bf16(float x) {
