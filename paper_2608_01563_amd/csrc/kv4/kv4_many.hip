@@ -20,11 +20,13 @@
 // A tile's words are loaded an iteration before they are unpacked, and its
 // group words one before that, because unpacking V needs them from LDS.
 //
-// 2 x 32 heads, 2,048 rows over 8,192 tokens of 128 channels, causal: 571 us, 842
+// 2 x 32 heads, 2,048 rows over 8,192 tokens of 128 channels, causal: 578 us, 833
 // TFLOP/s where a large bf16 product reaches 1,206.  The matrix units are busy 40 %
-// of the time; operand reads from LDS cost the most of the rest (without them 475
-// of then 603 us; without unpacking 570, without the exponentials 590).  32x32
-// products, because they read half as much of LDS for their work as 16x16 ones.
+// of the time and the vector units 55 %, hardly at once; operand reads from LDS cost
+// the most of the rest (without them 475 of then 603 us; without unpacking 570, without
+// the exponentials 590).  Bounds that leave out what a row does not see, and a unit of K
+// for the workgroup's rows, cost 4 us of it.  32x32 products, because they read half as
+// much of LDS for their work as 16x16 ones.
 #include "cdiv.h"
 #include "kv4_launch.h"
 #include "kv4_sweep.h"
@@ -51,6 +53,42 @@ struct ManyArgs {
     float scale_log2;
     int splits, row_tiles;
 };
+
+// What a workgroup and its wave w work on.
+struct ManyPlace {
+    int bh, split, G, rows;   // head, share of the tokens, query heads and rows of the head
+    Kv4Mask mask;
+    int front, back, r0;      // first row in front, at the back, of the wave
+    int front_end, back_end;  // tokens that these rows see
+    int begin, stop;          // tiles
+
+    // tokens that some of the rows from, ..., from + n - 1 sees
+    __device__ __forceinline__ int end_of(int from, int n) const {
+        return from < rows && from / G < mask.rows
+            ? max(mask.limit(min((min(rows, from + n) - 1) / G, mask.rows - 1)), 0) : 0;
+    }
+};
+__device__ __forceinline__ ManyPlace many_place(const ManyArgs &a, int id, int w) {
+    ManyPlace p;
+    const int share = id / a.row_tiles, tile = id - share * a.row_tiles;
+    p.bh = share / a.splits;
+    p.split = share - p.bh * a.splits;
+    p.G = a.G;
+    p.rows = a.G * a.Lq;
+    p.mask = sequence_mask(a.key_len, a.q_len, p.bh / a.H, a.L, a.Lq, a.causal);
+    // Four waves take rows from the front and four from the back: causal
+    // workgroups differ less in work, the first ones having the most.
+    p.front = kRows / 2 * tile;
+    p.back = kRows / 2 * (2 * a.row_tiles - 1 - tile);
+    p.r0 = w < kManyWaves / 2 ? p.front + 32 * w : p.back + 32 * (w - kManyWaves / 2);
+    p.front_end = p.end_of(p.front, kRows / 2);
+    p.back_end = p.end_of(p.back, kRows / 2);
+    const int tiles = (max(p.front_end, p.back_end) + kTokens - 1) / kTokens;
+    const int each = (tiles + a.splits - 1) / a.splits;
+    p.begin = p.split * each;
+    p.stop = min(tiles, p.begin + each);
+    return p;
+}
 
 // 32 query rows as operands of 32x32x16 products: lane column l%32, channels
 // 16s + 8(l/32) + e, in the slots of code_operand.
@@ -151,6 +189,30 @@ __device__ __forceinline__ void anew(const ManyArgs &a, int bh, int split, int f
     if (g == 0) a.LSE[at.at] = l != l ? l : row_lse(sweep.m, l);
 }
 
+// Those of the wave's rows in `which` anew, by halves of 16.  Last of all and from the
+// kernel's arguments, which are read again: with all that this needs kept through the
+// tile loop, scalars had to move to vector registers and back there (16 heads of 16,384
+// rows over 4,096 tokens of 128 channels: 462 us, so 457, and 451 without this part).
+template <int D>
+__device__ __forceinline__ void far_rows(uint32_t which, int w, int lane, void *lds) {
+    typedef const __attribute__((address_space(4))) ManyArgs *Arguments;
+    Arguments p = (Arguments)__builtin_amdgcn_kernarg_segment_ptr();
+    uint32_t id = blockIdx.x;
+    asm volatile("" : "+s"(p), "+s"(id));
+    const ManyArgs a = {p->Q, p->kw, p->vw, p->kp, p->vp, p->O, p->LSE, p->part, p->stat,
+                        p->key_len, p->q_len, p->H, p->G, p->Lq, p->L, p->Lp, p->causal,
+                        p->scale_log2, p->splits, p->row_tiles};
+    const ManyPlace at = many_place(a, id, w);
+    auto &groups = static_cast<BlockGroups<Kv4Dim<D>::kGroups> *>(lds)[w];
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half)
+        if (which >> (16 * half) & 0xffffu) {
+            const int first = at.r0 + 16 * half;
+            anew<D>(a, at.bh, at.split, first, 2 * at.begin,
+                    min(2 * at.stop, (at.end_of(first, 16) + 31) / 32), at.mask, groups, lane);
+        }
+}
+
 template <int D>
 __global__ __launch_bounds__(64 * kManyWaves) __attribute__((amdgpu_waves_per_eu(2, 8)))
 void kv4_many(ManyArgs a) {
@@ -165,37 +227,31 @@ void kv4_many(ManyArgs a) {
     __shared__ uint64_t Bad[4][NG];   // tokens whose V is not finite
     __shared__ int Es[4], Sizes[kManyWaves];
     __shared__ int FarCount, Far[kFarTiles][2];   // rows with limits in (first, second]
+    __shared__ int Ends[4];   // first and last limit of the rows in front, and at the back
 
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int share = blockIdx.x / a.row_tiles;
-    const int tile = blockIdx.x - share * a.row_tiles;
-    const int bh = share / a.splits, split = share - bh * a.splits;
-    const int rows = a.G * a.Lq;
-    const Kv4Mask mask = sequence_mask(a.key_len, a.q_len, bh / a.H, a.L, a.Lq, a.causal);
+    const ManyPlace place = many_place(a, blockIdx.x, w);
+    const Kv4Mask mask = place.mask;
+    const int bh = place.bh, split = place.split, rows = place.rows;
+    const int begin = place.begin, stop = place.stop;
 
-    // Four waves take rows from the front and four from the back: causal
-    // workgroups differ less in work, the first ones having the most.
-    const int front = kRows / 2 * tile, back = kRows / 2 * (2 * a.row_tiles - 1 - tile);
-    const int r0 = w < kManyWaves / 2 ? front + 32 * w : back + 32 * (w - kManyWaves / 2);
-    const int r = r0 + c;
+    const int r0 = place.r0, r = r0 + c;
     const bool in = r < rows;
     const int rr = in ? r : rows - 1, i = rr / a.G;
     const size_t at = ((size_t)bh * a.G + (rr - i * a.G)) * a.Lq + i;
     const int limit = mask.limit(i);
-    // tokens that some row of the workgroup, some row of the wave, every row
-    // of the wave sees
-    const auto end_of = [&](int from, int n) {
-        return from < rows && from / a.G < mask.rows
-            ? max(mask.limit(min((min(rows, from + n) - 1) / a.G, mask.rows - 1)), 0) : 0;
-    };
-    const int front_end = end_of(front, kRows / 2), back_end = end_of(back, kRows / 2);
-    const int end = max(front_end, back_end);
-    const int wave_end = end_of(r0, 32);
+    // tokens that some row of the wave, every row of the wave sees
+    const int wave_end = place.end_of(r0, 32);
     const int wave_all = r0 < rows ? mask.limit(r0 / a.G) : 0;
-
-    const int tiles = (end + kTokens - 1) / kTokens, each = (tiles + a.splits - 1) / a.splits;
-    const int begin = split * each, stop = min(tiles, begin + each);
+    if (tid == 64) {   // for wave 1, seldom
+        FarCount = 0;
+        Ends[0] = place.front < rows ? mask.limit(place.front / a.G) : INT32_MAX;
+        Ends[1] = place.front_end;
+        Ends[2] = place.back < rows ? mask.limit(place.back / a.G) : INT32_MAX;
+        Ends[3] = place.back_end;
+    }
+    __builtin_amdgcn_wave_barrier();   // one wave's LDS accesses stay in order
 
     const size_t head = (size_t)bh * a.Lp;
     const uint32_t *kw = a.kw + head * KR, *vw = a.vw + head / 8 * D;
@@ -228,8 +284,7 @@ void kv4_many(ManyArgs a) {
     int bound = kManyExp, known = kNone, far_tiles = 0;
     // whether [from, to] holds the limit of a row of the workgroup
     auto limits_in = [&](int from, int to) {
-        return (front < rows && max(mask.limit(front / a.G), from) <= min(front_end, to)) ||
-               (back < rows && max(mask.limit(back / a.G), from) <= min(back_end, to));
+        return max(Ends[0], from) <= min(Ends[1], to) || max(Ends[2], from) <= min(Ends[3], to);
     };
     auto put_params = [&](int t) {
         const int b = t & 3;
@@ -253,11 +308,9 @@ void kv4_many(ManyArgs a) {
                 if (lane == 0) Bad[b][g] = bad;
             }
             const float most = max_of_wave(size);
-            const int moved = __builtin_amdgcn_readfirstlane(
-                most > 0.f ? max(bound, __builtin_amdgcn_frexp_expf(most)) : kNone);
-            bound = max(bound, moved);
+            if (most > 0.f) bound = max(bound, __builtin_amdgcn_frexp_expf(most));
             if (lane == 0) Es[b] = bound;
-            if (bound > known + kFar) {
+            if (__any(bound > known + kFar)) {   // (the same in all lanes)
                 // Rows that see nothing of the tile from its first value near E on, if they
                 // see a value other than 0; after a leap also what a wave that works on
                 // the tile has of rows that end before it.
@@ -277,7 +330,7 @@ void kv4_many(ManyArgs a) {
                     ++far_tiles;
                 }
             }
-            known = moved != kNone ? bound : known;
+            if (most > 0.f) known = bound;
             // in the octet's slot order
             const int slot = (lane & 0x38) | (lane & 1) << 2 | (lane & 6) >> 1;
 #pragma unroll
@@ -455,7 +508,6 @@ void kv4_many(ManyArgs a) {
     };
 
     if (begin < stop) {
-        if (tid == 64) FarCount = 0;
         load_params(begin);
         load_words(begin);
         const float wave_size = max_of<16>(max_xor16((float)q.size));
@@ -519,23 +571,17 @@ void kv4_many(ManyArgs a) {
     }
 
     const bool valid = i < mask.rows;
+    uint32_t which = 0;   // rows of the wave that are computed anew (lanes l and l + 32 agree)
     if (begin < stop && FarCount > 0) {
-        __syncthreads();   // Ks is free
         bool far = false;
         for (int k = 0; k < FarCount; ++k) far |= limit > Far[k][0] && limit <= Far[k][1];
-        const uint32_t which = (uint32_t)__ballot(in && valid && far);   // lanes l and l + 32 agree
-        auto &groups = reinterpret_cast<BlockGroups<NG> *>(&Ks[0][0])[w];
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half)
-            if (which >> (16 * half) & 0xffffu)
-                anew<D>(a, bh, split, r0 + 16 * half, 2 * begin,
-                        min(2 * stop, (end_of(r0 + 16 * half, 16) + 31) / 32), mask, groups, lane);
-        if (which >> (c & 16) & 0xffffu) return;
+        which = (uint32_t)__ballot(in && valid && far);
+        __syncthreads();   // Ks is free
     }
 
     l = sum_xor32(l);
-    if (!in) return;
-    if (a.splits > 1) {
+    const bool stays = in && (which >> (c & 16) & 0xffffu) == 0;
+    if (stays && a.splits > 1) {
         const size_t slot = ((size_t)bh * a.splits + split) * rows + r;
         float *to = a.part + slot * D;
 #pragma unroll
@@ -552,23 +598,24 @@ void kv4_many(ManyArgs a) {
             a.stat[2 * slot] = valid ? m : -INFINITY;
             a.stat[2 * slot + 1] = valid ? ldexpf(l, -kLift) : 0.f;
         }
-        return;
+    } else if (stays) {
+        if (!valid) l = 0.f;
+        const float inv = 1.f / l;   // (2^(E - 15) of it may be below f32's normal numbers)
+        uint16_t *to = a.O + at * D;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                uint16_t x[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    x[k] = to_bf16(l == 0.f ? 0.f : ldexpf(o[b][4 * u + k] * inv, E - 15));
+                *reinterpret_cast<u32x2 *>(to + 32 * b + 8 * u + 4 * h) =
+                    u32x2{x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16};
+            }
+        if (h == 0) a.LSE[at] = l != l ? l : row_lse(m, ldexpf(l, -kLift));
     }
-    if (!valid) l = 0.f;
-    const float inv = 1.f / l;   // (2^(E - 15) of it may be below f32's normal numbers)
-    uint16_t *to = a.O + at * D;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            uint16_t x[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                x[k] = to_bf16(l == 0.f ? 0.f : ldexpf(o[b][4 * u + k] * inv, E - 15));
-            *reinterpret_cast<u32x2 *>(to + 32 * b + 8 * u + 4 * h) =
-                u32x2{x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16};
-        }
-    if (h == 0) a.LSE[at] = l != l ? l : row_lse(m, ldexpf(l, -kLift));
+    if (which != 0) far_rows<D>(which, w, lane, &Ks[0][0]);
 }
 
 template <int D>
