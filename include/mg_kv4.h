@@ -33,11 +33,17 @@
  * probabilities that query rows gave it.
  *
  * Contracts: MG_CONTRACT_FAST_BF16 (K, V, Q, O bf16) and MG_CONTRACT_STRICT_F32
- * (all f32).  Codes are exact matrix operands in every form.  Scores are exact
- * products summed in f32; strict operands Q and P enter as two f16 parts (within
- * 2^-23 of the f32 value), bf16 Q exactly.  Q is scaled by a power of two a row;
- * values 2^-29 below the row's largest lose bits.  MG_CONTRACT_ACCELERATED
- * gives exactly the strict results.  LSE, weights and the workspace are f32.
+ * (all f32).  Codes are exact matrix operands in every form but one, and scores are
+ * exact products summed in f32.  What is rounded to f16 on the way:
+ *   strict  Q, and a probability times a V scale, as two f16 parts (within 2^-23 of
+ *           the f32 value)
+ *   bf16    a probability times a V scale, once (2^-11); Q is exact
+ *   bf16, 128 query rows a cache head and more (2^25 pairs of a row and a token, and
+ *           more)  probabilities and V's values scale * code + min, each once (2^-11)
+ * f16 has no more range than that: Q's rows are scaled by a power of two, and values
+ * below 2^-29 (strict: 2^-17) of the row's largest are off by up to 2^-39 of it.  What
+ * it means for O stands at mg_attn_fwd_kv4.  MG_CONTRACT_ACCELERATED gives exactly the
+ * strict results.  LSE, weights and the workspace are f32.
  *
  * Ownership, asynchrony, errors: as for mg_attn.h.  The caller owns every
  * buffer; nothing is allocated; calls enqueue on `stream` and return;
@@ -101,9 +107,20 @@ mg_status_t mg_kv4_read(const void *cache, void *K, void *V,
  * (may be NULL), weight[b][h][j] grows by the probabilities that all rows of
  * h's query heads give token j < key_len[b].
  *
- * Q's rows are scaled to f16 range by a power of two: |scale| * max |Q| must
- * stay below 2^126, and V's scales below 2^100, or results are not finite.
- * Beside its relative errors O has an absolute one of up to 2^-110.
+ * In range are: |V| below 2^96 and |scale| * max |Q| * max |K| below 2^110, of the
+ * tokens and of the query rows that share them; Q, K and scale may have any size
+ * beside that (a scale whose product with log2 e is infinite is refused; one below
+ * 2^-126 loses bits).  Beyond it results may be infinite or NaN.
+ *
+ * Beside errors relative to sum p |v|, O has absolute ones, from f16's range.  With the
+ * largest V scale s that a row sees and its n tokens: up to 15 n 2^-35 s (strict 8 n).
+ * With many bf16 rows (above): up to 2^-22 of the largest |v| that it sees, and n 2^-35
+ * of it.  So a row's outputs lose bits where a token it sees has V above 2^25 times
+ * (strict: 2^13) that of those that matter, whatever its own probability.  Tokens that a
+ * row does not see have no part in it.  In any case: up to 2^-110.
+ *
+ * Sums are f32, in chains of at most 2^18 tokens (more where the workspace would pass
+ * 8 GiB): terms that are all alike may drift by some 2^-11 of their sum in one.
  */
 mg_status_t mg_attn_fwd_kv4(const void *Q, const void *cache, void *O, float *LSE,
                             float *weight, const int32_t *key_len, const int32_t *q_len,
@@ -113,7 +130,7 @@ mg_status_t mg_attn_fwd_kv4(const void *Q, const void *cache, void *O, float *LS
 
 /*
  * Bytes of workspace for it: partial outputs of the key splits that small
- * grids are cut into and, when weights are gathered, for at most 16 rows a
+ * grids and caches above 2^18 tokens are cut into and, when weights are gathered, for at most 16 rows a
  * cache head (Hq/H * Lq) their scores, for more the sums of the shares that
  * their rows are cut into.  0 also for invalid arguments.
  */

@@ -9,7 +9,11 @@
 // in registers for sequences up to 32,768 tokens.  Many tokens share a digit, so
 // LDS additions meet: from 4,097 tokens on first digits are counted in four places
 // (16 heads of 32,768: 24 us, 26 without), else a wave adds its first lane's digit
-// once for all that share it (37 us with plain additions, 27 so).
+// once for all that share it (37 us with plain additions, 27 so).  Registers are
+// laid out for 4, 12 or 32 times 1,024 tokens, unused ones costing their part of the
+// passes (16 heads of 5,000 to 12,000 tokens: 14.5 us with 12, 25 with 32).  Beyond, or
+// without them, weights are read in every pass: 33 us at 16,384 tokens where registers
+// take 25, 60 at 32,768 (25), 73 at 40,000, 222 at 131,072.
 //
 // kv4_compact: moves rows to where select's indices put them.  A workgroup owns
 // whole 128-byte columns of the cache (the K rows, 128 bytes of the V octets, or the

@@ -8,11 +8,12 @@
 // lane ends with D/64 whole words).  Tokens of the octet that are not written
 // keep their bits: their words are read, merged and written by this wave alone.
 //
-// Both directions are bound by HBM: 2 D elements and D + 8 max(1, D/64) cache
-// bytes a token and head.  4 x 8 heads of up to 8,192 bf16 tokens of 128 channels
-// (96 MB each way): 29 us written and 22 read back, 3.6 TB/s with both launches;
-// reading 134 MB of f32 25 us, 5.9 TB/s.  A wave an octet,
-// because V's words then have one writer and rows are read whole.
+// Either way moves 2 D elements and D + 8 max(1, D/64) cache bytes a token and head.
+// 4 x 8 heads of up to 8,192 bf16 tokens of 128 channels (108 MB each way): 22 us read
+// back, 4.9 TB/s, and 134 MB of f32 25 us, 5.9 TB/s: bound by HBM.  Written in 29 us,
+// 3.7 TB/s: the 700 vector instructions of an octet take some 70 % of a SIMD's issue
+// time beside it.  A wave an octet, because V's words then have one writer and rows are
+// read whole.
 #include "kv4_device.h"
 #include "kv4_launch.h"
 #include "cdiv.h"

@@ -11,7 +11,7 @@
 // above 1, and the scales to a power of two, moved up (and the sums rescaled, as
 // for a new maximum) when a block has a larger one that the row sees.  kRaise
 // lifts the products to the top of f16's range, so that products 2^-25 below the
-// largest keep all their bits (of the two strict parts: 2^-13).
+// largest scale's keep all their bits (of the two strict parts: 2^-13).
 #pragma once
 
 #include "kv4_tile.h"

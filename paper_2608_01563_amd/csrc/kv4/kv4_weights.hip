@@ -3,13 +3,13 @@
 // exp(S_ij - LSE_i).
 //
 // Tokens stay, rows stream: a wave keeps the codes (strict: less 8, as the forward that
-// made LSE does) of 32 tokens in registers and takes rows 32 at a time (32x32x16 products, S^T as in
-// kv4_many.hip) from LDS, where its workgroup's eight waves prepare them once:
-// scaled f16 operands, group sums, factors, LSE and limits.  Sums stay in the
-// lanes until the end.  Where token tiles are too few for the GPU, the rows are
+// made LSE does) of 32 tokens in registers and takes rows 32 at a time (32x32x16
+// products, S^T as in kv4_many.hip) from LDS, where its workgroup's eight waves prepare
+// them once: scaled f16 operands, group sums, exponents, LSE and limits.  Sums stay in
+// the lanes until the end.  Where token tiles are too few for the GPU, the rows are
 // shared out too, and shares of a weight are added in order by a second kernel.
 //
-// 16 heads of 16,384 causal rows over 4,096 tokens of 128 channels: 273 us, half of
+// 16 heads of 16,384 causal rows over 4,096 tokens of 128 channels: 274 us, half of
 // it vector instructions (about 200 for 32 x 32 probabilities, 16 of them
 // exponentials), a quarter matrix products.  Two workgroups a compute unit need at
 // most 128 registers, so scales come from LDS (with them in registers: 416 us where this made 286).

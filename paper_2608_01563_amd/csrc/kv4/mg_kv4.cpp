@@ -18,11 +18,12 @@ namespace mg {
 // with 128, 656/1034 with 512; d = 64: 200/181 with 128, 227/329 with 256.  It
 // needs the work too: 43/47 at 8 heads x 512 rows x 8,192 tokens (2^25) and 41/53
 // at 256 x 128 x 1,024 (the same), but 35/28 with 8 x 256 x 8,192, where its split
-// form hardly fills the GPU.  (128-row workgroups were slower at d = 128: their
-// unpacked tiles fill the LDS all the same.)  Tokens are split over workgroups
-// where there are fewer than the GPU holds at once: one of kv4_many or two of
-// kv4_rows a compute unit (with 1,280 drafted rows took 22.9 instead of 19.9 us, a
-// long batch 51 either way: each workgroup prepares its query rows and joins its
+// form hardly fills the GPU.  One bound for every d costs a tenth at most beside it
+// (96 rows of d = 128, 128 rows of d = 64).  (128-row workgroups were slower at d =
+// 128: their unpacked tiles fill the LDS all the same.)  Tokens are split over
+// workgroups where there are fewer than the GPU holds at once: one of kv4_many or two
+// of kv4_rows a compute unit (with 1,280 workgroups drafts took 22.9 instead of 19.9
+// us, a long batch 51 either way: each workgroup prepares its query rows and joins its
 // waves).  A split has at least 256 tokens.  It has at most 2^18, also where the GPU
 // is full: f32 sums of more drift where terms are alike (65,536 rows over 2^24 tokens of
 // equal score in one split: O off by 2.8 %, LSE by 0.02; so 3e-4), unless the

@@ -317,3 +317,29 @@ def test_sums_of_many_rows_over_many_tokens(gpu_lib):
     sums = 2.0 ** 15 * 2.0 ** -24
     assert float((LSE.double() - (score + np.log(L))).abs().max()) <= sums + 2.0 ** -20
     assert float((O.double() / 0.7109375 - 1).abs().max()) <= 2 * sums + 2.0 ** -8
+
+
+@pytest.mark.parametrize("Lq", [3, 24])
+def test_strict_queries_with_one_large_channel(gpu_lib, Lq):
+    """A channel 2^20 above a query's others, whose keys are 0: the others are held within
+    2^-39 of it (two f16 parts, of which the second ends at 2^-24 where the largest value
+    lies above 2^14), so scores are off by that times the keys beside the reference's
+    bound."""
+    say("kv4 strict queries with one large channel Lq%d" % Lq)
+    rng = np.random.default_rng(22)
+    L, d, scale = 200, 64, 0.1
+    K = rng.integers(-7, 7, (1, 1, L, d)).astype(np.float32)
+    K[..., 0], K[..., 1], K[..., 2] = -8, 7, 0          # scale 1, base 0: exact
+    c = one_head(rng, L, d, K=K[0])
+    assert np.array_equal(c.rows(0)[0, 0, :L], K[0, 0])
+    Q = rng.standard_normal((1, 1, Lq, d)).astype(np.float32)
+    Q[..., 2] = 2.0 ** 20
+    O, LSE = gpu_lib.attention_forward_kv4(dev(Q), dev(c.to_bytes()), H=1, L=L, causal=True,
+                                           scale=scale, contract="strict_f32")
+    rO, rL, _, tO, tL, _ = ref.attention(
+        Q[0, 0].astype(np.float64), [x[0, 0] for x in c.code],
+        [tuple(p[0, 0] for p in c.group(i)) for i in range(2)], L, Lq, True, scale, True)
+    score = scale * 2.0 ** (20 - 39) * np.abs(K).sum(-1).max()
+    O, LSE = host(O)[0, 0].astype(np.float64), host(LSE)[0, 0].astype(np.float64)
+    assert np.all(np.abs(LSE - rL) <= tL + score)
+    assert np.all(np.abs(O - rO) <= tO + 2 * score * np.abs(c.rows(1)).max())
