@@ -103,7 +103,7 @@ mg_status_t mg_kv4_read(const void *cache, void *K, void *V,
  *   (!causal or j <= i + key_len[b] - q_len[b])
  *
  * (its rows are the sequence's last tokens).  Rows that see nothing, rows at
- * or behind q_len[b] among them, get O = 0 and LSE = -inf.  With `weight`
+ * or behind q_len[b] among them (whatever these hold), get O = 0 and LSE = -inf.  With `weight`
  * (may be NULL), weight[b][h][j] grows by the probabilities that all rows of
  * h's query heads give token j < key_len[b].
  *

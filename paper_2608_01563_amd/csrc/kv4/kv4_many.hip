@@ -148,7 +148,7 @@ __device__ __forceinline__ void anew(const ManyArgs &a, int bh, int split, int f
     const RowAt at = row_at(in ? r : rows - 1, bh, a.G, a.Lq);
     const size_t head = (size_t)bh * a.Lp;
     Kv4Query<D, 1> q;
-    q.load(a.Q + at.at * D, in, g, a.scale_log2 < 0.f);
+    q.load(a.Q + at.at * D, in && at.i < mask.rows, g, a.scale_log2 < 0.f);
     const auto factors = Kv4Sweep<D, 1>::factors(q, a.scale_log2, lane);
     const int limit = mask.limit(at.i), all = mask.limit(first / a.G);
     Kv4Sweep<D, 1> sweep;
@@ -365,7 +365,8 @@ void kv4_many(ManyArgs a) {
     };
 
     Query32<D> q;
-    q.load(a.Q + at * D, in, h, a.scale_log2 < 0.f);
+    // (rows behind the sequence's, whatever they hold, are taken as zeros)
+    q.load(a.Q + at * D, in && i < mask.rows, h, a.scale_log2 < 0.f);
     float factor = 0.f;
     float m = -INFINITY, l = 0.f;
     int E = kManyExp;

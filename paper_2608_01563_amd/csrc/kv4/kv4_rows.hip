@@ -73,7 +73,9 @@ void kv4_rows(RowsArgs a) {
     const bool in = r < rows;
     const RowAt at = row_at(in ? r : rows - 1, bh, a.G, a.Lq);
     Kv4Query<D, NP> q;
-    q.load(static_cast<const T *>(a.Q) + at.at * D, in, g, a.scale_log2 < 0.f);
+    // (rows behind the sequence's, whatever they hold, are taken as zeros)
+    q.load(static_cast<const T *>(a.Q) + at.at * D, in && at.i < mask.rows, g,
+           a.scale_log2 < 0.f);
     const auto factors = Kv4Sweep<D, NP>::factors(q, a.scale_log2, lane);
 
     // the tokens that the tile's last and its first row see

@@ -343,3 +343,33 @@ def test_strict_queries_with_one_large_channel(gpu_lib, Lq):
     O, LSE = host(O)[0, 0].astype(np.float64), host(LSE)[0, 0].astype(np.float64)
     assert np.all(np.abs(LSE - rL) <= tL + score)
     assert np.all(np.abs(O - rO) <= tO + 2 * score * np.abs(c.rows(1)).max())
+
+
+@pytest.mark.parametrize("fill", [3e38, -1e30, np.inf, np.nan, 0.0])
+@pytest.mark.parametrize("contract,Hq,H,Lq,L", [
+    ("fast_bf16", 4, 2, 5, 70), ("strict_f32", 4, 2, 5, 70), ("fast_bf16", 4, 2, 60, 300),
+    ("strict_f32", 4, 2, 60, 300), ("fast_bf16", 16, 8, 600, 4000)])
+def test_rows_behind_the_last_query_may_hold_anything(gpu_lib, contract, Hq, H, Lq, L, fill):
+    """Query rows at and behind q_len have no part in what the others get."""
+    import torch
+    mg = gpu_lib
+    say("kv4 attention, padding of %g %s Lq%d" % (fill, contract, Lq))
+    rng = np.random.default_rng(23)
+    B, d, dt = 3, 64, dtype_of(contract)
+    K, V = (dev(rows(rng, (B, H, L, d), contract), dt) for _ in range(2))
+    cache = mg.kv4_cache(B, H, L, d)
+    mg.mg_kv4_append(K, V, cache, L=L, contract=contract)
+    q_len = [Lq, Lq // 2 + 1, 0]
+    Q = dev(rows(rng, (B, Hq, Lq, d), contract), dt)
+
+    def run():
+        w = torch.zeros(B, H, L, device="cuda")
+        O, LSE = mg.attention_forward_kv4(Q, cache, H=H, L=L, causal=True, scale=0.1, weight=w,
+                                          q_len=dev(np.array(q_len, np.int32)), contract=contract)
+        return O, LSE, w
+
+    want = run()
+    for b, n in enumerate(q_len):
+        Q[b, :, n:] = fill
+    for a, b in zip(run(), want):
+        assert torch.equal(a, b)
