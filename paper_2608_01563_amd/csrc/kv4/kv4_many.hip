@@ -10,7 +10,8 @@
 //       so far, so that one product per 16 tokens covers scale and minimum;
 //       rows that see a tile in part, and of its values only some that are
 //       2^kFar below its E, are computed anew in kv4_sweep.h's form, whose
-//       bounds are a row's own
+//       bounds are a row's own (a call with such rows in every tile takes about
+//       twice as long, with one token so far above the others no longer at 8,192)
 //   P   f16, at most 2^15
 //
 // The row order of the score product swaps bits 2 and 3 of the token, which
