@@ -103,9 +103,9 @@ mg_status_t mg_kv4_read(const void *cache, void *K, void *V,
  *   (!causal or j <= i + key_len[b] - q_len[b])
  *
  * (its rows are the sequence's last tokens).  Rows that see nothing, rows at
- * or behind q_len[b] among them (whatever these hold), get O = 0 and LSE = -inf.  With `weight`
- * (may be NULL), weight[b][h][j] grows by the probabilities that all rows of
- * h's query heads give token j < key_len[b].
+ * or behind q_len[b] among them (whatever these hold), get O = 0 and LSE =
+ * -inf.  With `weight` (may be NULL), weight[b][h][j] grows by the probabilities
+ * that all rows of h's query heads give token j < key_len[b].
  *
  * In range are: |V| below 2^96 and |scale| * max |Q| * max |K| below 2^110, of the
  * tokens and of the query rows that share them; Q, K and scale may have any size
@@ -130,9 +130,10 @@ mg_status_t mg_attn_fwd_kv4(const void *Q, const void *cache, void *O, float *LS
 
 /*
  * Bytes of workspace for it: partial outputs of the key splits that small
- * grids and caches above 2^18 tokens are cut into and, when weights are gathered, for at most 16 rows a
- * cache head (Hq/H * Lq) their scores, for more the sums of the shares that
- * their rows are cut into.  0 also for invalid arguments.
+ * grids and caches above 2^18 tokens are cut into and, when weights are
+ * gathered, for at most 16 rows a cache head (Hq/H * Lq) their scores, for more
+ * the sums of the shares that their rows are cut into.  0 also for invalid
+ * arguments.
  */
 size_t mg_attn_fwd_kv4_workspace_bytes(int B, int Hq, int H, int Lq, int L, int d, int weights,
                                        mg_contract_t contract);

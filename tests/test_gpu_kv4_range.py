@@ -373,3 +373,45 @@ def test_rows_behind_the_last_query_may_hold_anything(gpu_lib, contract, Hq, H, 
         Q[b, :, n:] = fill
     for a, b in zip(run(), want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("Hq,H,Lq,L,d", [(16, 4, 700, 4000, 64), (6, 2, 1500, 3100, 128)])
+def test_many_rows_of_a_padded_batch_before_far_values(gpu_lib, Hq, H, Lq, L, d):
+    """Sequences of different length and number of rows, grouped heads: in each a token
+    2^70 above the others somewhere among those that only later rows see."""
+    mg = gpu_lib
+    say("kv4 attention of many rows, a padded batch, far values Hq%d Lq%d d%d" % (Hq, Lq, d))
+    key_len, q_len = [L - 7, Lq, Lq + 300, 0], [Lq, Lq, Lq - 90, 5]
+    B = len(key_len)
+    assert many_rows(B * H, Hq // H * Lq, L)
+    rng = np.random.default_rng(24)
+    c = filled(rng, B, H, L, d)
+    cuts = [n - q + 3 * q // 5 for n, q in zip(key_len, q_len)]
+    for b, cut in enumerate(cuts[:3]):
+        big = rows(rng, (H, 1, d), "strict_f32") * np.float32(2.0 ** 70)
+        c.put(1, b, np.array([cut]), big.astype(np.float32))
+    Q = rows(rng, (B, Hq, Lq, d), "fast_bf16")
+    ints = lambda x: dev(np.array(x, np.int32))
+    O, LSE = mg.attention_forward_kv4(dev(Q, dtype_of("fast_bf16")), dev(c.to_bytes()), H=H, L=L,
+                                      causal=True, scale=0.1, key_len=ints(key_len),
+                                      q_len=ints(q_len), contract="fast_bf16")
+    O, LSE = host(O).astype(np.float64), host(LSE).astype(np.float64)
+    for b in range(B):
+        n, q = key_len[b], q_len[b]
+        assert not O[b, :, q:].any() and np.isneginf(LSE[b, :, q:]).all()
+        if n == 0:
+            assert not O[b].any() and np.isneginf(LSE[b]).all()
+            continue
+        for hq in (0, Hq - 1):
+            h = hq // (Hq // H)
+            done = 0
+            for end in (cuts[b], n):
+                m = end - (n - q)
+                rO, rL, _, tO, tL, _ = ref.attention(
+                    Q[b, hq, :m].astype(np.float64), [x[b, h] for x in c.code],
+                    [tuple(p[b, h] for p in c.group(i)) for i in range(2)], end, m, True, 0.1,
+                    False, True)
+                tO = tO + MANY_UNITS * np.abs(c.rows(1)[b, h, :end]).max()
+                assert np.all(np.abs(O[b, hq, done:m] - rO[done:]) <= tO[done:]), (b, hq, end)
+                assert np.all(np.abs(LSE[b, hq, done:m] - rL[done:]) <= tL[done:]), (b, hq, end)
+                done = m
