@@ -1,9 +1,10 @@
 """MI355X (gfx950) attention forward and backward, attention over a 4-bit
-key/value cache, and the two derivatives of a 2-D convolution, behind a C ABI.
+and over a paged key/value cache, and the two derivatives of a 2-D convolution, behind a C ABI.
 
 The compute path is libmg.so (hand-written HIP kernels, see csrc/,
-include/mg_attn.h, include/mg_kv4.h and include/mg_conv.h); this package is its ctypes binding.  PyTorch is used only
-for device memory and streams.
+include/mg_attn.h, include/mg_kv4.h, include/mg_paged.h and include/mg_conv.h);
+this package is its ctypes binding.  PyTorch is used only for device memory and
+streams.
 """
 from ._binding import (  # noqa: F401
     ACCELERATED,
@@ -12,6 +13,7 @@ from ._binding import (  # noqa: F401
     HEADER_PATH,
     KV4_HEADER_PATH,
     LIB_PATH,
+    PAGED_HEADER_PATH,
     STRICT_F32,
     MgError,
     attention_backward,
@@ -49,4 +51,17 @@ from ._kv4 import (  # noqa: F401
     mg_kv4_cache_bytes,
     mg_kv4_evict,
     mg_kv4_read,
+)
+from ._paged import (  # noqa: F401
+    attention_forward_paged,
+    mg_attn_fwd_paged,
+    mg_attn_fwd_paged_sparse,
+    mg_attn_fwd_paged_sparse_workspace_bytes,
+    mg_attn_fwd_paged_workspace_bytes,
+    mg_paged_append,
+    mg_paged_resize,
+    mg_paged_resize_workspace_bytes,
+    mg_paged_select,
+    mg_paged_select_workspace_bytes,
+    paged_cache,
 )

@@ -14,6 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libmg.so")
 HEADER_PATH = os.path.join(os.path.dirname(HERE), "include", "mg_attn.h")
 KV4_HEADER_PATH = os.path.join(os.path.dirname(HERE), "include", "mg_kv4.h")
+PAGED_HEADER_PATH = os.path.join(os.path.dirname(HERE), "include", "mg_paged.h")
 CONV_HEADER_PATH = os.path.join(os.path.dirname(HERE), "include", "mg_conv.h")
 
 STRICT_F32 = 0
@@ -93,6 +94,25 @@ def _declare(lib):
     lib.mg_kv4_evict.argtypes = [vp, vp, vp, vp, vp, vp, vp, c_int, c_int, c_int, c_int, c_int,
                                  c_int, vp]
     lib.mg_kv4_evict.restype = c_int
+    lib.mg_paged_resize_workspace_bytes.argtypes = [c_int] * 2
+    lib.mg_paged_resize_workspace_bytes.restype = c_size
+    lib.mg_paged_resize.argtypes = [vp] * 9 + [c_int] * 5 + [vp, c_size, vp]
+    lib.mg_paged_resize.restype = c_int
+    lib.mg_paged_append.argtypes = [vp] * 6 + [c_int] * 6 + [vp]
+    lib.mg_paged_append.restype = c_int
+    lib.mg_attn_fwd_paged_workspace_bytes.argtypes = [c_int] * 8
+    lib.mg_attn_fwd_paged_workspace_bytes.restype = c_size
+    lib.mg_attn_fwd_paged.argtypes = [vp] * 8 + [c_int] * 9 + [c_float, c_int, vp, c_size, vp]
+    lib.mg_attn_fwd_paged.restype = c_int
+    lib.mg_paged_select_workspace_bytes.argtypes = [c_int] * 8
+    lib.mg_paged_select_workspace_bytes.restype = c_size
+    lib.mg_paged_select.argtypes = [vp] * 6 + [c_int] * 13 + [vp, c_size, vp]
+    lib.mg_paged_select.restype = c_int
+    lib.mg_attn_fwd_paged_sparse_workspace_bytes.argtypes = [c_int] * 8
+    lib.mg_attn_fwd_paged_sparse_workspace_bytes.restype = c_size
+    lib.mg_attn_fwd_paged_sparse.argtypes = [vp] * 9 + [c_int] * 10 + [c_float, c_int, vp, c_size,
+                                                                       vp]
+    lib.mg_attn_fwd_paged_sparse.restype = c_int
     lib.mg_status_string.argtypes = [c_int]
     lib.mg_status_string.restype = ctypes.c_char_p
     lib.mg_last_error_detail.argtypes = []

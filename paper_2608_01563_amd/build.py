@@ -1,5 +1,5 @@
-"""Build libmg.so (the C-ABI attention, convolution-derivative and 4-bit cache
-library) in-tree for gfx950.
+"""Build libmg.so (the C-ABI attention, convolution-derivative, 4-bit and paged
+cache library) in-tree for gfx950.
 
     python -m paper_2608_01563_amd.build [-v]
 
@@ -18,7 +18,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
-PARTS = ("conv", "kv4")   # folders of csrc/ with sources of their own
+PARTS = ("conv", "kv4", "paged")   # folders of csrc/ with sources of their own
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libmg.so")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")

@@ -1,0 +1,220 @@
+// paged_append.hip -- rows of K and V into their slots, and the bounds of the
+// pages they go to.
+//
+// A wave takes R rows of one head, 16 bytes a lane, and keeps their K.  Rows whose
+// slots follow each other inside a page are a run; the wave in whose rows a run
+// begins owns it, reads on to the run's end where that lies behind its rows, and
+// writes its bounds: every page has one writer, and no order of waves matters.  A
+// run of one row (a decode step) needs no reduction over lanes and costs nothing
+// beside its row.
+#include "paged_device.h"
+#include "paged_launch.h"
+
+namespace mg {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+
+struct AppendArgs {
+    const char *K, *V;
+    char *Kp, *Vp, *bounds;
+    const int32_t *slot;
+    int T, H, shift, N;
+    int64_t waves;
+};
+
+template <typename T>
+struct Piece {   // the elements of 16 bytes
+    static constexpr int kN = 16 / sizeof(T);
+    // the largest finite value
+    static constexpr float kMost = sizeof(T) == 2 ? 0x1.fep127f : 0x1.fffffep127f;
+    float x[kN];
+
+    __device__ __forceinline__ static Piece of(u32x4 v) {
+        Piece p;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 2) {
+                p.x[2 * e] = __uint_as_float(v[e] << 16);
+                p.x[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+            } else {
+                p.x[e] = __uint_as_float(v[e]);
+            }
+        }
+        return p;
+    }
+    __device__ __forceinline__ void store(char *to) const {
+        u32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 2)
+                v[e] = to_bf16(x[2 * e]) | (uint32_t)to_bf16(x[2 * e + 1]) << 16;
+            else
+                v[e] = __float_as_uint(x[e]);
+        }
+        *reinterpret_cast<u32x4 *>(to) = v;
+    }
+};
+
+// Smallest and largest (fminf and fmaxf leave NaN out).
+template <typename T>
+struct Bounds {
+    Piece<T> lo, hi;
+
+    __device__ __forceinline__ Bounds() {
+#pragma unroll
+        for (int e = 0; e < Piece<T>::kN; ++e) lo.x[e] = Piece<T>::kMost, hi.x[e] = -Piece<T>::kMost;
+    }
+    __device__ __forceinline__ void join(const Piece<T> &l, const Piece<T> &h) {
+#pragma unroll
+        for (int e = 0; e < Piece<T>::kN; ++e) {
+            lo.x[e] = fminf(lo.x[e], l.x[e]);
+            hi.x[e] = fmaxf(hi.x[e], h.x[e]);
+        }
+    }
+    __device__ __forceinline__ void add(const Piece<T> &p) { join(p, p); }
+    // With what the page's bounds were, unless the run begins it.
+    __device__ __forceinline__ void write(char *at, int row_bytes, bool begun) {
+        if (begun)
+            join(Piece<T>::of(*reinterpret_cast<const u32x4 *>(at)),
+                 Piece<T>::of(*reinterpret_cast<const u32x4 *>(at + row_bytes)));
+#pragma unroll
+        for (int e = 0; e < Piece<T>::kN; ++e) {
+            lo.x[e] = fmaxf(lo.x[e], -Piece<T>::kMost);   // infinities
+            hi.x[e] = fminf(hi.x[e], Piece<T>::kMost);
+        }
+        lo.store(at);
+        hi.store(at + row_bytes);
+    }
+};
+
+template <typename T, int D, int NI>
+__global__ __launch_bounds__(kThreads)
+void paged_append(AppendArgs a) {
+    constexpr int RB = D * (int)sizeof(T), RL = RB / 16;   // lanes a row
+    constexpr int RPI = 64 / RL, R = RPI * NI;             // rows a read, rows a wave
+    static_assert(R < 64, "a lane for every row's slot and the next one's");
+    const int lane = threadIdx.x & 63, sub = lane / RL;
+    const int64_t wave = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (wave >= a.waves) return;
+    const int h = (int)(wave % a.H), t0 = (int)(wave / a.H) * R;
+    const int page = 1 << a.shift;
+    const uint32_t slots = (uint32_t)a.N << a.shift;
+    const size_t piece = (size_t)16 * (lane % RL);
+
+    const auto slot_of = [&](int t) { return t < a.T ? a.slot[t] : -1; };
+    const auto row_of = [&](const char *rows, int t) {
+        return *reinterpret_cast<const u32x4 *>(rows + ((size_t)t * a.H + h) * RB + piece);
+    };
+    // lane j <= R: the slot of row t0 + j, whether it goes on with the one before
+    const int slot = slot_of(t0 + lane);
+    const int before = t0 + lane > 0 ? slot_of(t0 + lane - 1) : -1;
+    u32x4 k[NI], v[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        const int t = min(t0 + i * RPI + sub, a.T - 1);
+        k[i] = row_of(a.K, t);
+        v[i] = row_of(a.V, t);
+    }
+    const bool good = (uint32_t)slot < slots;
+    const bool on = good && (slot & (page - 1)) != 0 && before == slot - 1;
+    const uint64_t mine = (1ull << R) - 1;
+    const uint64_t ons = __ballot(on), starts = __ballot(good && !on) & mine;
+    const uint64_t singles = starts & ~(ons >> 1);
+    // a head's rows in the pools, and its bounds
+    const auto head_of = [&](int s) { return (size_t)(s >> a.shift) * a.H + h; };
+    const auto bounds_of = [&](int s) { return a.bounds + head_of(s) * 2 * RB + piece; };
+
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        const int j = i * RPI + sub, s = __shfl(slot, j, 64);
+        if ((uint32_t)s >= slots) continue;
+        const size_t to = ((head_of(s) << a.shift) + (s & (page - 1))) * RB + piece;
+        *reinterpret_cast<u32x4 *>(a.Kp + to) = k[i];
+        *reinterpret_cast<u32x4 *>(a.Vp + to) = v[i];
+        if (a.bounds != nullptr && (singles >> j & 1)) {
+            Bounds<T> b;
+            b.add(Piece<T>::of(k[i]));
+            b.write(bounds_of(s), RB, (s & (page - 1)) != 0);
+        }
+    }
+    if (a.bounds == nullptr) return;
+    for (uint64_t left = starts & ~singles; left != 0; left &= left - 1) {
+        const int from = __builtin_ctzll(left);
+        const int s = __builtin_amdgcn_readlane(slot, from);
+        // rows from .. end - 1 of the wave's, and those behind them
+        const uint64_t rest = ~ons >> (from + 1);
+        int end = from + 1 + (rest == 0 ? 64 : __builtin_ctzll(rest));
+        const bool further = end > R;
+        end = min(end, R);
+        Bounds<T> b;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int j = i * RPI + sub;
+            if (j >= from && j < end) b.add(Piece<T>::of(k[i]));
+        }
+        if (further)
+            for (int t = t0 + R;; t += 64) {
+                // how many of the next 64 rows are the run's
+                const int want = s + (t - t0 - from) + lane;
+                const bool same = (want >> a.shift) == (s >> a.shift) && slot_of(t + lane) == want;
+                const uint64_t other = ~__ballot(same);
+                const int count = other == 0 ? 64 : __builtin_ctzll(other);
+                constexpr int AT_ONCE = 4;
+                for (int j = sub; j < count; j += AT_ONCE * RPI) {
+                    u32x4 x[AT_ONCE];
+#pragma unroll
+                    for (int e = 0; e < AT_ONCE; ++e)   // (past the end the last row again)
+                        x[e] = row_of(a.K, t + min(j + e * RPI, count - 1));
+#pragma unroll
+                    for (int e = 0; e < AT_ONCE; ++e) b.add(Piece<T>::of(x[e]));
+                }
+                if (count < 64) break;
+            }
+#pragma unroll
+        for (int m = RL; m < 64; m *= 2) {
+            Piece<T> l, u;
+#pragma unroll
+            for (int e = 0; e < Piece<T>::kN; ++e) {
+                l.x[e] = xor_lanes(b.lo.x[e], m);
+                u.x[e] = xor_lanes(b.hi.x[e], m);
+            }
+            b.join(l, u);
+        }
+        if (sub == 0) b.write(bounds_of(s), RB, (s & (page - 1)) != 0);
+    }
+}
+
+template <typename T, int D, int NI>
+hipError_t append(const PagedAppend &p, AppendArgs a, hipStream_t s) {
+    constexpr int R = 64 / (D * (int)sizeof(T) / 16) * NI;
+    a.waves = (int64_t)((p.T + R - 1) / R) * p.H;
+    paged_append<T, D, NI><<<(unsigned)((a.waves + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+// Few rows: one read a wave, so that all compute units have some; many: as many as
+// keep their loads together.
+template <typename T, int D>
+hipError_t append(const PagedAppend &p, const AppendArgs &a, hipStream_t s) {
+    constexpr int RPI = 64 / (D * (int)sizeof(T) / 16);
+    if ((int64_t)p.T * p.H <= 16384) return append<T, D, 1>(p, a, s);
+    return append<T, D, (32 / RPI > 8 ? 8 : 32 / RPI)>(p, a, s);
+}
+
+}  // namespace
+
+hipError_t launch_paged_append(const PagedAppend &p, const void *K, const void *V, void *Kp,
+                               void *Vp, void *bounds, bool bf16, hipStream_t s) {
+    const AppendArgs a = {static_cast<const char *>(K), static_cast<const char *>(V),
+                          static_cast<char *>(Kp), static_cast<char *>(Vp),
+                          static_cast<char *>(bounds), p.slot, p.T, p.H, p.shift, p.N, 0};
+    if (bf16)
+        return p.d == 32 ? append<uint16_t, 32>(p, a, s) : p.d == 64 ? append<uint16_t, 64>(p, a, s)
+                                                                     : append<uint16_t, 128>(p, a, s);
+    return p.d == 32 ? append<float, 32>(p, a, s) : p.d == 64 ? append<float, 64>(p, a, s)
+                                                              : append<float, 128>(p, a, s);
+}
+
+}  // namespace mg

@@ -1,0 +1,622 @@
+// paged_attn.hip -- attention of a few query rows over a paged cache.
+//
+// A workgroup takes one cache head, 16 of the rows that share it and one unit: a
+// stretch of a sequence's tokens (or of the pages that a row's list names).  Its
+// four waves take blocks of 32 tokens (f32, d = 128: 16) in turn, each with its
+// own online softmax, and join through LDS; units of one sequence join in
+// paged_join.
+//
+// No operand passes through LDS.  A score tile is S^T = K Q^T: lane (c, g) = (l %
+// 16, l / 16) holds 16-byte pieces 4 s + g of token c's K row and of row c's Q row,
+// whatever channels these are, since a contraction's order is free.  S^T leaves
+// lane (c, g) with tokens 4 g .. 4 g + 3 of row c, which is the operand of the
+// second product O^T = V^T P^T if V's tokens come in that order: the lane reads
+// D/16 channels of the rows 4 g + t, 16 lanes a whole row, and pairs of them are
+// put together by one byte permutation a word (bf16).
+//
+// Pages are found through a table whose next 64 entries a wave keeps in a
+// register.  Tiles of 16 tokens are read through buffer descriptors that end where
+// the sequence does: behind it zeros come back, and nothing is read.
+//
+// bf16 probabilities enter as two bf16 parts each, which the matrix units have room
+// for.
+#include <type_traits>
+
+#include "paged_device.h"
+#include "paged_launch.h"
+
+namespace mg {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kRows = 16;
+constexpr int kFar = 1 << 30;   // a token that no row sees
+
+struct AttnArgs {
+    const void *Q, *Kp, *Vp;
+    void *O;
+    float *LSE, *part;
+    float2 *stat;
+    int2 *info;   // nullptr: every sequence (sparse: row) is one unit, nothing to join
+    const int32_t *table, *index, *key_len, *q_len;
+    int B, H, G, Lq, P, N, shift, causal, keep;
+    float scale_log2;
+    int splits, chunk, share, tiles;
+};
+
+// One unit: blocks [first, first + count) of sequence b (sparse: of row i's list);
+// its sequence has `splits` units, the first of them number `base`.
+struct Unit {
+    int b, i, first, count, splits, base, split;
+};
+
+// Which sequence unit u belongs to where lengths decide: every sequence is cut
+// into units of `chunk` blocks (at least one unit each), chunk so that all lengths
+// together make about `share` units.
+__device__ __forceinline__ Unit unit_by_length(const AttnArgs &a, int u, int lane) {
+    const int capacity = a.P << a.shift;
+    const auto blocks_of = [&](int b) {
+        return b < a.B ? (uint32_t)(key_limit(a.key_len, b, capacity) + 31) / 32 : 0u;
+    };
+    const uint32_t mine = blocks_of(lane);
+    uint32_t total = mine;
+    for (int b = 64 + lane; b < a.B + lane; b += 64) total += blocks_of(b);
+    total = wave_sum(total);
+    uint32_t chunk = (total + a.share - 1) / a.share;
+    chunk = min(max((chunk + kWaves - 1) / kWaves * kWaves, (uint32_t)a.chunk), 1u << 13);
+    Unit r = {-1, 0, 0, (int)chunk, 0, 0, 0};
+    uint32_t carry = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        const uint32_t n = b0 == 0 ? mine : blocks_of(b0 + lane);
+        const uint32_t parts = b0 + lane < a.B ? max((n + chunk - 1) / chunk, 1u) : 0u;
+        const uint32_t end = wave_scan(parts, lane);
+        const uint64_t past = __ballot(carry + end > (uint32_t)u);
+        if (past != 0) {
+            const int at = __builtin_ctzll(past);
+            r.b = b0 + at;
+            r.splits = __builtin_amdgcn_readlane(parts, at);
+            r.base = carry + __builtin_amdgcn_readlane(end, at) - r.splits;
+            r.split = u - r.base;
+            r.first = r.split * (int)chunk;
+            return r;
+        }
+        carry += __builtin_amdgcn_readlane(end, 63);
+    }
+    return r;
+}
+
+template <typename T, int D>
+struct Shape {
+    static constexpr bool kHalf = sizeof(T) == 2;
+    static constexpr int kRowBytes = D * (int)sizeof(T);
+    static constexpr int kTiles = !kHalf && D == 128 ? 1 : 2;   // of 16 tokens a block
+    static constexpr int kTok = 16 * kTiles;
+    static constexpr int kPieces = kRowBytes / 64;   // 16-byte pieces of K a lane
+    static constexpr int kN = D / 16;                // channels of V a lane
+    static constexpr int kWords = kRowBytes / 64;    // 4-byte words of them
+    // channel j (of kN) of the m-th lane that shares a V row
+    static __device__ __forceinline__ constexpr int channel(int m, int j) {
+        if (!kHalf && D == 128) return 64 * (j / 4) + 4 * m + j % 4;
+        return kN * m + j;
+    }
+};
+
+// A block's K pieces and V words.
+template <typename T, int D>
+struct Block {
+    using S = Shape<T, D>;
+    u32x4 k[S::kTiles][S::kPieces];
+    uint32_t v[S::kTiles][4][S::kWords];
+
+    __device__ __forceinline__ void load_k(int t, __amdgpu_buffer_rsrc_t r, int at) {
+#pragma unroll
+        for (int s = 0; s < S::kPieces; ++s)
+            k[t][s] = __builtin_bit_cast(
+                u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at + 64 * s, 0, 0));
+    }
+    __device__ __forceinline__ void load_v(int t, __amdgpu_buffer_rsrc_t r, int at) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int o = at + x * S::kRowBytes;
+            if constexpr (S::kWords >= 4) {
+#pragma unroll
+                for (int q = 0; q < S::kWords / 4; ++q) {
+                    const u32x4 y = __builtin_bit_cast(
+                        u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, o + 256 * q, 0, 0));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[t][x][4 * q + e] = y[e];
+                }
+            } else if constexpr (S::kWords == 2) {
+                const u32x2 y =
+                    __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, o, 0, 0));
+                v[t][x][0] = y[0], v[t][x][1] = y[1];
+            } else {
+                v[t][x][0] = __builtin_amdgcn_raw_buffer_load_b32(r, o, 0, 0);
+            }
+        }
+    }
+};
+
+// A block's probabilities as two bf16 parts.  The first is the next bf16 number below
+// p, so that the second is above 0 where p is and an infinite V stays what it is; it
+// leaves less than 2^-7 of p, of which the second is within 2^-8.
+struct Parts {
+    bf16x8 hi, lo;
+
+    __device__ __forceinline__ explicit Parts(const f32x4 (&p)[2]) {
+        u32x4 high;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            uint32_t u[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float x = p[(e + k) / 4][(e + k) % 4];
+                u[k] = __builtin_elementwise_sub_sat(__float_as_uint(x), 1u);
+                lo[e + k] = (__bf16)(x - __uint_as_float(u[k] & 0xffff0000u));
+            }
+            high[e / 2] = __builtin_amdgcn_perm(u[1], u[0], 0x07060302);
+        }
+        hi = __builtin_bit_cast(bf16x8, high);
+    }
+};
+
+template <typename T, int D, bool SPARSE>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 8)))
+void paged_attn(AttnArgs a) {
+    using S = Shape<T, D>;
+    constexpr int NT = S::kTiles, N = S::kN, RB = S::kRowBytes;
+    constexpr int LD = D + 4;
+    __shared__ __attribute__((aligned(16))) float Os[kWaves][kRows][LD];
+    __shared__ float Ms[kWaves][kRows], Ls[kWaves][kRows];
+
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tile = blockIdx.x % a.tiles, rest = blockIdx.x / a.tiles;
+    const int h = rest % a.H, u = rest / a.H;
+    Unit un;
+    if (a.splits > 0) {
+        const int at = u / a.splits;
+        un.split = u - at * a.splits;
+        un.b = SPARSE ? at / a.Lq : at;
+        un.i = SPARSE ? at - un.b * a.Lq : 0;
+        un.base = at * a.splits;
+        un.splits = a.splits;
+        un.count = a.chunk;
+        un.first = un.split * a.chunk;
+    } else {
+        un = unit_by_length(a, u, lane);
+        if (un.b < 0) return;
+    }
+    const PagedMask mask =
+        paged_mask(a.key_len, a.q_len, un.b, a.P << a.shift, a.Lq, a.causal);
+    if (a.splits > 0 && !SPARSE)   // units behind the sequence's end are none
+        un.splits = max(1, min(a.splits, ((mask.n + 31) / 32 + a.chunk - 1) / a.chunk));
+    if (!SPARSE && a.info != nullptr && h == 0 && tile == 0 && un.split == 0 && tid == 0)
+        a.info[un.b] = make_int2(un.base, un.splits);
+    if (un.split >= un.splits) return;
+
+    // the lane's row, and what the tile's rows see
+    const int rows = SPARSE ? a.G : a.G * a.Lq;
+    const int r = kRows * tile + c;
+    const bool in = r < rows;
+    const int i = SPARSE ? un.i : (in ? r : rows - 1) / a.G;
+    const int head = SPARSE ? min(r, rows - 1) : (in ? r : rows - 1) - i * a.G;
+    const size_t at = ((size_t)(un.b * a.H + h) * a.G + head) * a.Lq + i;   // of [B][Hq][Lq]
+    const bool valid = in && i < mask.rows;
+    const int limit = valid ? mask.limit(i) : 0;
+    const int first_i = SPARSE ? un.i : kRows * tile / a.G;
+    const int last_i =
+        SPARSE ? un.i : min((min(rows, kRows * (tile + 1)) - 1) / a.G, mask.rows - 1);
+    const int all = mask.limit(first_i);   // below: every row sees the token
+    const int end = first_i < mask.rows ? mask.limit(last_i) : 0;
+
+    // the pages: entries pb .. pb + 63 of the table (sparse: of the row's list)
+    const int32_t *table = a.table + (size_t)un.b * a.P;
+    int pb = (32 * un.first) >> a.shift;
+    int stop = min(((SPARSE ? a.keep << a.shift : end) + S::kTok - 1) / S::kTok,
+                   (un.first + un.count) * (32 / S::kTok));
+    const auto entry = [&](int p) { return table[min(p, a.P - 1)]; };
+    int ids, ids_next = 0, place = 0;
+    if constexpr (SPARSE) {
+        const int32_t *list = a.index + (((size_t)un.b * a.H + h) * a.Lq + un.i) * a.keep;
+        const int k = pb + lane;
+        place = k < a.keep ? list[k] : -1;
+        const int before = k > 0 && k <= a.keep ? list[k - 1] : -1;
+        const bool good = place > before && place >= 0 && place < a.P;
+        ids = good ? table[place] : -1;
+        const uint64_t any = __ballot(good);   // nothing is listed behind the last
+        const int listed = any == 0 ? 0 : 64 - __builtin_clzll(any);
+        stop = min(stop, (((pb + listed) << a.shift) + S::kTok - 1) / S::kTok);
+    } else {
+        ids = entry(pb + lane);
+        ids_next = entry(pb + 64 + lane);
+    }
+
+    // where a tile of 16 tokens lies, and its first token (kFar: it is not seen)
+    const char *kp = static_cast<const char *>(a.Kp), *vp = static_cast<const char *>(a.Vp);
+    const size_t head_bytes = (size_t)RB << a.shift;
+    struct Place {
+        size_t at;
+        int token, bytes;
+    };
+    const auto place_of = [&](int block, int t) {
+        const int v = S::kTok * block + 16 * t, rel = (v >> a.shift) - pb;
+        const int row = v & ((1 << a.shift) - 1);
+        int id = __builtin_amdgcn_readlane(ids, rel), token = v;
+        if constexpr (SPARSE) token = (__builtin_amdgcn_readlane(place, rel) << a.shift) + row;
+        if ((uint32_t)id >= (uint32_t)a.N) id = 0, token = kFar;
+        const int left = min(max(end - token, 0), 16);
+        return Place{((size_t)id * a.H + h) * head_bytes + (size_t)row * RB, token, left * RB};
+    };
+
+    Block<T, D> x;
+    Place now[NT], next[NT];
+    const int per = kWaves;
+    const int k_at = c * RB + 16 * g, v_at = 4 * g * RB + (RB / 16 > 16 ? 16 : RB / 16) * c;
+    int block = un.first * (32 / S::kTok) + w;
+    const bool any = block < stop;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        now[t] = any ? place_of(block, t) : Place{0, kFar, 0};
+        x.load_k(t, buffer_rsrc(kp + now[t].at, now[t].bytes), k_at);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) x.load_v(t, buffer_rsrc(vp + now[t].at, now[t].bytes), v_at);
+
+    // (rows behind the sequence's, whatever they hold, are taken as zeros)
+    u32x4 q[S::kPieces];
+#pragma unroll
+    for (int s = 0; s < S::kPieces; ++s)
+        q[s] = valid ? *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.Q) +
+                                                        at * RB + 64 * s + 16 * g)
+                     : u32x4{0, 0, 0, 0};
+
+    float m = -INFINITY, l = 0.f;
+    f32x4 o[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) o[j] = zero4();
+
+    while (block < stop) {
+        f32x4 s[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            s[t] = zero4();
+#pragma unroll
+            for (int y = 0; y < S::kPieces; ++y) {
+                if constexpr (S::kHalf) {
+                    s[t] = mfma16x16x32bf16(__builtin_bit_cast(bf16x8, x.k[t][y]),
+                                            __builtin_bit_cast(bf16x8, q[y]), s[t]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        s[t] = mfma16x16x4(__uint_as_float(x.k[t][y][e]),
+                                           __uint_as_float(q[y][e]), s[t]);
+                }
+            }
+        }
+        // the next block's K comes while this one's scores are worked on (behind
+        // the last block: descriptors of no bytes)
+        const int following = block + per;
+        if (!SPARSE && ((S::kTok * following) >> a.shift) - pb >= 64) {
+            pb += 64;
+            ids = ids_next;
+            ids_next = entry(pb + 64 + lane);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            next[t] = following < stop ? place_of(following, t) : Place{0, kFar, 0};
+            x.load_k(t, buffer_rsrc(kp + next[t].at, next[t].bytes), k_at);
+        }
+
+        bool diagonal = false;   // a token that some rows see and some do not
+        float top = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            s[t] *= a.scale_log2;
+            if (now[t].token + 16 > all) {
+                diagonal |= end > all && now[t].token < end;
+                const int left = limit - now[t].token - 4 * g;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e >= left) s[t][e] = -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, s[t][e]);
+        }
+        top = fmaxf(m, max_over_groups(top));
+        if (__any(top > m)) {
+            const float alpha = m == -INFINITY ? 0.f : exp2_fast(m - top);
+            l *= alpha;
+#pragma unroll
+            for (int j = 0; j < N; ++j) o[j] *= alpha;
+            m = top;
+        }
+        const float from = m == -INFINITY ? 0.f : m;
+        f32x4 p[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                p[t][e] = exp2_fast(s[t][e] - from);
+                l += p[t][e];
+            }
+
+        // O^T += V^T P^T (CUT: with V's tokens from `below` on taken as zeros)
+        const auto product = [&](auto CUT, f32x4 (&to)[N], int below) {
+            const auto value = [&](int t, int y, int word) {
+                if constexpr (!decltype(CUT)::value) return x.v[t][y][word];
+                else return now[t].token + 4 * g + y < below ? x.v[t][y][word] : 0u;
+            };
+            if constexpr (S::kHalf) {
+                const Parts parts(p);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    u32x4 av;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        av[e] = __builtin_amdgcn_perm(value(e / 2, 2 * (e % 2) + 1, j / 2),
+                                                      value(e / 2, 2 * (e % 2), j / 2),
+                                                      j % 2 ? 0x07060302 : 0x05040100);
+                    const bf16x8 vt = __builtin_bit_cast(bf16x8, av);
+                    to[j] = mfma16x16x32bf16(vt, parts.hi, to[j]);
+                    to[j] = mfma16x16x32bf16(vt, parts.lo, to[j]);
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+#pragma unroll
+                        for (int j = 0; j < N; ++j)
+                            to[j] = mfma16x16x4(__uint_as_float(value(t, y, j)), p[t][y], to[j]);
+            }
+        };
+        bool special = false;   // V that is infinite or NaN where not all rows see it
+        if (diagonal) {
+            bool mine = false;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    if (now[t].token + 4 * g + y >= all)
+#pragma unroll
+                        for (int word = 0; word < S::kWords; ++word) {
+                            const uint32_t bits = x.v[t][y][word];
+                            mine |= (bits & 0x7f800000u) == 0x7f800000u;
+                            if (S::kHalf) mine |= (bits & 0x7f80u) == 0x7f80u;
+                        }
+            special = __any(mine);
+        }
+        if (!special) {
+            product(std::false_type(), o, 0);
+        } else {
+            // a product for every limit there is, of which the rows that have it take theirs
+            for (int row = first_i; row <= last_i; ++row) {
+                f32x4 y[N];
+#pragma unroll
+                for (int j = 0; j < N; ++j) y[j] = o[j];
+                product(std::true_type(), y, mask.limit(row));
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        o[j][e] = i == row ? y[j][e] : o[j][e];
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            x.load_v(t, buffer_rsrc(vp + next[t].at, next[t].bytes), v_at);
+            now[t] = next[t];
+        }
+        block = following;
+    }
+
+    // the waves' shares through LDS
+    l = sum_over_groups(l);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < N; ++j) Os[w][c][S::channel(4 * g + e, j)] = o[j][e];
+    if (g == 0) {
+        Ms[w][c] = m;
+        Ls[w][c] = l;
+    }
+    __syncthreads();
+
+    const int row = tid >> 4, d0 = N * (tid & 15), rr = kRows * tile + row;
+    if (rr >= rows) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) top = fmaxf(top, Ms[k][row]);
+    float sum = 0.f, y[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) y[k] = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+        // without a score above -inf the sums are 0, or NaN where a score is
+        const float f = top == -INFINITY ? 1.f : exp2_fast(Ms[k][row] - top);
+        sum = fmaf(f, Ls[k][row], sum);
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = fmaf(f, Os[k][row][d0 + e], y[e]);
+    }
+    const int ri = SPARSE ? un.i : rr / a.G, rh = SPARSE ? rr : rr - ri * a.G;
+    const size_t to = ((size_t)(un.b * a.H + h) * a.G + rh) * a.Lq + ri;
+    const bool live = ri < mask.rows;
+    if (un.splits > 1) {
+        const size_t slot = ((size_t)u * a.H + h) * rows + rr;
+        float *p = a.part + slot * D + d0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) p[e] = live ? y[e] : 0.f;
+        if (d0 == 0) a.stat[slot] = live ? make_float2(top, sum) : make_float2(-INFINITY, 0.f);
+        return;
+    }
+    if (!live) sum = 0.f;
+    const float inv = 1.f / sum;
+#pragma unroll
+    for (int e = 0; e < N; ++e) y[e] = sum == 0.f ? 0.f : y[e] * inv;
+    T *out = static_cast<T *>(a.O) + to * D + d0;
+    if constexpr (N >= 4) {
+        store_row(out, y);
+    } else if constexpr (S::kHalf) {
+        *reinterpret_cast<uint32_t *>(out) = to_bf16(y[0]) | (uint32_t)to_bf16(y[1]) << 16;
+    } else {
+        *reinterpret_cast<f32x2 *>(out) = f32x2{y[0], y[1]};
+    }
+    if (d0 == 0) a.LSE[to] = sum != sum ? sum : row_lse(top, sum);
+}
+
+// ------------------------------------------------------------------- joining --
+struct JoinArgs {
+    void *O;
+    float *LSE;
+    const float *part;
+    const float2 *stat;
+    const int2 *info;   // nullptr: every sequence (row) has `splits` units
+    int H, G, Lq, rows, splits, total;
+};
+
+// WAVES waves join a row.  Lanes in teams of D / 4, four channels each, take the
+// units in turn; the maximum comes first, a unit a lane.
+template <typename T, int D, int WAVES>
+__global__ __launch_bounds__(kThreads)
+void paged_join(JoinArgs a) {
+    constexpr int TEAMS = 256 / D;
+    __shared__ float tops[kWaves];
+    __shared__ __attribute__((aligned(16))) float Ys[kWaves][D];
+    __shared__ float Sums[kWaves];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int wave = WAVES == 1 ? 0 : w;
+    const int id = WAVES == 1 ? blockIdx.x * kWaves + w : blockIdx.x;
+    if (id >= a.total) return;   // (a whole workgroup where several waves join a row)
+    const int r = id % a.rows, rest = id / a.rows;
+    const int h = rest % a.H, seq = rest / a.H;   // sequence, or sparse its row
+    const int2 in = a.info ? a.info[seq] : make_int2(seq * a.splits, a.splits);
+    if (in.y <= 1) return;
+    const auto slot = [&](int k) { return ((size_t)(in.x + k) * a.H + h) * a.rows + r; };
+
+    float top = -INFINITY;
+    for (int k = 64 * wave + lane; k < in.y; k += 64 * WAVES) top = fmaxf(top, a.stat[slot(k)].x);
+    top = max_xor32(max_xor16(max_of<16>(top)));
+    if constexpr (WAVES > 1) {
+        if (lane == 0) tops[w] = top;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) top = fmaxf(top, tops[k]);
+    }
+    // four units at a time, so that their reads are on the way together
+    const int team = lane / (D / 4), d0 = 4 * (lane % (D / 4));
+    constexpr int STEP = TEAMS * WAVES;
+    f32x4 x = zero4();
+    float sum = 0.f;
+    for (int k = wave * TEAMS + team; k < in.y; k += 4 * STEP) {
+        f32x4 y[4];
+        float2 st[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const size_t at = slot(min(k + e * STEP, in.y - 1));
+            st[e] = a.stat[at];
+            y[e] = *reinterpret_cast<const f32x4 *>(a.part + at * D + d0);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (k + e * STEP >= in.y) continue;
+            const float f = top == -INFINITY ? 1.f : exp2_fast(st[e].x - top);
+            sum = fmaf(f, st[e].y, sum);
+            x += f * y[e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (TEAMS >= 2) x[e] = sum_xor32(x[e]);
+        if (TEAMS >= 4) x[e] = sum_xor16(x[e]);
+        if (TEAMS >= 8) x[e] += xor_lanes(x[e], 8);
+    }
+    if (TEAMS >= 2) sum = sum_xor32(sum);
+    if (TEAMS >= 4) sum = sum_xor16(sum);
+    if (TEAMS >= 8) sum += xor_lanes(sum, 8);
+    if constexpr (WAVES > 1) {
+        if (team == 0) *reinterpret_cast<f32x4 *>(&Ys[w][d0]) = x;
+        if (lane == 0) Sums[w] = sum;
+        __syncthreads();
+        if (w != 0) return;
+        x = zero4();
+        sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) {
+            x += *reinterpret_cast<const f32x4 *>(&Ys[k][d0]);
+            sum += Sums[k];
+        }
+    }
+    // dense: rows r = i G + g of the sequence; sparse: head r of row seq % Lq
+    const bool sparse = a.info == nullptr;
+    const int b = sparse ? seq / a.Lq : seq;
+    const int i = sparse ? seq - b * a.Lq : r / a.G, hd = sparse ? r : r - i * a.G;
+    const size_t to = ((size_t)(b * a.H + h) * a.G + hd) * a.Lq + i;
+    if (team == 0) {
+        const float inv = 1.f / sum;
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = sum == 0.f ? 0.f : x[e] * inv;
+        store_row(static_cast<T *>(a.O) + to * D + d0, y);
+    }
+    if (lane == 0) a.LSE[to] = sum != sum ? sum : row_lse(top, sum);
+}
+
+template <typename T, int D>
+hipError_t attn(const PagedAttn &p, const PagedPlan &plan, const void *Q, const void *Kp,
+                const void *Vp, void *O, float *LSE, char *ws, hipStream_t s) {
+    const AttnArgs a = {Q, Kp, Vp, O, LSE, (float *)(ws + plan.part), (float2 *)(ws + plan.stat),
+                        plan.most > 1 ? (int2 *)(ws + plan.info) : nullptr, p.table, p.index, p.key_len, p.q_len,
+                        p.B, p.H, p.G, p.Lq, p.P, p.N, p.shift, p.causal, p.keep,
+                        p.scale * kLog2e, plan.splits, plan.chunk, plan.share, plan.tiles};
+    const unsigned grid = (unsigned)((int64_t)plan.units * p.H * plan.tiles);
+    if (p.index != nullptr) paged_attn<T, D, true><<<grid, kThreads, 0, s>>>(a);
+    else paged_attn<T, D, false><<<grid, kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t join(const PagedAttn &p, const PagedPlan &plan, void *O, float *LSE, const char *ws,
+                hipStream_t s) {
+    const bool sparse = p.index != nullptr;
+    const int rows = (int)paged_rows(p, sparse);
+    const int64_t total = (int64_t)p.B * (sparse ? p.Lq : 1) * p.H * rows;
+    const JoinArgs a = {O, LSE, (const float *)(ws + plan.part), (const float2 *)(ws + plan.stat),
+                        sparse ? nullptr : (const int2 *)(ws + plan.info), p.H, p.G, p.Lq, rows,
+                        plan.splits, (int)total};
+    if (plan.most <= 64)
+        paged_join<T, D, 1><<<(unsigned)((total + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
+    else
+        paged_join<T, D, kWaves><<<(unsigned)total, kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_attn(const PagedAttn &p, const PagedPlan &plan, const void *Q,
+                             const void *Kp, const void *Vp, bool bf16, void *O, float *LSE,
+                             void *ws, hipStream_t s) {
+    char *w = static_cast<char *>(ws);
+    if (bf16)
+        return p.d == 32 ? attn<uint16_t, 32>(p, plan, Q, Kp, Vp, O, LSE, w, s)
+             : p.d == 64 ? attn<uint16_t, 64>(p, plan, Q, Kp, Vp, O, LSE, w, s)
+                         : attn<uint16_t, 128>(p, plan, Q, Kp, Vp, O, LSE, w, s);
+    return p.d == 32 ? attn<float, 32>(p, plan, Q, Kp, Vp, O, LSE, w, s)
+         : p.d == 64 ? attn<float, 64>(p, plan, Q, Kp, Vp, O, LSE, w, s)
+                     : attn<float, 128>(p, plan, Q, Kp, Vp, O, LSE, w, s);
+}
+
+hipError_t launch_paged_join(const PagedAttn &p, const PagedPlan &plan, bool bf16, void *O,
+                             float *LSE, const void *ws, hipStream_t s) {
+    const char *w = static_cast<const char *>(ws);
+    if (bf16)
+        return p.d == 32 ? join<uint16_t, 32>(p, plan, O, LSE, w, s)
+             : p.d == 64 ? join<uint16_t, 64>(p, plan, O, LSE, w, s)
+                         : join<uint16_t, 128>(p, plan, O, LSE, w, s);
+    return p.d == 32 ? join<float, 32>(p, plan, O, LSE, w, s)
+         : p.d == 64 ? join<float, 64>(p, plan, O, LSE, w, s)
+                     : join<float, 128>(p, plan, O, LSE, w, s);
+}
+
+}  // namespace mg
