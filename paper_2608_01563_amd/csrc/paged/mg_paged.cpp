@@ -16,6 +16,7 @@ namespace mg {
 namespace {
 constexpr int kWant = 1024;       // workgroups that a call is cut into
 constexpr int kLeast = 8;         // blocks of a unit
+constexpr int64_t kCached = 256 << 20;   // bytes that the last cache holds
 constexpr int kLongest = 1 << 13; // blocks of a unit (2^18 tokens)
 
 void paged_workspace(PagedPlan &plan, const PagedAttn &p, int64_t rows) {
@@ -31,9 +32,13 @@ void paged_workspace(PagedPlan &plan, const PagedAttn &p, int64_t rows) {
 PagedPlan paged_plan(const PagedAttn &p, bool sparse) {
     PagedPlan plan = {};
     const int64_t rows = paged_rows(p, sparse);
-    plan.tiles = (int)((rows + 15) / 16);
-    const int64_t groups = (int64_t)p.H * plan.tiles;   // workgroups of a unit
+    const int64_t tiles = (rows + 15) / 16;
+    plan.wide = tiles == 1 ? 1 : tiles == 2 ? 2 : 4;
+    plan.tile_groups = (int)((tiles + plan.wide - 1) / plan.wide);
+    const int64_t groups = (int64_t)p.H * plan.tile_groups;   // workgroups of a unit
     const int64_t cut = std::max<int64_t>(1, kWant / groups);
+    const int64_t pages = std::min<int64_t>(p.N, (int64_t)p.B * (sparse ? p.Lq * p.keep : p.P));
+    plan.once = (pages << p.shift) * p.H * p.d * (p.half ? 4 : 8) > kCached;
     if (sparse) {
         // lists are short of their `keep` pages only where sequences are: all alike.
         // A unit has at most 64 pages, whose entries a wave holds.
@@ -168,7 +173,7 @@ mg_status_t check_attn(const mg::PagedAttn &p, int Hq, int page, bool sparse,
     if (!std::isfinite(p.scale * kLog2e))
         return fail(MG_ERR_INVALID_ARGUMENT, "scale log2 e is not finite (scale %g)", p.scale);
     *plan = mg::paged_plan(p, sparse);
-    if ((int64_t)plan->units * p.H * plan->tiles > kMaxGroups)
+    if ((int64_t)plan->units * p.H * plan->tile_groups > kMaxGroups)
         return fail(MG_ERR_INVALID_ARGUMENT, "too much work for one call (B=%d H=%d Lq=%d P=%d)",
                     p.B, p.H, p.Lq, p.P);
     return MG_OK;
@@ -176,9 +181,9 @@ mg_status_t check_attn(const mg::PagedAttn &p, int Hq, int page, bool sparse,
 
 mg::PagedAttn attn_of(int B, int Hq, int H, int Lq, int d, int page, int P, int N, int causal,
                       int keep, float scale, const int32_t *table, const int32_t *index,
-                      const int32_t *key_len, const int32_t *q_len) {
-    return {B, H, H > 0 ? Hq / H : 0, Lq, d, shift_of(page), P, N, causal != 0, keep, scale,
-            table, index, key_len, q_len};
+                      const int32_t *key_len, const int32_t *q_len, mg_contract_t contract) {
+    return {B, H, H > 0 ? Hq / H : 0, Lq, d, shift_of(page), P, N, causal != 0, keep,
+            contract == MG_CONTRACT_FAST_BF16, scale, table, index, key_len, q_len};
 }
 
 mg_status_t attn_call(const mg::PagedAttn &p, int Hq, int page, bool sparse, const void *Q,
@@ -189,17 +194,20 @@ mg_status_t attn_call(const mg::PagedAttn &p, int Hq, int page, bool sparse, con
     if (plan.bytes > 0 && (workspace == nullptr || workspace_bytes < plan.bytes))
         return fail(MG_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed",
                     workspace ? workspace_bytes : (size_t)0, plan.bytes);
-    const void *index = sparse ? p.index : p.table, *ws = plan.bytes > 0 ? workspace : O;
-    MG_TRY(check_ptrs({{Q, "Q"}, {Kp, "Kp"}, {Vp, "Vp"}, {O, "O"}, {LSE, "LSE"}, {ws, "workspace"}},
-                      {{p.table, "table"}, {index, "index"}, {p.key_len, "key_len"}},
-                      {{p.q_len, "q_len"}}, 4));
-    const bool bf16 = contract == MG_CONTRACT_FAST_BF16;
+    const void *ws = plan.bytes > 0 ? workspace : nullptr;
+    if (reinterpret_cast<uintptr_t>(ws) % 16 != 0)
+        return fail(MG_ERR_MISALIGNED, "workspace is not 16-byte aligned");
+    if (sparse && p.index == nullptr) return fail(MG_ERR_INVALID_ARGUMENT, "index is NULL");
+    MG_TRY(check_ptrs({{Q, "Q"}, {Kp, "Kp"}, {Vp, "Vp"}, {O, "O"}, {LSE, "LSE"}},
+                      {{p.table, "table"}, {p.key_len, "key_len"}},
+                      {{p.q_len, "q_len"}, {sparse ? p.index : nullptr, "index"},
+                       {ws, "workspace"}}, 4));
     MG_TRY(run_kernel("paged_attn", stream, [&] {
-        return mg::launch_paged_attn(p, plan, Q, Kp, Vp, bf16, O, LSE, workspace, stream);
+        return mg::launch_paged_attn(p, plan, Q, Kp, Vp, O, LSE, workspace, stream);
     }));
     if (plan.most > 1)
         MG_TRY(run_kernel("paged_join", stream, [&] {
-            return mg::launch_paged_join(p, plan, bf16, O, LSE, workspace, stream);
+            return mg::launch_paged_join(p, plan, O, LSE, workspace, stream);
         }));
     return ok();
 }
@@ -302,7 +310,7 @@ size_t mg_attn_fwd_paged_workspace_bytes(int B, int Hq, int H, int Lq, int d, in
     return asked([&]() -> size_t {
         mg::PagedPlan plan;
         const mg::PagedAttn p = attn_of(B, Hq, H, Lq, d, page, P, 1, 1, 0, 1.f, nullptr, nullptr,
-                                        nullptr, nullptr);
+                                        nullptr, nullptr, contract);
         return check_attn(p, Hq, page, false, contract, &plan) == MG_OK ? plan.bytes : 0;
     });
 }
@@ -313,7 +321,7 @@ mg_status_t mg_attn_fwd_paged(const void *Q, const void *Kp, const void *Vp, voi
                               int causal, float scale, mg_contract_t contract, void *workspace,
                               size_t workspace_bytes, hipStream_t stream) {
     const mg::PagedAttn p = attn_of(B, Hq, H, Lq, d, page, P, N, causal, 0, scale, table, nullptr,
-                                    key_len, q_len);
+                                    key_len, q_len, contract);
     return attn_call(p, Hq, page, false, Q, Kp, Vp, O, LSE, contract, workspace, workspace_bytes,
                      stream);
 }
@@ -323,7 +331,7 @@ size_t mg_attn_fwd_paged_sparse_workspace_bytes(int B, int Hq, int H, int Lq, in
     return asked([&]() -> size_t {
         mg::PagedPlan plan;
         const mg::PagedAttn p = attn_of(B, Hq, H, Lq, d, page, 1, 1, 1, keep, 1.f, nullptr, nullptr,
-                                        nullptr, nullptr);
+                                        nullptr, nullptr, contract);
         return check_attn(p, Hq, page, true, contract, &plan) == MG_OK ? plan.bytes : 0;
     });
 }
@@ -335,7 +343,7 @@ mg_status_t mg_attn_fwd_paged_sparse(const void *Q, const void *Kp, const void *
                                      int keep, float scale, mg_contract_t contract,
                                      void *workspace, size_t workspace_bytes, hipStream_t stream) {
     const mg::PagedAttn p = attn_of(B, Hq, H, Lq, d, page, P, N, causal, keep, scale, table, index,
-                                    key_len, q_len);
+                                    key_len, q_len, contract);
     return attn_call(p, Hq, page, true, Q, Kp, Vp, O, LSE, contract, workspace, workspace_bytes,
                      stream);
 }

@@ -31,6 +31,8 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kRows = 16;
+constexpr int kOnce = 2;   // cache policy: non-temporal
+constexpr uint32_t kShort = 20;   // blocks of a unit
 constexpr int kFar = 1 << 30;   // a token that no row sees
 
 struct AttnArgs {
@@ -42,7 +44,7 @@ struct AttnArgs {
     const int32_t *table, *index, *key_len, *q_len;
     int B, H, G, Lq, P, N, shift, causal, keep;
     float scale_log2;
-    int splits, chunk, share, tiles;
+    int splits, chunk, share, tile_groups;
 };
 
 // One unit: blocks [first, first + count) of sequence b (sparse: of row i's list);
@@ -53,7 +55,11 @@ struct Unit {
 
 // Which sequence unit u belongs to where lengths decide: every sequence is cut
 // into units of `chunk` blocks (at least one unit each), chunk so that all lengths
-// together make about `share` units.
+// together make about `share` units, or half of them where these are short: a
+// workgroup on every slot the GPU has and no second round (8 sequences of 2,500
+// tokens, 8 heads, 28 rows: 22 us with 448 workgroups of 12 blocks, 29 with 640 of
+// 8); long ones are better evened out by two rounds (32 sequences of 2,560 tokens,
+// 8 heads: 62 us with units of 20 blocks, 72 with 40).
 __device__ __forceinline__ Unit unit_by_length(const AttnArgs &a, int u, int lane) {
     const int capacity = a.P << a.shift;
     const auto blocks_of = [&](int b) {
@@ -64,13 +70,14 @@ __device__ __forceinline__ Unit unit_by_length(const AttnArgs &a, int u, int lan
     for (int b = 64 + lane; b < a.B + lane; b += 64) total += blocks_of(b);
     total = wave_sum(total);
     uint32_t chunk = (total + a.share - 1) / a.share;
+    if (2 * chunk <= kShort) chunk = (2 * total + a.share - 1) / a.share;
     chunk = min(max((chunk + kWaves - 1) / kWaves * kWaves, (uint32_t)a.chunk), 1u << 13);
     Unit r = {-1, 0, 0, (int)chunk, 0, 0, 0};
     uint32_t carry = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
         const uint32_t n = b0 == 0 ? mine : blocks_of(b0 + lane);
         const uint32_t parts = b0 + lane < a.B ? max((n + chunk - 1) / chunk, 1u) : 0u;
-        const uint32_t end = wave_scan(parts, lane);
+        const uint32_t end = wave_scan(parts);
         const uint64_t past = __ballot(carry + end > (uint32_t)u);
         if (past != 0) {
             const int at = __builtin_ctzll(past);
@@ -103,7 +110,7 @@ struct Shape {
 };
 
 // A block's K pieces and V words.
-template <typename T, int D>
+template <typename T, int D, int CACHE>
 struct Block {
     using S = Shape<T, D>;
     u32x4 k[S::kTiles][S::kPieces];
@@ -113,7 +120,7 @@ struct Block {
 #pragma unroll
         for (int s = 0; s < S::kPieces; ++s)
             k[t][s] = __builtin_bit_cast(
-                u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at + 64 * s, 0, 0));
+                u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at + 64 * s, 0, CACHE));
     }
     __device__ __forceinline__ void load_v(int t, __amdgpu_buffer_rsrc_t r, int at) {
 #pragma unroll
@@ -123,28 +130,39 @@ struct Block {
 #pragma unroll
                 for (int q = 0; q < S::kWords / 4; ++q) {
                     const u32x4 y = __builtin_bit_cast(
-                        u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, o + 256 * q, 0, 0));
+                        u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, o + 256 * q, 0, CACHE));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[t][x][4 * q + e] = y[e];
                 }
             } else if constexpr (S::kWords == 2) {
                 const u32x2 y =
-                    __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, o, 0, 0));
+                    __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, o, 0, CACHE));
                 v[t][x][0] = y[0], v[t][x][1] = y[1];
             } else {
-                v[t][x][0] = __builtin_amdgcn_raw_buffer_load_b32(r, o, 0, 0);
+                v[t][x][0] = __builtin_amdgcn_raw_buffer_load_b32(r, o, 0, CACHE);
             }
         }
     }
 };
 
-// A block's probabilities as two bf16 parts.  The first is the next bf16 number below
-// p, so that the second is above 0 where p is and an infinite V stays what it is; it
-// leaves less than 2^-7 of p, of which the second is within 2^-8.
-struct Parts {
+// A block's probabilities as the second product's operand: f32, or two bf16 parts.
+// The first part is the next bf16 number below p, so that the second is above 0 where
+// p is and an infinite V stays what it is; it leaves less than 2^-7 of p, of which the
+// second is within 2^-8.
+template <typename T, int D>
+struct Operand {
+    f32x4 p[Shape<T, D>::kTiles];
+
+    __device__ __forceinline__ explicit Operand(const f32x4 (&x)[Shape<T, D>::kTiles]) {
+#pragma unroll
+        for (int t = 0; t < Shape<T, D>::kTiles; ++t) p[t] = x[t];
+    }
+};
+template <int D>
+struct Operand<uint16_t, D> {
     bf16x8 hi, lo;
 
-    __device__ __forceinline__ explicit Parts(const f32x4 (&p)[2]) {
+    __device__ __forceinline__ explicit Operand(const f32x4 (&p)[2]) {
         u32x4 high;
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
@@ -161,19 +179,19 @@ struct Parts {
     }
 };
 
-template <typename T, int D, bool SPARSE>
+template <typename T, int D, bool SPARSE, int TW, int CACHE>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 8)))
 void paged_attn(AttnArgs a) {
     using S = Shape<T, D>;
     constexpr int NT = S::kTiles, N = S::kN, RB = S::kRowBytes;
-    constexpr int LD = D + 4;
+    constexpr int LD = D + 4, WV = kWaves / TW;   // waves a tile
     __shared__ __attribute__((aligned(16))) float Os[kWaves][kRows][LD];
     __shared__ float Ms[kWaves][kRows], Ls[kWaves][kRows];
 
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int tile = blockIdx.x % a.tiles, rest = blockIdx.x / a.tiles;
-    const int h = rest % a.H, u = rest / a.H;
+    const int tiles0 = blockIdx.x % a.tile_groups, rest = blockIdx.x / a.tile_groups;
+    const int h = rest % a.H, u = rest / a.H, tile = tiles0 * TW + w % TW;
     Unit un;
     if (a.splits > 0) {
         const int at = u / a.splits;
@@ -192,7 +210,7 @@ void paged_attn(AttnArgs a) {
         paged_mask(a.key_len, a.q_len, un.b, a.P << a.shift, a.Lq, a.causal);
     if (a.splits > 0 && !SPARSE)   // units behind the sequence's end are none
         un.splits = max(1, min(a.splits, ((mask.n + 31) / 32 + a.chunk - 1) / a.chunk));
-    if (!SPARSE && a.info != nullptr && h == 0 && tile == 0 && un.split == 0 && tid == 0)
+    if (!SPARSE && a.info != nullptr && h == 0 && tiles0 == 0 && un.split == 0 && tid == 0)
         a.info[un.b] = make_int2(un.base, un.splits);
     if (un.split >= un.splits) return;
 
@@ -208,8 +226,9 @@ void paged_attn(AttnArgs a) {
     const int first_i = SPARSE ? un.i : kRows * tile / a.G;
     const int last_i =
         SPARSE ? un.i : min((min(rows, kRows * (tile + 1)) - 1) / a.G, mask.rows - 1);
-    const int all = mask.limit(first_i);   // below: every row sees the token
-    const int end = first_i < mask.rows ? mask.limit(last_i) : 0;
+    const bool some = kRows * tile < rows && first_i < mask.rows;
+    const int all = some ? mask.limit(first_i) : 0;   // below: every row sees the token
+    const int end = some ? mask.limit(last_i) : 0;
 
     // the pages: entries pb .. pb + 63 of the table (sparse: of the row's list)
     const int32_t *table = a.table + (size_t)un.b * a.P;
@@ -250,11 +269,10 @@ void paged_attn(AttnArgs a) {
         return Place{((size_t)id * a.H + h) * head_bytes + (size_t)row * RB, token, left * RB};
     };
 
-    Block<T, D> x;
+    Block<T, D, CACHE> x;
     Place now[NT], next[NT];
-    const int per = kWaves;
     const int k_at = c * RB + 16 * g, v_at = 4 * g * RB + (RB / 16 > 16 ? 16 : RB / 16) * c;
-    int block = un.first * (32 / S::kTok) + w;
+    int block = un.first * (32 / S::kTok) + w / TW;
     const bool any = block < stop;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -297,7 +315,7 @@ void paged_attn(AttnArgs a) {
         }
         // the next block's K comes while this one's scores are worked on (behind
         // the last block: descriptors of no bytes)
-        const int following = block + per;
+        const int following = block + WV;
         if (!SPARSE && ((S::kTok * following) >> a.shift) - pb >= 64) {
             pb += 64;
             ids = ids_next;
@@ -342,34 +360,31 @@ void paged_attn(AttnArgs a) {
                 l += p[t][e];
             }
 
-        // O^T += V^T P^T (CUT: with V's tokens from `below` on taken as zeros)
-        const auto product = [&](auto CUT, f32x4 (&to)[N], int below) {
+        // Channel block j of O^T += V^T P^T (CUT: with V's tokens from `below` on taken
+        // as zeros)
+        const Operand<T, D> operand(p);
+        const auto product = [&](auto CUT, int j, f32x4 to, int below) {
             const auto value = [&](int t, int y, int word) {
                 if constexpr (!decltype(CUT)::value) return x.v[t][y][word];
                 else return now[t].token + 4 * g + y < below ? x.v[t][y][word] : 0u;
             };
             if constexpr (S::kHalf) {
-                const Parts parts(p);
+                u32x4 av;
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    u32x4 av;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        av[e] = __builtin_amdgcn_perm(value(e / 2, 2 * (e % 2) + 1, j / 2),
-                                                      value(e / 2, 2 * (e % 2), j / 2),
-                                                      j % 2 ? 0x07060302 : 0x05040100);
-                    const bf16x8 vt = __builtin_bit_cast(bf16x8, av);
-                    to[j] = mfma16x16x32bf16(vt, parts.hi, to[j]);
-                    to[j] = mfma16x16x32bf16(vt, parts.lo, to[j]);
-                }
+                for (int e = 0; e < 4; ++e)
+                    av[e] = __builtin_amdgcn_perm(value(e / 2, 2 * (e % 2) + 1, j / 2),
+                                                  value(e / 2, 2 * (e % 2), j / 2),
+                                                  j % 2 ? 0x07060302 : 0x05040100);
+                const bf16x8 vt = __builtin_bit_cast(bf16x8, av);
+                to = mfma16x16x32bf16(vt, operand.hi, to);
+                return mfma16x16x32bf16(vt, operand.lo, to);
             } else {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int y = 0; y < 4; ++y)
-#pragma unroll
-                        for (int j = 0; j < N; ++j)
-                            to[j] = mfma16x16x4(__uint_as_float(value(t, y, j)), p[t][y], to[j]);
+                        to = mfma16x16x4(__uint_as_float(value(t, y, j)), operand.p[t][y], to);
+                return to;
             }
         };
         bool special = false;   // V that is infinite or NaN where not all rows see it
@@ -389,19 +404,19 @@ void paged_attn(AttnArgs a) {
             special = __any(mine);
         }
         if (!special) {
-            product(std::false_type(), o, 0);
+#pragma unroll
+            for (int j = 0; j < N; ++j) o[j] = product(std::false_type(), j, o[j], 0);
         } else {
             // a product for every limit there is, of which the rows that have it take theirs
-            for (int row = first_i; row <= last_i; ++row) {
-                f32x4 y[N];
 #pragma unroll
-                for (int j = 0; j < N; ++j) y[j] = o[j];
-                product(std::true_type(), y, mask.limit(row));
+            for (int j = 0; j < N; ++j) {
+                f32x4 sum = o[j];
+                for (int row = first_i; row <= last_i; ++row) {
+                    const f32x4 y = product(std::true_type(), j, o[j], mask.limit(row));
 #pragma unroll
-                for (int j = 0; j < N; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        o[j][e] = i == row ? y[j][e] : o[j][e];
+                    for (int e = 0; e < 4; ++e) sum[e] = i == row ? y[e] : sum[e];
+                }
+                o[j] = sum;
             }
         }
 #pragma unroll
@@ -424,46 +439,50 @@ void paged_attn(AttnArgs a) {
     }
     __syncthreads();
 
-    const int row = tid >> 4, d0 = N * (tid & 15), rr = kRows * tile + row;
-    if (rr >= rows) return;
-    float top = -INFINITY;
+    const int row = tid >> 4, d0 = N * (tid & 15);
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) top = fmaxf(top, Ms[k][row]);
-    float sum = 0.f, y[N];
+    for (int part = 0; part < TW; ++part) {
+        const int rr = kRows * (tiles0 * TW + part) + row;
+        if (rr >= rows) return;
+        float top = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < N; ++k) y[k] = 0.f;
+        for (int k = part; k < kWaves; k += TW) top = fmaxf(top, Ms[k][row]);
+        float sum = 0.f, y[N];
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) {
-        // without a score above -inf the sums are 0, or NaN where a score is
-        const float f = top == -INFINITY ? 1.f : exp2_fast(Ms[k][row] - top);
-        sum = fmaf(f, Ls[k][row], sum);
+        for (int k = 0; k < N; ++k) y[k] = 0.f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) y[e] = fmaf(f, Os[k][row][d0 + e], y[e]);
+        for (int k = part; k < kWaves; k += TW) {
+            // without a score above -inf the sums are 0, or NaN where a score is
+            const float f = top == -INFINITY ? 1.f : exp2_fast(Ms[k][row] - top);
+            sum = fmaf(f, Ls[k][row], sum);
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] = fmaf(f, Os[k][row][d0 + e], y[e]);
+        }
+        const int ri = SPARSE ? un.i : rr / a.G, rh = SPARSE ? rr : rr - ri * a.G;
+        const size_t to = ((size_t)(un.b * a.H + h) * a.G + rh) * a.Lq + ri;
+        const bool live = ri < mask.rows;
+        if (un.splits > 1) {
+            const size_t slot = ((size_t)u * a.H + h) * rows + rr;
+            float *p = a.part + slot * D + d0;
+#pragma unroll
+            for (int e = 0; e < N; ++e) p[e] = live ? y[e] : 0.f;
+            if (d0 == 0) a.stat[slot] = live ? make_float2(top, sum) : make_float2(-INFINITY, 0.f);
+            continue;
+        }
+        if (!live) sum = 0.f;
+        const float inv = 1.f / sum;
+#pragma unroll
+        for (int e = 0; e < N; ++e) y[e] = sum == 0.f ? 0.f : y[e] * inv;
+        T *out = static_cast<T *>(a.O) + to * D + d0;
+        if constexpr (N >= 4) {
+            store_row(out, y);
+        } else if constexpr (S::kHalf) {
+            *reinterpret_cast<uint32_t *>(out) = to_bf16(y[0]) | (uint32_t)to_bf16(y[1]) << 16;
+        } else {
+            *reinterpret_cast<f32x2 *>(out) = f32x2{y[0], y[1]};
+        }
+        if (d0 == 0) a.LSE[to] = sum != sum ? sum : row_lse(top, sum);
     }
-    const int ri = SPARSE ? un.i : rr / a.G, rh = SPARSE ? rr : rr - ri * a.G;
-    const size_t to = ((size_t)(un.b * a.H + h) * a.G + rh) * a.Lq + ri;
-    const bool live = ri < mask.rows;
-    if (un.splits > 1) {
-        const size_t slot = ((size_t)u * a.H + h) * rows + rr;
-        float *p = a.part + slot * D + d0;
-#pragma unroll
-        for (int e = 0; e < N; ++e) p[e] = live ? y[e] : 0.f;
-        if (d0 == 0) a.stat[slot] = live ? make_float2(top, sum) : make_float2(-INFINITY, 0.f);
-        return;
-    }
-    if (!live) sum = 0.f;
-    const float inv = 1.f / sum;
-#pragma unroll
-    for (int e = 0; e < N; ++e) y[e] = sum == 0.f ? 0.f : y[e] * inv;
-    T *out = static_cast<T *>(a.O) + to * D + d0;
-    if constexpr (N >= 4) {
-        store_row(out, y);
-    } else if constexpr (S::kHalf) {
-        *reinterpret_cast<uint32_t *>(out) = to_bf16(y[0]) | (uint32_t)to_bf16(y[1]) << 16;
-    } else {
-        *reinterpret_cast<f32x2 *>(out) = f32x2{y[0], y[1]};
-    }
-    if (d0 == 0) a.LSE[to] = sum != sum ? sum : row_lse(top, sum);
 }
 
 // ------------------------------------------------------------------- joining --
@@ -495,6 +514,22 @@ void paged_join(JoinArgs a) {
     if (in.y <= 1) return;
     const auto slot = [&](int k) { return ((size_t)(in.x + k) * a.H + h) * a.rows + r; };
 
+    // four units at a time, so that their reads are on the way together (the first ones
+    // beside the maxima's; past the end the last unit again, unused)
+    const int team = lane / (D / 4), d0 = 4 * (lane % (D / 4));
+    constexpr int STEP = TEAMS * WAVES;
+    f32x4 y[4];
+    float2 st[4];
+    const auto read = [&](int k) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const size_t at = slot(min(k + e * STEP, in.y - 1));
+            st[e] = a.stat[at];
+            y[e] = *reinterpret_cast<const f32x4 *>(a.part + at * D + d0);
+        }
+    };
+    const int k0 = wave * TEAMS + team;
+    read(k0);
     float top = -INFINITY;
     for (int k = 64 * wave + lane; k < in.y; k += 64 * WAVES) top = fmaxf(top, a.stat[slot(k)].x);
     top = max_xor32(max_xor16(max_of<16>(top)));
@@ -504,20 +539,9 @@ void paged_join(JoinArgs a) {
 #pragma unroll
         for (int k = 0; k < WAVES; ++k) top = fmaxf(top, tops[k]);
     }
-    // four units at a time, so that their reads are on the way together
-    const int team = lane / (D / 4), d0 = 4 * (lane % (D / 4));
-    constexpr int STEP = TEAMS * WAVES;
     f32x4 x = zero4();
     float sum = 0.f;
-    for (int k = wave * TEAMS + team; k < in.y; k += 4 * STEP) {
-        f32x4 y[4];
-        float2 st[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const size_t at = slot(min(k + e * STEP, in.y - 1));
-            st[e] = a.stat[at];
-            y[e] = *reinterpret_cast<const f32x4 *>(a.part + at * D + d0);
-        }
+    for (int k = k0; k < in.y; k += 4 * STEP) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (k + e * STEP >= in.y) continue;
@@ -525,6 +549,7 @@ void paged_join(JoinArgs a) {
             sum = fmaf(f, st[e].y, sum);
             x += f * y[e];
         }
+        if (k + 4 * STEP < in.y) read(k + 4 * STEP);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -569,11 +594,22 @@ hipError_t attn(const PagedAttn &p, const PagedPlan &plan, const void *Q, const 
     const AttnArgs a = {Q, Kp, Vp, O, LSE, (float *)(ws + plan.part), (float2 *)(ws + plan.stat),
                         plan.most > 1 ? (int2 *)(ws + plan.info) : nullptr, p.table, p.index, p.key_len, p.q_len,
                         p.B, p.H, p.G, p.Lq, p.P, p.N, p.shift, p.causal, p.keep,
-                        p.scale * kLog2e, plan.splits, plan.chunk, plan.share, plan.tiles};
-    const unsigned grid = (unsigned)((int64_t)plan.units * p.H * plan.tiles);
-    if (p.index != nullptr) paged_attn<T, D, true><<<grid, kThreads, 0, s>>>(a);
-    else paged_attn<T, D, false><<<grid, kThreads, 0, s>>>(a);
-    return hipGetLastError();
+                        p.scale * kLog2e, plan.splits, plan.chunk, plan.share, plan.tile_groups};
+    const unsigned grid = (unsigned)((int64_t)plan.units * p.H * plan.tile_groups);
+    const auto run = [&](auto SPARSE, auto TW, auto CACHE) {
+        paged_attn<T, D, decltype(SPARSE)::value, decltype(TW)::value, decltype(CACHE)::value>
+            <<<grid, kThreads, 0, s>>>(a);
+        return hipGetLastError();
+    };
+    const auto tiles = [&](auto SPARSE) {
+        const std::integral_constant<int, 0> keep;
+        if (plan.wide == 4) return run(SPARSE, std::integral_constant<int, 4>(), keep);
+        if (plan.wide == 2) return run(SPARSE, std::integral_constant<int, 2>(), keep);
+        if (plan.once)
+            return run(SPARSE, std::integral_constant<int, 1>(), std::integral_constant<int, kOnce>());
+        return run(SPARSE, std::integral_constant<int, 1>(), keep);
+    };
+    return p.index != nullptr ? tiles(std::true_type()) : tiles(std::false_type());
 }
 
 template <typename T, int D>
@@ -595,10 +631,10 @@ hipError_t join(const PagedAttn &p, const PagedPlan &plan, void *O, float *LSE, 
 }  // namespace
 
 hipError_t launch_paged_attn(const PagedAttn &p, const PagedPlan &plan, const void *Q,
-                             const void *Kp, const void *Vp, bool bf16, void *O, float *LSE,
-                             void *ws, hipStream_t s) {
+                             const void *Kp, const void *Vp, void *O, float *LSE, void *ws,
+                             hipStream_t s) {
     char *w = static_cast<char *>(ws);
-    if (bf16)
+    if (p.half)
         return p.d == 32 ? attn<uint16_t, 32>(p, plan, Q, Kp, Vp, O, LSE, w, s)
              : p.d == 64 ? attn<uint16_t, 64>(p, plan, Q, Kp, Vp, O, LSE, w, s)
                          : attn<uint16_t, 128>(p, plan, Q, Kp, Vp, O, LSE, w, s);
@@ -607,10 +643,10 @@ hipError_t launch_paged_attn(const PagedAttn &p, const PagedPlan &plan, const vo
                      : attn<float, 128>(p, plan, Q, Kp, Vp, O, LSE, w, s);
 }
 
-hipError_t launch_paged_join(const PagedAttn &p, const PagedPlan &plan, bool bf16, void *O,
-                             float *LSE, const void *ws, hipStream_t s) {
+hipError_t launch_paged_join(const PagedAttn &p, const PagedPlan &plan, void *O, float *LSE,
+                             const void *ws, hipStream_t s) {
     const char *w = static_cast<const char *>(ws);
-    if (bf16)
+    if (p.half)
         return p.d == 32 ? join<uint16_t, 32>(p, plan, O, LSE, w, s)
              : p.d == 64 ? join<uint16_t, 64>(p, plan, O, LSE, w, s)
                          : join<uint16_t, 128>(p, plan, O, LSE, w, s);

@@ -33,6 +33,7 @@ hipError_t launch_paged_append(const PagedAppend &p, const void *K, const void *
 struct PagedAttn {
     int B, H, G, Lq, d;   // G query heads a cache head
     int shift, P, N, causal, keep;
+    bool half;   // bf16, else f32
     float scale;
     const int32_t *table, *index, *key_len, *q_len;
 };
@@ -50,17 +51,19 @@ struct PagedPlan {
     int splits;    // units of every sequence; 0: as many as its length asks for
     int chunk;     // blocks of a unit (splits 0: at least)
     int share;     // splits 0: units that all lengths together are cut into
-    int tiles;     // of 16 rows
+    int wide;      // tiles of 16 rows of a workgroup: 1, 2 or 4
+    int tile_groups;   // workgroups of a unit and cache head
+    bool once;     // K and V are read past the caches
     int most;      // units a sequence has at most
     size_t part, stat, info, bytes;   // workspace: offsets of the parts, size
 };
 PagedPlan paged_plan(const PagedAttn &p, bool sparse);
 
 hipError_t launch_paged_attn(const PagedAttn &p, const PagedPlan &plan, const void *Q,
-                             const void *Kp, const void *Vp, bool bf16, void *O, float *LSE,
-                             void *ws, hipStream_t s);
-hipError_t launch_paged_join(const PagedAttn &p, const PagedPlan &plan, bool bf16, void *O,
-                             float *LSE, const void *ws, hipStream_t s);
+                             const void *Kp, const void *Vp, void *O, float *LSE, void *ws,
+                             hipStream_t s);
+hipError_t launch_paged_join(const PagedAttn &p, const PagedPlan &plan, void *O, float *LSE,
+                             const void *ws, hipStream_t s);
 
 struct PagedSelect {
     int B, H, G, Lq, d, shift, P, N, causal, keep, first, recent;

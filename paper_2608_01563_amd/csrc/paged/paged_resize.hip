@@ -7,13 +7,17 @@
 // is little, in the grid of paged_slots otherwise.  A page that is taken is read
 // from the stack or, where it was given back in the same call, from the table of
 // the sequence that lost it, so that nothing waits for what is written.
+//
+// Latency bounds it: one read of the lengths, two scans (what a sequence needs
+// counts only if its rows fit), a search, one read of table or stack.
+#include <type_traits>
+
 #include "paged_device.h"
 #include "paged_launch.h"
 
 namespace mg {
 namespace {
 
-constexpr int kThreads = 1024;
 constexpr int kSlotThreads = 256;
 constexpr int kHeld = 1024;   // sequences whose sums fit the LDS
 
@@ -28,37 +32,46 @@ struct Records {
 };
 enum { kCount, kBack, kAvailable, kSums };
 
-// The first b with end[b] > x (x below end[B - 1]).
-__device__ __forceinline__ int find(const int32_t *end, int B, int x) {
-    int lo = 0, hi = B - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (end[mid] > x) hi = mid;
-        else lo = mid + 1;
-    }
-    return lo;
+// The first b with end[b] > x[e] (x below end[B - 1]), for all e at a time: a search
+// waits for each of its reads, so several wait together.
+template <int M>
+__device__ __forceinline__ void find(const int32_t *end, int B, const int (&x)[M], int (&b)[M]) {
+#pragma unroll
+    for (int e = 0; e < M; ++e) b[e] = 0;
+    for (int half = B > 1 ? 1 << (31 - __builtin_clz(B - 1)) : 0; half > 0; half /= 2)
+#pragma unroll
+        for (int e = 0; e < M; ++e)
+            if (b[e] + half < B && end[b[e] + half - 1] <= x[e]) b[e] += half;
 }
 
-// Pages given back and slots, by threads first, first + step, ...; r.row_end and
-// r.back_end may be copies in LDS.
+// Slots and pages given back (M at a time), by threads first, first + step, ...;
+// r.row_end and r.back_end may be copies in LDS.
+template <int M>
 __device__ __forceinline__ void pages_and_slots(const PagedResize &p, const Records &r, int first,
                                                 int step) {
     const int count = r.sums[kCount], back = r.sums[kBack], available = r.sums[kAvailable];
     // the k-th page given back, the k-th page taken
+    const auto entry_of = [&](int b, int k) {
+        return (size_t)b * p.P + r.left[b] + k - (b > 0 ? r.back_end[b - 1] : 0);
+    };
     const auto given = [&](int k) {
-        const int b = find(r.back_end, p.B, k);
-        return p.table[(size_t)b * p.P + r.left[b] + k - (b > 0 ? r.back_end[b - 1] : 0)];
+        const int x[1] = {k};
+        int b[1];
+        find(r.back_end, p.B, x, b);
+        return p.table[entry_of(b[0], k)];
     };
     const auto taken = [&](int k) {
         const int at = available - 1 - k;
         return at < count ? p.free_pages[at] : given(at - count);
     };
-    for (int k = first; k < back && k < p.N - count; k += step) p.free_pages[count + k] = given(k);
     const int rows = r.row_end[p.B - 1], page = 1 << p.shift;
     for (int t = first; t < p.T; t += step) {
         int slot = -1;
         if (t < rows) {
-            const int b = find(r.row_end, p.B, t), base = r.base[b];
+            const int x[1] = {t};
+            int found[1];
+            find(r.row_end, p.B, x, found);
+            const int b = found[0], base = r.base[b];
             if (base >= 0) {
                 const int len = r.len[b], have = (len + page - 1) >> p.shift;
                 const int pos = len + t - (b > 0 ? r.row_end[b - 1] : 0), at = pos >> p.shift;
@@ -71,95 +84,132 @@ __device__ __forceinline__ void pages_and_slots(const PagedResize &p, const Reco
         }
         p.slot[t] = slot;
     }
+    const int pushed = min(back, p.N - count);
+    for (int k = first; k < pushed; k += M * step) {
+        int x[M], b[M], id[M];
+#pragma unroll
+        for (int e = 0; e < M; ++e) x[e] = min(k + e * step, pushed - 1);
+        find(r.back_end, p.B, x, b);
+#pragma unroll
+        for (int e = 0; e < M; ++e) id[e] = p.table[entry_of(b[e], x[e])];
+#pragma unroll
+        for (int e = 0; e < M; ++e)
+            if (k + e * step < pushed) p.free_pages[count + k + e * step] = id[e];
+    }
 }
 
-// Sum over the threads before, and with, each one; `total` over all.
-template <typename T>
-__device__ __forceinline__ T block_scan(T v, T *part, T &total) {
+// Sums over the threads up to and with each one, and over all, of two values at a
+// time.  `part` may be written again behind another barrier.
+template <int THREADS, typename A, typename B>
+__device__ __forceinline__ void block_scan(A &a, B &b, A &all_a, B &all_b, A *part_a, B *part_b) {
+    constexpr int W = THREADS / 64;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const T upto = wave_scan(v, lane);
-    __syncthreads();   // the last scan's parts have been read
-    if (lane == 63) part[w] = upto;
-    __syncthreads();
-    T before = 0;
-    total = 0;
-    for (int k = 0; k < kThreads / 64; ++k) {
-        if (k < w) before += part[k];
-        total += part[k];
+    a = wave_scan(a);
+    b = wave_scan(b);
+    if (lane == 63) {
+        part_a[w] = a;
+        part_b[w] = b;
     }
-    return before + upto;
+    __syncthreads();
+    all_a = 0;
+    all_b = 0;
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+        const A x = part_a[k];
+        const B y = part_b[k];
+        if (k < w) {
+            a += x;
+            b += y;
+        }
+        all_a += x;
+        all_b += y;
+    }
 }
 
-// ALONE: at most kHeld sequences, records in LDS, and the second part follows.
-template <bool ALONE>
-__global__ __launch_bounds__(kThreads)
+// ALONE: at most THREADS sequences, records in LDS, and the second part follows.
+template <int THREADS, bool ALONE>
+__global__ __launch_bounds__(THREADS)
 void paged_resize(PagedResize p, Records r) {
-    __shared__ int64_t wide[kThreads / 64];
-    __shared__ int32_t part[kThreads / 64];
-    __shared__ int32_t kept, sums[kSums];
-    __shared__ int32_t records[5][ALONE ? kHeld : 1];
-    if constexpr (ALONE) {
+    constexpr int W = THREADS / 64;
+    using Rows = std::conditional_t<ALONE, int32_t, int64_t>;   // T and THREADS are small: clamped
+    __shared__ Rows wide[W];
+    __shared__ int32_t part[3][W], sums[kSums];
+    __shared__ int32_t records[5][ALONE ? THREADS : 1];
+    if constexpr (ALONE)
         r = {records[0], records[1], records[2], records[3], records[4], sums};
-    }
     const int tid = threadIdx.x, page = 1 << p.shift, capacity = p.P << p.shift;
     const auto pages = [&](int n) { return (int)(((int64_t)n + page - 1) >> p.shift); };
     const int count = min(max(p.free_count[0], 0), p.N);
-    if (tid == 0) kept = 0;
+    struct Sequence {
+        int len, goal;
+    };
+    const auto sequence = [&](int b) {
+        if (b >= p.B) return Sequence{0, 0};
+        return Sequence{min(max(p.key_len[b], 0), capacity), max(p.want[b], 0)};
+    };
+    const auto back_of = [&](Sequence q) { return max(pages(q.len) - pages(q.goal), 0); };
 
+    // pages given back by all come first: they may be taken by any
     int back_total = 0;
-    for (int b0 = 0; b0 < p.B; b0 += kThreads) {
-        const int b = b0 + tid;
-        int back = 0;
-        if (b < p.B) {
-            const int len = min(max(p.key_len[b], 0), capacity), goal = max(p.want[b], 0);
-            back = max(pages(len) - pages(goal), 0);
-        }
-        int total;
-        const int end = back_total + block_scan(back, part, total);
-        if (b < p.B) r.back_end[b] = end;
-        back_total += total;
+    if (p.B > THREADS) {
+        int none = 0, nothing;
+        for (int b = tid; b < p.B; b += THREADS) none += back_of(sequence(b));
+        int same = 0;
+        block_scan<THREADS>(none, same, back_total, nothing, part[1], part[2]);
     }
-    const int available = (int)min((int64_t)count + back_total, (int64_t)p.N);
-
-    int64_t rows_before = 0;
-    int need_before = 0;
-    for (int b0 = 0; b0 < p.B; b0 += kThreads) {
+    Rows rows_before = 0;
+    int need_before = 0, back_before = 0, took_before = 0;
+    for (int b0 = 0; b0 < p.B; b0 += THREADS) {
         const int b = b0 + tid;
-        int len = 0, goal = 0;
+        const Sequence q = sequence(b);
+        const int add = max(q.goal - q.len, 0);
+        Rows row_end = min(add, p.T + 1), rows;   // (one row too many is as bad as more)
+        int back_end = back_of(q), backs;
+        block_scan<THREADS>(row_end, back_end, rows, backs, wide, part[0]);
+        row_end += rows_before;
+        if (p.B <= THREADS) back_total = backs;
+        const int available = (int)min((int64_t)count + back_total, (int64_t)p.N);
+        const bool fits = add > 0 && q.goal <= capacity && row_end <= p.T;
+        const int need = fits ? pages(q.goal) - pages(q.len) : 0;
+        // whether a sequence is granted its pages hangs on those before it only: they
+        // are, if it is
+        int need_end = need, all, unused = 0, none;
+        block_scan<THREADS>(need_end, unused, all, none, part[1], part[2]);
+        need_end += need_before;
+        const bool granted = fits && (need == 0 || need_end <= available);
+        if (granted && need > 0) took_before = need_end;
         if (b < p.B) {
-            len = min(max(p.key_len[b], 0), capacity);
-            goal = max(p.want[b], 0);
-        }
-        const int add = max(goal - len, 0);
-        int64_t rows;
-        const int64_t row_end = rows_before + block_scan((int64_t)add, wide, rows);
-        const bool fits = add > 0 && goal <= capacity && row_end <= p.T;
-        const int need = fits ? pages(goal) - pages(len) : 0;
-        int all;
-        const int end = need_before + block_scan(need, part, all);
-        const bool granted = fits && (need == 0 || end <= available);
-        if (granted && need > 0) atomicAdd(&kept, need);
-        if (b < p.B) {
-            const int upto = (int)min(row_end, (int64_t)p.T);
+            const int upto = (int)min(row_end, (Rows)p.T);
             r.row_end[b] = upto;
-            r.base[b] = granted ? end - need : -1;
-            r.len[b] = len;
-            r.left[b] = pages(goal);
+            r.back_end[b] = back_before + back_end;
+            r.base[b] = granted ? need_end - need : -1;
+            r.len[b] = q.len;
+            r.left[b] = pages(q.goal);
             p.offset[b + 1] = upto;
             if (b == 0) p.offset[0] = 0;
-            p.new_len[b] = add == 0 || granted ? goal : len;
+            p.new_len[b] = add == 0 || granted ? q.goal : q.len;
         }
         rows_before += rows;
+        back_before += backs;
         need_before += all;
     }
+    // pages taken: up to the last granted sequence's
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) took_before = max(took_before, __shfl_xor(took_before, m, 64));
+    if ((tid & 63) == 0) part[2][tid >> 6] = took_before;
+    const int available = (int)min((int64_t)count + back_total, (int64_t)p.N);
     if (tid == 0) {
         r.sums[kCount] = count;
         r.sums[kBack] = back_total;
         r.sums[kAvailable] = available;
     }
     __syncthreads();
-    if (tid == 0) p.new_count[0] = available - kept;
-    if constexpr (ALONE) pages_and_slots(p, r, tid, kThreads);
+    if (tid == 0) {
+        int took = 0;
+        for (int k = 0; k < W; ++k) took = max(took, part[2][k]);
+        p.new_count[0] = available - took;
+    }
+    if constexpr (ALONE) pages_and_slots<4>(p, r, tid, THREADS);
 }
 
 __global__ __launch_bounds__(kSlotThreads)
@@ -174,7 +224,7 @@ void paged_slots(PagedResize p, Records r) {
         r.row_end = ends[0];
         r.back_end = ends[1];
     }
-    pages_and_slots(p, r, blockIdx.x * kSlotThreads + threadIdx.x, gridDim.x * kSlotThreads);
+    pages_and_slots<1>(p, r, blockIdx.x * kSlotThreads + threadIdx.x, gridDim.x * kSlotThreads);
 }
 
 Records records_of(const PagedResize &p, void *ws) {
@@ -185,17 +235,17 @@ Records records_of(const PagedResize &p, void *ws) {
 
 }  // namespace
 
-bool paged_resize_alone(int B, int T) { return B <= kHeld && T <= 2048; }
+bool paged_resize_alone(int B, int T) { return B <= 1024 && T <= 2048; }
 
 size_t paged_resize_bytes(int B, int T) {
     return paged_resize_alone(B, T) ? 0 : ((size_t)5 * B + kSums) * 4;
 }
 
 hipError_t launch_paged_resize(const PagedResize &p, void *ws, hipStream_t s) {
-    if (paged_resize_alone(p.B, p.T))
-        paged_resize<true><<<1, kThreads, 0, s>>>(p, Records{});
+    if (!paged_resize_alone(p.B, p.T))
+        paged_resize<1024, false><<<1, 1024, 0, s>>>(p, records_of(p, ws));
     else
-        paged_resize<false><<<1, kThreads, 0, s>>>(p, records_of(p, ws));
+        paged_resize<1024, true><<<1, 1024, 0, s>>>(p, Records{});
     return hipGetLastError();
 }
 

@@ -146,7 +146,7 @@ void paged_select(SelectArgs a) {
             uint32_t n[4], sum = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) n[e] = counts[255 - 4 * lane - e], sum += n[e];
-            const uint32_t upto = wave_scan(sum, lane);
+            const uint32_t upto = wave_scan(sum);
             uint32_t above = upto - sum;
             if (above < (uint32_t)left && upto >= (uint32_t)left)
 #pragma unroll
