@@ -142,8 +142,9 @@ size_t mg_attn_fwd_paged_workspace_bytes(int B, int Hq, int H, int Lq, int d, in
  *
  *   max over the group's heads g of  sum_c max(Q[g][c] lo[c], Q[g][c] hi[c])
  *
- * each sum in 64 bits, rounded to f32.  (A page without an entry in [0, N) counts
- * as NaN.)
+ * each sum in 64 bits, rounded to f32.  (Bounds are finite, as mg_paged_append
+ * leaves them: a sum in which 0 meets an infinite one is NaN.  A page without an
+ * entry in [0, N) counts as NaN.)
  *   index  int32 [B][H][Lq][keep]: pages j / page, ascending; -1 behind the last
  */
 mg_status_t mg_paged_select(const void *Q, const void *bounds, const int32_t *table,
