@@ -16,7 +16,7 @@ namespace mg {
 namespace {
 constexpr int kWant = 1024;       // workgroups that a call is cut into
 constexpr int kLeast = 8;         // blocks of a unit
-constexpr int64_t kCached = 256 << 20;   // bytes that the last cache holds
+constexpr int64_t kCached = 64 << 20;   // bytes that caches may hold from call to call
 constexpr int kLongest = 1 << 13; // blocks of a unit (2^18 tokens)
 
 void paged_workspace(PagedPlan &plan, const PagedAttn &p, int64_t rows) {
@@ -32,19 +32,19 @@ void paged_workspace(PagedPlan &plan, const PagedAttn &p, int64_t rows) {
 PagedPlan paged_plan(const PagedAttn &p, bool sparse) {
     PagedPlan plan = {};
     const int64_t rows = paged_rows(p, sparse);
-    const int64_t tiles = (rows + 15) / 16;
-    plan.wide = tiles == 1 ? 1 : tiles == 2 ? 2 : 4;
-    plan.tile_groups = (int)((tiles + plan.wide - 1) / plan.wide);
-    const int64_t groups = (int64_t)p.H * plan.tile_groups;   // workgroups of a unit
+    plan.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+    plan.groups = (int)((rows + plan.rows - 1) / plan.rows);
+    const int64_t groups = (int64_t)p.H * plan.groups;   // workgroups of a unit
     const int64_t cut = std::max<int64_t>(1, kWant / groups);
     const int64_t pages = std::min<int64_t>(p.N, (int64_t)p.B * (sparse ? p.Lq * p.keep : p.P));
     plan.once = (pages << p.shift) * p.H * p.d * (p.half ? 4 : 8) > kCached;
     if (sparse) {
-        // lists are short of their `keep` pages only where sequences are: all alike.
+        // lists are short of their `keep` pages only where sequences are: units are all
+        // alike, and one round of them will do.
         // A unit has at most 64 pages, whose entries a wave holds.
         const int blocks = (int)(((int64_t)p.keep << p.shift) + 31) / 32;
         const int64_t seqs = (int64_t)p.B * p.Lq;
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(cut / seqs, blocks / kLeast));
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(cut / 2 / seqs, blocks / kLeast));
         plan.chunk = (cdiv(blocks, (int)want) + 3) / 4 * 4;
         plan.chunk = std::min(plan.chunk, 2 << p.shift);
         plan.splits = cdiv(blocks, plan.chunk);
@@ -173,7 +173,7 @@ mg_status_t check_attn(const mg::PagedAttn &p, int Hq, int page, bool sparse,
     if (!std::isfinite(p.scale * kLog2e))
         return fail(MG_ERR_INVALID_ARGUMENT, "scale log2 e is not finite (scale %g)", p.scale);
     *plan = mg::paged_plan(p, sparse);
-    if ((int64_t)plan->units * p.H * plan->tile_groups > kMaxGroups)
+    if ((int64_t)plan->units * p.H * plan->groups > kMaxGroups)
         return fail(MG_ERR_INVALID_ARGUMENT, "too much work for one call (B=%d H=%d Lq=%d P=%d)",
                     p.B, p.H, p.Lq, p.P);
     return MG_OK;

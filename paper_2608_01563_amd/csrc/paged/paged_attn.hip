@@ -44,7 +44,7 @@ struct AttnArgs {
     const int32_t *table, *index, *key_len, *q_len;
     int B, H, G, Lq, P, N, shift, causal, keep;
     float scale_log2;
-    int splits, chunk, share, tile_groups;
+    int splits, chunk, share, groups;
 };
 
 // One unit: blocks [first, first + count) of sequence b (sparse: of row i's list);
@@ -153,7 +153,7 @@ template <typename T, int D>
 struct Operand {
     f32x4 p[Shape<T, D>::kTiles];
 
-    __device__ __forceinline__ explicit Operand(const f32x4 (&x)[Shape<T, D>::kTiles]) {
+    __device__ __forceinline__ void set(const f32x4 (&x)[Shape<T, D>::kTiles]) {
 #pragma unroll
         for (int t = 0; t < Shape<T, D>::kTiles; ++t) p[t] = x[t];
     }
@@ -162,7 +162,7 @@ template <int D>
 struct Operand<uint16_t, D> {
     bf16x8 hi, lo;
 
-    __device__ __forceinline__ explicit Operand(const f32x4 (&p)[2]) {
+    __device__ __forceinline__ void set(const f32x4 (&p)[2]) {
         u32x4 high;
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
@@ -179,19 +179,20 @@ struct Operand<uint16_t, D> {
     }
 };
 
-template <typename T, int D, bool SPARSE, int TW, int CACHE>
+template <typename T, int D, bool SPARSE, int RT, int TW, int CACHE>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 8)))
 void paged_attn(AttnArgs a) {
     using S = Shape<T, D>;
     constexpr int NT = S::kTiles, N = S::kN, RB = S::kRowBytes;
-    constexpr int LD = D + 4, WV = kWaves / TW;   // waves a tile
-    __shared__ __attribute__((aligned(16))) float Os[kWaves][kRows][LD];
-    __shared__ float Ms[kWaves][kRows], Ls[kWaves][kRows];
+    constexpr int LD = D + 4, WV = kWaves / TW, WR = kRows * RT;   // waves, rows a stream
+    __shared__ __attribute__((aligned(16))) float Os[kWaves][WR][LD];
+    __shared__ float Ms[kWaves][WR], Ls[kWaves][WR];
+    __shared__ bool Odd[kWaves];
 
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int tiles0 = blockIdx.x % a.tile_groups, rest = blockIdx.x / a.tile_groups;
-    const int h = rest % a.H, u = rest / a.H, tile = tiles0 * TW + w % TW;
+    const int group = blockIdx.x % a.groups, rest = blockIdx.x / a.groups;
+    const int h = rest % a.H, u = rest / a.H;
     Unit un;
     if (a.splits > 0) {
         const int at = u / a.splits;
@@ -210,23 +211,26 @@ void paged_attn(AttnArgs a) {
         paged_mask(a.key_len, a.q_len, un.b, a.P << a.shift, a.Lq, a.causal);
     if (a.splits > 0 && !SPARSE)   // units behind the sequence's end are none
         un.splits = max(1, min(a.splits, ((mask.n + 31) / 32 + a.chunk - 1) / a.chunk));
-    if (!SPARSE && a.info != nullptr && h == 0 && tiles0 == 0 && un.split == 0 && tid == 0)
+    if (!SPARSE && a.info != nullptr && h == 0 && group == 0 && un.split == 0 && tid == 0)
         a.info[un.b] = make_int2(un.base, un.splits);
     if (un.split >= un.splits) return;
 
-    // the lane's row, and what the tile's rows see
+    // the lane's rows, one a tile, and what the wave's rows see
     const int rows = SPARSE ? a.G : a.G * a.Lq;
-    const int r = kRows * tile + c;
-    const bool in = r < rows;
-    const int i = SPARSE ? un.i : (in ? r : rows - 1) / a.G;
-    const int head = SPARSE ? min(r, rows - 1) : (in ? r : rows - 1) - i * a.G;
-    const size_t at = ((size_t)(un.b * a.H + h) * a.G + head) * a.Lq + i;   // of [B][Hq][Lq]
-    const bool valid = in && i < mask.rows;
-    const int limit = valid ? mask.limit(i) : 0;
-    const int first_i = SPARSE ? un.i : kRows * tile / a.G;
-    const int last_i =
-        SPARSE ? un.i : min((min(rows, kRows * (tile + 1)) - 1) / a.G, mask.rows - 1);
-    const bool some = kRows * tile < rows && first_i < mask.rows;
+    const int row0 = WR * (group * TW + w % TW);
+    int row_i[RT], limit[RT];
+    size_t row_at[RT];   // of [B][Hq][Lq]
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const int row = min(row0 + kRows * r + c, rows - 1);
+        row_i[r] = SPARSE ? un.i : row / a.G;
+        const int head = SPARSE ? row : row - row_i[r] * a.G;
+        row_at[r] = ((size_t)(un.b * a.H + h) * a.G + head) * a.Lq + row_i[r];
+        limit[r] = row0 + kRows * r + c < rows ? mask.limit(row_i[r]) : 0;
+    }
+    const int first_i = SPARSE ? un.i : row0 / a.G;
+    const int last_i = SPARSE ? un.i : min((min(rows, row0 + WR) - 1) / a.G, mask.rows - 1);
+    const bool some = row0 < rows && first_i < mask.rows;
     const int all = some ? mask.limit(first_i) : 0;   // below: every row sees the token
     const int end = some ? mask.limit(last_i) : 0;
 
@@ -282,37 +286,48 @@ void paged_attn(AttnArgs a) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) x.load_v(t, buffer_rsrc(vp + now[t].at, now[t].bytes), v_at);
 
-    // (rows behind the sequence's, whatever they hold, are taken as zeros)
-    u32x4 q[S::kPieces];
+    // (rows that see nothing, whatever they hold, are taken as zeros)
+    u32x4 q[RT][S::kPieces];
 #pragma unroll
-    for (int s = 0; s < S::kPieces; ++s)
-        q[s] = valid ? *reinterpret_cast<const u32x4 *>(static_cast<const char *>(a.Q) +
-                                                        at * RB + 64 * s + 16 * g)
-                     : u32x4{0, 0, 0, 0};
-
-    float m = -INFINITY, l = 0.f;
-    f32x4 o[N];
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
-    for (int j = 0; j < N; ++j) o[j] = zero4();
+        for (int s = 0; s < S::kPieces; ++s)
+            q[r][s] = limit[r] > 0 ? *reinterpret_cast<const u32x4 *>(
+                                         static_cast<const char *>(a.Q) + row_at[r] * RB + 64 * s +
+                                         16 * g)
+                                   : u32x4{0, 0, 0, 0};
 
+    float m[RT], l[RT];
+    f32x4 o[RT][N];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        m[r] = -INFINITY;
+        l[r] = 0.f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) o[r][j] = zero4();
+    }
+
+    bool left_out = false;   // V of tokens that not all rows see
     while (block < stop) {
-        f32x4 s[NT];
+        f32x4 s[RT][NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            s[t] = zero4();
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int y = 0; y < S::kPieces; ++y) {
-                if constexpr (S::kHalf) {
-                    s[t] = mfma16x16x32bf16(__builtin_bit_cast(bf16x8, x.k[t][y]),
-                                            __builtin_bit_cast(bf16x8, q[y]), s[t]);
-                } else {
+            for (int r = 0; r < RT; ++r) {
+                s[r][t] = zero4();
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        s[t] = mfma16x16x4(__uint_as_float(x.k[t][y][e]),
-                                           __uint_as_float(q[y][e]), s[t]);
+                for (int y = 0; y < S::kPieces; ++y) {
+                    if constexpr (S::kHalf) {
+                        s[r][t] = mfma16x16x32bf16(__builtin_bit_cast(bf16x8, x.k[t][y]),
+                                                   __builtin_bit_cast(bf16x8, q[r][y]), s[r][t]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            s[r][t] = mfma16x16x4(__uint_as_float(x.k[t][y][e]),
+                                                  __uint_as_float(q[r][y][e]), s[r][t]);
+                    }
                 }
             }
-        }
         // the next block's K comes while this one's scores are worked on (behind
         // the last block: descriptors of no bytes)
         const int following = block + WV;
@@ -327,96 +342,99 @@ void paged_attn(AttnArgs a) {
             x.load_k(t, buffer_rsrc(kp + next[t].at, next[t].bytes), k_at);
         }
 
-        bool diagonal = false;   // a token that some rows see and some do not
-        float top = -INFINITY;
+        bool partly = false, diagonal = false;   // tokens that not all, that some rows see
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            s[t] *= a.scale_log2;
-            if (now[t].token + 16 > all) {
-                diagonal |= end > all && now[t].token < end;
-                const int left = limit - now[t].token - 4 * g;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (e >= left) s[t][e] = -INFINITY;
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) top = fmaxf(top, s[t][e]);
+            partly |= now[t].token + 16 > all;
+            diagonal |= end > all && now[t].token + 16 > all && now[t].token < end;
         }
-        top = fmaxf(m, max_over_groups(top));
-        if (__any(top > m)) {
-            const float alpha = m == -INFINITY ? 0.f : exp2_fast(m - top);
-            l *= alpha;
+        Operand<T, D> operand[RT];
 #pragma unroll
-            for (int j = 0; j < N; ++j) o[j] *= alpha;
-            m = top;
-        }
-        const float from = m == -INFINITY ? 0.f : m;
-        f32x4 p[NT];
+        for (int r = 0; r < RT; ++r) {
+            float top = -INFINITY;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+            for (int t = 0; t < NT; ++t) {
+                s[r][t] *= a.scale_log2;
+                if (partly) {
+                    const int left = limit[r] - now[t].token - 4 * g;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                p[t][e] = exp2_fast(s[t][e] - from);
-                l += p[t][e];
+                    for (int e = 0; e < 4; ++e)
+                        if (e >= left) s[r][t][e] = -INFINITY;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = fmaxf(top, s[r][t][e]);
             }
+            top = fmaxf(m[r], max_over_groups(top));
+            if (__any(top > m[r])) {
+                const float alpha = m[r] == -INFINITY ? 0.f : exp2_fast(m[r] - top);
+                l[r] *= alpha;
+#pragma unroll
+                for (int j = 0; j < N; ++j) o[r][j] *= alpha;
+                m[r] = top;
+            }
+            const float from = m[r] == -INFINITY ? 0.f : m[r];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[r][t][e] = exp2_fast(s[r][t][e] - from);
+                    l[r] += s[r][t][e];
+                }
+            operand[r].set(s[r]);
+        }
 
-        // Channel block j of O^T += V^T P^T (CUT: with V's tokens from `below` on taken
-        // as zeros)
-        const Operand<T, D> operand(p);
-        const auto product = [&](auto CUT, int j, f32x4 to, int below) {
-            const auto value = [&](int t, int y, int word) {
-                if constexpr (!decltype(CUT)::value) return x.v[t][y][word];
-                else return now[t].token + 4 * g + y < below ? x.v[t][y][word] : 0u;
-            };
-            if constexpr (S::kHalf) {
-                u32x4 av;
+        // channel block j of V^T, from words that `word` gives: an operand (bf16), or
+        // the values of tokens 4 g + y of tile t (f32)
+        const auto channels = [&](auto word, int j) {
+            u32x4 v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    av[e] = __builtin_amdgcn_perm(value(e / 2, 2 * (e % 2) + 1, j / 2),
-                                                  value(e / 2, 2 * (e % 2), j / 2),
-                                                  j % 2 ? 0x07060302 : 0x05040100);
-                const bf16x8 vt = __builtin_bit_cast(bf16x8, av);
-                to = mfma16x16x32bf16(vt, operand.hi, to);
-                return mfma16x16x32bf16(vt, operand.lo, to);
-            } else {
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        to = mfma16x16x4(__uint_as_float(value(t, y, j)), operand.p[t][y], to);
-                return to;
-            }
+            for (int e = 0; e < 4; ++e)
+                v[e] = __builtin_amdgcn_perm(word(e / 2, 2 * (e % 2) + 1, j / 2),
+                                             word(e / 2, 2 * (e % 2), j / 2),
+                                             j % 2 ? 0x07060302 : 0x05040100);
+            return __builtin_bit_cast(bf16x8, v);
         };
-        bool special = false;   // V that is infinite or NaN where not all rows see it
-        if (diagonal) {
+        const auto value = [&](int t, int y, int word) { return x.v[t][y][word]; };
+        if (!SPARSE && diagonal) {
+            // V that is infinite or NaN and that not all rows see would reach the others as
+            // 0 times it: it is left out here and added to the rows that see it in the end
+            const auto odd = [](uint32_t v) { return (v & 0x7f800000u) == 0x7f800000u; };
             bool mine = false;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int y = 0; y < 4; ++y)
-                    if (now[t].token + 4 * g + y >= all)
 #pragma unroll
-                        for (int word = 0; word < S::kWords; ++word) {
-                            const uint32_t bits = x.v[t][y][word];
-                            mine |= (bits & 0x7f800000u) == 0x7f800000u;
-                            if (S::kHalf) mine |= (bits & 0x7f80u) == 0x7f80u;
-                        }
-            special = __any(mine);
+                    for (int word = 0; word < S::kWords; ++word) {
+                        uint32_t &v = x.v[t][y][word];
+                        const bool unseen = now[t].token + 4 * g + y >= all;
+                        const bool high = unseen && odd(v);
+                        const bool low = unseen && S::kHalf && odd(v << 16);
+                        mine |= high || low;
+                        v = high ? S::kHalf ? v & 0xffffu : 0u : v;
+                        v = low ? v & 0xffff0000u : v;
+                    }
+            left_out |= __any(mine);
         }
-        if (!special) {
+        // O^T += V^T P^T
 #pragma unroll
-            for (int j = 0; j < N; ++j) o[j] = product(std::false_type(), j, o[j], 0);
-        } else {
-            // a product for every limit there is, of which the rows that have it take theirs
+        for (int j = 0; j < N; ++j) {
+            if constexpr (S::kHalf) {
+                const bf16x8 v = channels(value, j);
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                f32x4 sum = o[j];
-                for (int row = first_i; row <= last_i; ++row) {
-                    const f32x4 y = product(std::true_type(), j, o[j], mask.limit(row));
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[e] = i == row ? y[e] : sum[e];
+                for (int r = 0; r < RT; ++r) {
+                    o[r][j] = mfma16x16x32bf16(v, operand[r].hi, o[r][j]);
+                    o[r][j] = mfma16x16x32bf16(v, operand[r].lo, o[r][j]);
                 }
-                o[j] = sum;
+            } else {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+#pragma unroll
+                        for (int r = 0; r < RT; ++r)
+                            o[r][j] = mfma16x16x4(__uint_as_float(value(t, y, j)),
+                                                  operand[r].p[t][y], o[r][j]);
             }
         }
 #pragma unroll
@@ -428,21 +446,25 @@ void paged_attn(AttnArgs a) {
     }
 
     // the waves' shares through LDS
-    l = sum_over_groups(l);
+    if (lane == 0) Odd[w] = left_out;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int r = 0; r < RT; ++r) {
+        l[r] = sum_over_groups(l[r]);
 #pragma unroll
-        for (int j = 0; j < N; ++j) Os[w][c][S::channel(4 * g + e, j)] = o[j][e];
-    if (g == 0) {
-        Ms[w][c] = m;
-        Ls[w][c] = l;
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                Os[w][kRows * r + c][S::channel(4 * g + e, j)] = o[r][j][e];
+        if (g == 0) {
+            Ms[w][kRows * r + c] = m[r];
+            Ls[w][kRows * r + c] = l[r];
+        }
     }
     __syncthreads();
 
-    const int row = tid >> 4, d0 = N * (tid & 15);
-#pragma unroll
-    for (int part = 0; part < TW; ++part) {
-        const int rr = kRows * (tiles0 * TW + part) + row;
+    const int d0 = N * (tid & 15);
+    for (int at = tid >> 4; at < WR * TW; at += kThreads / 16) {
+        const int part = at / WR, row = at % WR, rr = WR * TW * group + at;
         if (rr >= rows) return;
         float top = -INFINITY;
 #pragma unroll
@@ -461,6 +483,26 @@ void paged_attn(AttnArgs a) {
         const int ri = SPARSE ? un.i : rr / a.G, rh = SPARSE ? rr : rr - ri * a.G;
         const size_t to = ((size_t)(un.b * a.H + h) * a.G + rh) * a.Lq + ri;
         const bool live = ri < mask.rows;
+        bool odd = false;
+#pragma unroll
+        for (int k = 0; k < WV; ++k) odd |= Odd[part + TW * k];
+        if (!SPARSE && odd) {
+            const int from = max(mask.limit(WR * (group * TW + part) / a.G), 32 * un.first);
+            for (int j = from; j < min(mask.limit(ri), 32 * (un.first + un.count)); ++j) {
+                const int id = table[j >> a.shift];
+                if ((uint32_t)id >= (uint32_t)a.N) continue;
+                const T *v = reinterpret_cast<const T *>(
+                    vp + ((size_t)id * a.H + h) * head_bytes +
+                    (size_t)(j & ((1 << a.shift) - 1)) * RB) + d0;
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    float x;
+                    if constexpr (S::kHalf) x = bf16_to_f32(v[e]);
+                    else x = v[e];
+                    if (!(fabsf(x) < INFINITY)) y[e] += x;
+                }
+            }
+        }
         if (un.splits > 1) {
             const size_t slot = ((size_t)u * a.H + h) * rows + rr;
             float *p = a.part + slot * D + d0;
@@ -594,22 +636,26 @@ hipError_t attn(const PagedAttn &p, const PagedPlan &plan, const void *Q, const 
     const AttnArgs a = {Q, Kp, Vp, O, LSE, (float *)(ws + plan.part), (float2 *)(ws + plan.stat),
                         plan.most > 1 ? (int2 *)(ws + plan.info) : nullptr, p.table, p.index, p.key_len, p.q_len,
                         p.B, p.H, p.G, p.Lq, p.P, p.N, p.shift, p.causal, p.keep,
-                        p.scale * kLog2e, plan.splits, plan.chunk, plan.share, plan.tile_groups};
-    const unsigned grid = (unsigned)((int64_t)plan.units * p.H * plan.tile_groups);
-    const auto run = [&](auto SPARSE, auto TW, auto CACHE) {
-        paged_attn<T, D, decltype(SPARSE)::value, decltype(TW)::value, decltype(CACHE)::value>
-            <<<grid, kThreads, 0, s>>>(a);
+                        p.scale * kLog2e, plan.splits, plan.chunk, plan.share, plan.groups};
+    const unsigned grid = (unsigned)((int64_t)plan.units * p.H * plan.groups);
+    const auto run = [&](auto SPARSE, auto RT, auto TW, auto CACHE) {
+        paged_attn<T, D, decltype(SPARSE)::value, decltype(RT)::value, decltype(TW)::value,
+                   decltype(CACHE)::value><<<grid, kThreads, 0, s>>>(a);
         return hipGetLastError();
     };
-    const auto tiles = [&](auto SPARSE) {
-        const std::integral_constant<int, 0> keep;
-        if (plan.wide == 4) return run(SPARSE, std::integral_constant<int, 4>(), keep);
-        if (plan.wide == 2) return run(SPARSE, std::integral_constant<int, 2>(), keep);
-        if (plan.once)
-            return run(SPARSE, std::integral_constant<int, 1>(), std::integral_constant<int, kOnce>());
-        return run(SPARSE, std::integral_constant<int, 1>(), keep);
+    const auto rows = [&](auto SPARSE) {
+        const std::integral_constant<int, 0> cached;
+        const std::integral_constant<int, kOnce> once;
+        const std::integral_constant<int, 1> one;
+        const std::integral_constant<int, 2> two;
+        const std::integral_constant<int, 4> four;
+        if (plan.rows == 16)
+            return plan.once ? run(SPARSE, one, one, once) : run(SPARSE, one, one, cached);
+        if (plan.rows == 32)
+            return plan.once ? run(SPARSE, two, one, once) : run(SPARSE, two, one, cached);
+        return plan.rows == 64 ? run(SPARSE, two, two, cached) : run(SPARSE, two, four, cached);
     };
-    return p.index != nullptr ? tiles(std::true_type()) : tiles(std::false_type());
+    return p.index != nullptr ? rows(std::true_type()) : rows(std::false_type());
 }
 
 template <typename T, int D>

@@ -45,14 +45,14 @@ inline int64_t paged_rows(const PagedAttn &p, bool sparse) {
 
 // How one call runs: every sequence (sparse: every query row) is cut into units
 // of the same number of blocks of 32 tokens, each a workgroup for every cache
-// head and 16 of the rows that share it.
+// head and so many of the rows that share it.
 struct PagedPlan {
     int units;     // of the grid, enough for any lengths
     int splits;    // units of every sequence; 0: as many as its length asks for
     int chunk;     // blocks of a unit (splits 0: at least)
     int share;     // splits 0: units that all lengths together are cut into
-    int wide;      // tiles of 16 rows of a workgroup: 1, 2 or 4
-    int tile_groups;   // workgroups of a unit and cache head
+    int rows;      // of a workgroup: 16, 32, 64 or 128
+    int groups;    // workgroups of a unit and cache head
     bool once;     // K and V are read past the caches
     int most;      // units a sequence has at most
     size_t part, stat, info, bytes;   // workspace: offsets of the parts, size
