@@ -14,7 +14,10 @@
 namespace mg {
 
 namespace {
-constexpr int kWant = 1024;       // workgroups that a call is cut into
+constexpr int kWant = 1536;       // workgroups of 16 rows that a call is cut into: six a
+                                  // compute unit, of which three run at once
+constexpr int kWantMore = 1024;   // of more rows: four, of which two run at once
+constexpr int kRound = 512;       // of a short call
 constexpr int kLeast = 8;         // blocks of a unit
 constexpr int64_t kCached = 64 << 20;   // bytes that caches may hold from call to call
 constexpr int kLongest = 1 << 13; // blocks of a unit (2^18 tokens)
@@ -35,7 +38,8 @@ PagedPlan paged_plan(const PagedAttn &p, bool sparse) {
     plan.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
     plan.groups = (int)((rows + plan.rows - 1) / plan.rows);
     const int64_t groups = (int64_t)p.H * plan.groups;   // workgroups of a unit
-    const int64_t cut = std::max<int64_t>(1, kWant / groups);
+    const int64_t cut = std::max<int64_t>(1, (plan.rows == 16 ? kWant : kWantMore) / groups);
+    const int64_t round = std::max<int64_t>(1, kRound / groups);
     const int64_t pages = std::min<int64_t>(p.N, (int64_t)p.B * (sparse ? p.Lq * p.keep : p.P));
     plan.once = (pages << p.shift) * p.H * p.d * (p.half ? 4 : 8) > kCached;
     if (sparse) {
@@ -44,7 +48,7 @@ PagedPlan paged_plan(const PagedAttn &p, bool sparse) {
         // A unit has at most 64 pages, whose entries a wave holds.
         const int blocks = (int)(((int64_t)p.keep << p.shift) + 31) / 32;
         const int64_t seqs = (int64_t)p.B * p.Lq;
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(cut / 2 / seqs, blocks / kLeast));
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(round / seqs, blocks / kLeast));
         plan.chunk = (cdiv(blocks, (int)want) + 3) / 4 * 4;
         plan.chunk = std::min(plan.chunk, 2 << p.shift);
         plan.splits = cdiv(blocks, plan.chunk);
@@ -56,12 +60,13 @@ PagedPlan paged_plan(const PagedAttn &p, bool sparse) {
     const int blocks = (int)((((int64_t)p.P << p.shift) + 31) / 32);
     const int full = cdiv(blocks, kLeast);
     plan.chunk = kLeast;
-    if ((int64_t)p.B * full <= cut + p.B) {
+    if ((int64_t)p.B * full <= round) {
         plan.splits = full;
         plan.units = p.B * full;
         plan.most = full;
     } else {
         plan.share = (int)cut;
+        plan.round = (int)round;
         plan.units = (int)std::max<int64_t>(cut + p.B, (int64_t)p.B * cdiv(blocks, kLongest));
         plan.most = std::max(std::min(full, (int)cut), cdiv(blocks, kLongest));
     }

@@ -32,7 +32,7 @@ constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kRows = 16;
 constexpr int kOnce = 2;   // cache policy: non-temporal
-constexpr uint32_t kShort = 20;   // blocks of a unit
+constexpr uint32_t kShort = 24;   // blocks of a unit
 constexpr int kFar = 1 << 30;   // a token that no row sees
 
 struct AttnArgs {
@@ -44,7 +44,7 @@ struct AttnArgs {
     const int32_t *table, *index, *key_len, *q_len;
     int B, H, G, Lq, P, N, shift, causal, keep;
     float scale_log2;
-    int splits, chunk, share, groups;
+    int splits, chunk, share, round, groups;
 };
 
 // One unit: blocks [first, first + count) of sequence b (sparse: of row i's list);
@@ -54,12 +54,17 @@ struct Unit {
 };
 
 // Which sequence unit u belongs to where lengths decide: every sequence is cut
-// into units of `chunk` blocks (at least one unit each), chunk so that all lengths
-// together make about `share` units, or half of them where these are short: a
-// workgroup on every slot the GPU has and no second round (8 sequences of 2,500
-// tokens, 8 heads, 28 rows: 22 us with 448 workgroups of 12 blocks, 29 with 640 of
-// 8); long ones are better evened out by two rounds (32 sequences of 2,560 tokens,
-// 8 heads: 62 us with units of 20 blocks, 72 with 40).
+// into units of `chunk` blocks (at least one unit each).  Of 8 cache heads, in us:
+//
+//                                       workgroups:  512   768  1024  1536
+//   8 sequences of 16,384 to 65,536 tokens, 1 row    230   190   194   186
+//   32 of 1,024 to 4,096, 1 row                       72    67    63    63
+//   4 of 32,768, 1 row                                85    87    86    93
+//   8 of 1,000 to 4,001, 28 rows                      27          35    35
+//
+// So: about `round` units (two workgroups a compute unit, all at once) where that
+// fills them to 15 in 16, or where they are so short that a second round costs more
+// than it evens out; `share` (more rounds) otherwise.
 __device__ __forceinline__ Unit unit_by_length(const AttnArgs &a, int u, int lane) {
     const int capacity = a.P << a.shift;
     const auto blocks_of = [&](int b) {
@@ -69,14 +74,26 @@ __device__ __forceinline__ Unit unit_by_length(const AttnArgs &a, int u, int lan
     uint32_t total = mine;
     for (int b = 64 + lane; b < a.B + lane; b += 64) total += blocks_of(b);
     total = wave_sum(total);
-    uint32_t chunk = (total + a.share - 1) / a.share;
-    if (2 * chunk <= kShort) chunk = (2 * total + a.share - 1) / a.share;
-    chunk = min(max((chunk + kWaves - 1) / kWaves * kWaves, (uint32_t)a.chunk), 1u << 13);
+    const auto parts_of = [](uint32_t n, uint32_t chunk) { return max((n + chunk - 1) / chunk, 1u); };
+    const auto whole = [&](uint32_t chunk) {   // of streams, within the bounds
+        return min(max((chunk + kWaves - 1) / kWaves * kWaves, (uint32_t)a.chunk), 1u << 13);
+    };
+    const uint32_t once = whole((total + a.round - 1) / a.round);
+    uint32_t chunk = once <= kShort ? once : 0;
+    for (int turn = 0; chunk == 0 && turn < 2 && a.B <= a.round; ++turn) {
+        const uint32_t longer = whole(turn == 0 ? once : once + once / 16);
+        uint32_t parts = lane < a.B ? parts_of(mine, longer) : 0u;
+        for (int b = 64 + lane; b < a.B + lane; b += 64)
+            parts += b < a.B ? parts_of(blocks_of(b), longer) : 0u;
+        if (wave_sum(parts) <= (uint32_t)a.round && 16u * (total / longer) >= 15u * a.round)
+            chunk = longer;
+    }
+    if (chunk == 0) chunk = whole((total + a.share - 1) / a.share);
     Unit r = {-1, 0, 0, (int)chunk, 0, 0, 0};
     uint32_t carry = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
         const uint32_t n = b0 == 0 ? mine : blocks_of(b0 + lane);
-        const uint32_t parts = b0 + lane < a.B ? max((n + chunk - 1) / chunk, 1u) : 0u;
+        const uint32_t parts = b0 + lane < a.B ? parts_of(n, chunk) : 0u;
         const uint32_t end = wave_scan(parts);
         const uint64_t past = __ballot(carry + end > (uint32_t)u);
         if (past != 0) {
@@ -636,7 +653,7 @@ hipError_t attn(const PagedAttn &p, const PagedPlan &plan, const void *Q, const 
     const AttnArgs a = {Q, Kp, Vp, O, LSE, (float *)(ws + plan.part), (float2 *)(ws + plan.stat),
                         plan.most > 1 ? (int2 *)(ws + plan.info) : nullptr, p.table, p.index, p.key_len, p.q_len,
                         p.B, p.H, p.G, p.Lq, p.P, p.N, p.shift, p.causal, p.keep,
-                        p.scale * kLog2e, plan.splits, plan.chunk, plan.share, plan.groups};
+                        p.scale * kLog2e, plan.splits, plan.chunk, plan.share, plan.round, plan.groups};
     const unsigned grid = (unsigned)((int64_t)plan.units * p.H * plan.groups);
     const auto run = [&](auto SPARSE, auto RT, auto TW, auto CACHE) {
         paged_attn<T, D, decltype(SPARSE)::value, decltype(RT)::value, decltype(TW)::value,
@@ -667,7 +684,7 @@ hipError_t join(const PagedAttn &p, const PagedPlan &plan, void *O, float *LSE, 
     const JoinArgs a = {O, LSE, (const float *)(ws + plan.part), (const float2 *)(ws + plan.stat),
                         sparse ? nullptr : (const int2 *)(ws + plan.info), p.H, p.G, p.Lq, rows,
                         plan.splits, (int)total};
-    if (plan.most <= 64)
+    if (plan.most <= 16)
         paged_join<T, D, 1><<<(unsigned)((total + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
     else
         paged_join<T, D, kWaves><<<(unsigned)total, kThreads, 0, s>>>(a);
