@@ -11,16 +11,16 @@ from ._kv4 import _call, _elem, _need
 
 
 def _room(workspace, need, dev, device, stream):
-    """The workspace to pass: the caller's, or one allocated here."""
+    """(pointer, bytes) of the workspace: the caller's, or one of need() bytes that
+    is allocated here (and kept by the third value)."""
     if workspace is None:
-        return _empty_bytes(need, device, stream) if need > 0 else None
-    if workspace.get_device() != dev or not workspace.is_contiguous():
+        nbytes = need()
+        if nbytes == 0:
+            return None, 0, None
+        workspace = _empty_bytes(nbytes, device, stream)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous and on cuda:%d" % dev)
-    return workspace
-
-
-def _bytes(workspace):
-    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.nbytes, workspace
 
 
 # -------------------------------------------------------------------- tables --
@@ -39,22 +39,17 @@ def mg_paged_resize(key_len, want, table, free_pages, free_count, new_len, new_c
         raise ValueError("table must be [B,P], free_pages [N] and slot [T]")
     B, P = table.shape
     N, T, dev, i32 = free_pages.shape[0], slot.shape[0], table.get_device(), torch.int32
-    _need(dev, (("table", table, i32, (B, P)), ("key_len", key_len, i32, (B,)),
-                ("want", want, i32, (B,)), ("free_pages", free_pages, i32, (N,)),
+    _need(dev, (("table", table, i32, None), ("key_len", key_len, i32, (B,)),
+                ("want", want, i32, (B,)), ("free_pages", free_pages, i32, None),
                 ("free_count", free_count, i32, (1,)), ("new_len", new_len, i32, (B,)),
-                ("new_count", new_count, i32, (1,)), ("slot", slot, i32, (T,)),
+                ("new_count", new_count, i32, (1,)), ("slot", slot, i32, None),
                 ("offset", offset, i32, (B + 1,))))
-    ws = _room(workspace, mg_paged_resize_workspace_bytes(B, T), dev, table.device, stream)
+    ws, nbytes, _kept = _room(workspace, lambda: mg_paged_resize_workspace_bytes(B, T), dev,
+                              table.device, stream)
     _call(dev, stream, load_library().mg_paged_resize, key_len.data_ptr(), want.data_ptr(),
           table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(), new_len.data_ptr(),
-          new_count.data_ptr(), slot.data_ptr(), offset.data_ptr(), B, page, P, N, T, _ptr(ws),
-          _bytes(ws))
-
-
-def _pools(Kp, Vp, dev, elem):
-    if Kp.dim() != 4:
-        raise ValueError("Kp must be [N,H,page,d]")
-    return (("Kp", Kp, elem, Kp.shape), ("Vp", Vp, elem, Kp.shape))
+          new_count.data_ptr(), slot.data_ptr(), offset.data_ptr(), B, page, P, N, T, ws,
+          nbytes)
 
 
 def mg_paged_append(K, V, Kp, Vp, slot, bounds=None, *, contract=FAST_BF16, stream=None):
@@ -64,14 +59,16 @@ def mg_paged_append(K, V, Kp, Vp, slot, bounds=None, *, contract=FAST_BF16, stre
     c = _contract_id(contract)
     if K.dim() != 3:
         raise ValueError("K must be [T,H,d]")
-    T, H, d = K.shape
+    if Kp.dim() != 4:
+        raise ValueError("Kp must be [N,H,page,d]")
+    rows, pool = K.shape, Kp.shape
+    (T, H, d), (N, _, page, _) = rows, pool
+    if pool[1] != H or pool[3] != d:
+        raise ValueError("Kp has shape %s, rows are [%d,%d,%d]" % (tuple(pool), T, H, d))
     dev, elem = K.get_device(), _elem(c)
-    pools = _pools(Kp, Vp, dev, elem)
-    N, page = Kp.shape[0], Kp.shape[2]
-    if Kp.shape[1] != H or Kp.shape[3] != d:
-        raise ValueError("Kp has shape %s, rows are [%d,%d,%d]" % (tuple(Kp.shape), T, H, d))
-    _need(dev, (("K", K, elem, K.shape), ("V", V, elem, K.shape), *pools,
-                ("slot", slot, torch.int32, (T,)), ("bounds", bounds, elem, (N, H, 2, d))))
+    _need(dev, (("K", K, elem, None), ("V", V, elem, rows), ("Kp", Kp, elem, None),
+                ("Vp", Vp, elem, pool), ("slot", slot, torch.int32, (T,)),
+                ("bounds", bounds, elem, (N, H, 2, d))))
     _call(dev, stream, load_library().mg_paged_append, K.data_ptr(), V.data_ptr(), Kp.data_ptr(),
           Vp.data_ptr(), _ptr(bounds), slot.data_ptr(), T, H, d, page, N, c)
 
@@ -92,26 +89,29 @@ def _attn(Q, Kp, Vp, table, key_len, q_len, index, O, LSE, c, workspace, stream)
     import torch
     if Q.dim() != 4 or table.dim() != 2:
         raise ValueError("Q must be [B,Hq,Lq,d] and table [B,P]")
-    B, Hq, Lq, d = Q.shape
-    dev, elem = Q.get_device(), _elem(c)
-    pools = _pools(Kp, Vp, dev, elem)
-    N, H, page, _ = Kp.shape
-    if Kp.shape[3] != d:
-        raise ValueError("Kp has shape %s, Q %s" % (tuple(Kp.shape), tuple(Q.shape)))
-    P, keep = table.shape[1], None
-    if index is not None:
-        if index.dim() != 4:
-            raise ValueError("index must be [B,H,Lq,keep]")
+    if Kp.dim() != 4:
+        raise ValueError("Kp must be [N,H,page,d]")
+    rows, pool = Q.shape, Kp.shape
+    (B, Hq, Lq, d), (N, H, page, _), (tables, P) = rows, pool, table.shape
+    if pool[3] != d:
+        raise ValueError("Kp has shape %s, Q %s" % (tuple(pool), tuple(rows)))
+    if tables != B:
+        raise ValueError("table has %d rows, Q %d sequences" % (tables, B))
+    if index is not None and index.dim() != 4:
+        raise ValueError("index must be [B,H,Lq,keep]")
+    dev, elem, i32 = Q.get_device(), _elem(c), torch.int32
+    _need(dev, (("Q", Q, elem, None), ("Kp", Kp, elem, None), ("Vp", Vp, elem, pool),
+                ("O", O, elem, rows), ("LSE", LSE, torch.float32, (B, Hq, Lq)),
+                ("table", table, i32, None), ("key_len", key_len, i32, (B,)),
+                ("q_len", q_len, i32, (B,))))
+    if index is None:
+        need = lambda: mg_attn_fwd_paged_workspace_bytes(B, Hq, H, Lq, d, page, P, c)
+    else:
         keep = index.shape[3]
-    _need(dev, (("Q", Q, elem, Q.shape), *pools, ("O", O, elem, Q.shape),
-                ("LSE", LSE, torch.float32, Q.shape[:3]), ("table", table, torch.int32, (B, P)),
-                ("key_len", key_len, torch.int32, (B,)), ("q_len", q_len, torch.int32, (B,)),
-                ("index", index, torch.int32, (B, H, Lq, keep))))
-    if workspace is None:
-        need = mg_attn_fwd_paged_workspace_bytes(B, Hq, H, Lq, d, page, P, c) if keep is None \
-            else mg_attn_fwd_paged_sparse_workspace_bytes(B, Hq, H, Lq, d, page, keep, c)
-    ws = _room(workspace, 0 if workspace is not None else need, dev, Q.device, stream)
-    return dev, (B, Hq, H, Lq, d, page, P, N), ws
+        _need(dev, (("index", index, i32, (B, H, Lq, keep)),))
+        need = lambda: mg_attn_fwd_paged_sparse_workspace_bytes(B, Hq, H, Lq, d, page, keep, c)
+    return (dev, (B, Hq, H, Lq, d, page, P, N),
+            _room(workspace, need, dev, Q.device if workspace is None else None, stream))
 
 
 def mg_attn_fwd_paged(Q, Kp, Vp, table, key_len, O, LSE, q_len=None, *, causal, scale,
@@ -120,10 +120,10 @@ def mg_attn_fwd_paged(Q, Kp, Vp, table, key_len, O, LSE, q_len=None, *, causal, 
     [B,P], into O and LSE [B,Hq,Lq].  `workspace` as for mg_attn_bwd (sized by
     mg_attn_fwd_paged_workspace_bytes; allocated here with torch when None)."""
     c = _contract_id(contract)
-    dev, sizes, ws = _attn(Q, Kp, Vp, table, key_len, q_len, None, O, LSE, c, workspace, stream)
+    dev, sizes, (ws, nbytes, _kept) = _attn(Q, Kp, Vp, table, key_len, q_len, None, O, LSE, c, workspace, stream)
     _call(dev, stream, load_library().mg_attn_fwd_paged, Q.data_ptr(), Kp.data_ptr(),
           Vp.data_ptr(), O.data_ptr(), LSE.data_ptr(), table.data_ptr(), key_len.data_ptr(),
-          _ptr(q_len), *sizes, 1 if causal else 0, scale, c, _ptr(ws), _bytes(ws))
+          _ptr(q_len), *sizes, 1 if causal else 0, scale, c, ws, nbytes)
 
 
 def mg_attn_fwd_paged_sparse(Q, Kp, Vp, table, key_len, index, O, LSE, q_len=None, *, causal,
@@ -131,11 +131,11 @@ def mg_attn_fwd_paged_sparse(Q, Kp, Vp, table, key_len, index, O, LSE, q_len=Non
     """As mg_attn_fwd_paged, where row i of cache head h sees the tokens of pages
     index[b,h,i] ([B,H,Lq,keep], ascending) only."""
     c = _contract_id(contract)
-    dev, sizes, ws = _attn(Q, Kp, Vp, table, key_len, q_len, index, O, LSE, c, workspace, stream)
+    dev, sizes, (ws, nbytes, _kept) = _attn(Q, Kp, Vp, table, key_len, q_len, index, O, LSE, c, workspace, stream)
     _call(dev, stream, load_library().mg_attn_fwd_paged_sparse, Q.data_ptr(), Kp.data_ptr(),
           Vp.data_ptr(), O.data_ptr(), LSE.data_ptr(), table.data_ptr(), index.data_ptr(),
           key_len.data_ptr(), _ptr(q_len), *sizes, 1 if causal else 0, index.shape[3], scale, c,
-          _ptr(ws), _bytes(ws))
+          ws, nbytes)
 
 
 # ----------------------------------------------------------------- selection --
@@ -154,17 +154,18 @@ def mg_paged_select(Q, bounds, table, key_len, index, q_len=None, *, page, causa
     if Q.dim() != 4 or table.dim() != 2 or bounds.dim() != 4 or index.dim() != 4:
         raise ValueError("Q must be [B,Hq,Lq,d], table [B,P], bounds [N,H,2,d] and index "
                          "[B,H,Lq,keep]")
-    B, Hq, Lq, d = Q.shape
-    N, H, P, keep = bounds.shape[0], bounds.shape[1], table.shape[1], index.shape[3]
+    (B, Hq, Lq, d), (N, H, _, _) = Q.shape, bounds.shape
+    P, keep, i32 = table.shape[1], index.shape[3], torch.int32
     dev, elem = Q.get_device(), _elem(c)
-    _need(dev, (("Q", Q, elem, Q.shape), ("bounds", bounds, elem, (N, H, 2, d)),
-                ("table", table, torch.int32, (B, P)), ("key_len", key_len, torch.int32, (B,)),
-                ("q_len", q_len, torch.int32, (B,)), ("index", index, torch.int32, (B, H, Lq, keep))))
-    ws = _room(workspace, 0 if workspace is not None else
-               mg_paged_select_workspace_bytes(B, Hq, H, Lq, d, page, P, c), dev, Q.device, stream)
+    _need(dev, (("Q", Q, elem, None), ("bounds", bounds, elem, (N, H, 2, d)),
+                ("table", table, i32, (B, P)), ("key_len", key_len, i32, (B,)),
+                ("q_len", q_len, i32, (B,)), ("index", index, i32, (B, H, Lq, keep))))
+    ws, nbytes, _kept = _room(
+        workspace, lambda: mg_paged_select_workspace_bytes(B, Hq, H, Lq, d, page, P, c), dev,
+        Q.device, stream)
     _call(dev, stream, load_library().mg_paged_select, Q.data_ptr(), bounds.data_ptr(),
           table.data_ptr(), key_len.data_ptr(), _ptr(q_len), index.data_ptr(), B, Hq, H, Lq, d,
-          page, P, N, 1 if causal else 0, keep, first, recent, c, _ptr(ws), _bytes(ws))
+          page, P, N, 1 if causal else 0, keep, first, recent, c, ws, nbytes)
 
 
 # ------------------------------------------------------------ conveniences --

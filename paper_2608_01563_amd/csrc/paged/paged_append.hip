@@ -74,6 +74,25 @@ struct Bounds {
         }
     }
     __device__ __forceinline__ void add(const Piece<T> &p) { join(p, p); }
+    // Over the lanes whose numbers differ by multiples of RL.
+    template <int RL>
+    __device__ __forceinline__ void join_lanes() {
+#pragma unroll
+        for (int e = 0; e < Piece<T>::kN; ++e) {
+            float h = hi.x[e], l = -lo.x[e];   // (the largest of both)
+            if (RL <= 4) h = fmaxf(h, rotated<0x124>(h)), l = fmaxf(l, rotated<0x124>(l));
+            if (RL <= 8) h = fmaxf(h, rotated<0x128>(h)), l = fmaxf(l, rotated<0x128>(l));
+            if (RL <= 16) h = max_xor16(h), l = max_xor16(l);
+            hi.x[e] = max_xor32(h);
+            lo.x[e] = -max_xor32(l);
+        }
+    }
+    // The value of the lane so many before in a row of 16.
+    template <int CONTROL>
+    __device__ __forceinline__ static float rotated(float v) {
+        return __int_as_float(
+            __builtin_amdgcn_update_dpp(0, __float_as_int(v), CONTROL, 0xf, 0xf, true));
+    }
     // With what the page's bounds were, unless the run begins it.
     __device__ __forceinline__ void write(char *at, int row_bytes, bool begun) {
         if (begun)
@@ -93,35 +112,50 @@ template <typename T, int D, int NI>
 __global__ __launch_bounds__(kThreads)
 void paged_append(AppendArgs a) {
     constexpr int RB = D * (int)sizeof(T), RL = RB / 16;   // lanes a row
-    constexpr int RPI = 64 / RL, R = RPI * NI;             // rows a read, rows a wave
+    constexpr int RPI = 64 / RL, R = RPI * NI;             // rows a read, rows at a time
     static_assert(R < 64, "a lane for every row's slot and the next one's");
     const int lane = threadIdx.x & 63, sub = lane / RL;
     const int64_t wave = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
     if (wave >= a.waves) return;
-    const int h = (int)(wave % a.H), t0 = (int)(wave / a.H) * R;
+    const int h = (int)(wave % a.H), t0 = __builtin_amdgcn_readfirstlane((int)(wave / a.H) * R);
     const int page = 1 << a.shift;
     const uint32_t slots = (uint32_t)a.N << a.shift;
     const size_t piece = (size_t)16 * (lane % RL);
+    const uint64_t mine = (1ull << R) - 1;
 
     const auto slot_of = [&](int t) { return t < a.T ? a.slot[t] : -1; };
-    const auto row_of = [&](const char *rows, int t) {
-        return *reinterpret_cast<const u32x4 *>(rows + ((size_t)t * a.H + h) * RB + piece);
+    const auto row_at = [&](const char *rows, int t) {
+        return reinterpret_cast<const u32x4 *>(rows + ((size_t)t * a.H + h) * RB + piece);
     };
-    // lane j <= R: the slot of row t0 + j, whether it goes on with the one before
+    // lane j: the slot of row t0 + j, whether it goes on with the one before
     const int slot = slot_of(t0 + lane);
-    const int before = t0 + lane > 0 ? slot_of(t0 + lane - 1) : -1;
+    const int first = t0 > 0 ? a.slot[t0 - 1] : -1;
+    const int shifted = __shfl_up(slot, 1, 64), before = lane == 0 ? first : shifted;
+    const bool good = (uint32_t)slot < slots;
+    // few rows do not wait for their slots; of many, those without one are not read.
+    // Rows are read past the caches (30 us instead of 36 for 168 MB, without bounds), but
+    // K of long pages, where a run's owner reads most rows a second time (pages of 64: 40
+    // us instead of 45 with bounds; of 16: 39 instead of 37).
+    if (NI > 1 && (__ballot(good) & mine) == 0) return;
     u32x4 k[NI], v[NI];
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
         const int t = min(t0 + i * RPI + sub, a.T - 1);
-        k[i] = row_of(a.K, t);
-        v[i] = row_of(a.V, t);
+        k[i] = a.shift < 6 ? __builtin_nontemporal_load(row_at(a.K, t)) : *row_at(a.K, t);
+        v[i] = __builtin_nontemporal_load(row_at(a.V, t));
     }
-    const bool good = (uint32_t)slot < slots;
     const bool on = good && (slot & (page - 1)) != 0 && before == slot - 1;
-    const uint64_t mine = (1ull << R) - 1;
     const uint64_t ons = __ballot(on), starts = __ballot(good && !on) & mine;
     const uint64_t singles = starts & ~(ons >> 1);
+    // the rows of the last run behind the wave's own, as far as slots are known: the
+    // first of them come with the own rows
+    const bool owner = a.bounds != nullptr && starts != 0;
+    const int behind = owner ? __builtin_ctzll(~(ons >> R)) : 0;
+    constexpr int NX = 4;
+    u32x4 x[NX];
+    if (behind > 0)
+#pragma unroll
+        for (int i = 0; i < NX; ++i) x[i] = *row_at(a.K, t0 + R + min(i * RPI + sub, behind - 1));
     // a head's rows in the pools, and its bounds
     const auto head_of = [&](int s) { return (size_t)(s >> a.shift) * a.H + h; };
     const auto bounds_of = [&](int s) { return a.bounds + head_of(s) * 2 * RB + piece; };
@@ -145,43 +179,40 @@ void paged_append(AppendArgs a) {
         const int s = __builtin_amdgcn_readlane(slot, from);
         // rows from .. end - 1 of the wave's, and those behind them
         const uint64_t rest = ~ons >> (from + 1);
-        int end = from + 1 + (rest == 0 ? 64 : __builtin_ctzll(rest));
-        const bool further = end > R;
-        end = min(end, R);
+        const int end = from + 1 + (rest == 0 ? 64 : __builtin_ctzll(rest));
         Bounds<T> b;
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
+            if (i * RPI >= end || (i + 1) * RPI <= from) continue;   // (so for all lanes)
             const int j = i * RPI + sub;
             if (j >= from && j < end) b.add(Piece<T>::of(k[i]));
         }
-        if (further)
-            for (int t = t0 + R;; t += 64) {
-                // how many of the next 64 rows are the run's
-                const int want = s + (t - t0 - from) + lane;
-                const bool same = (want >> a.shift) == (s >> a.shift) && slot_of(t + lane) == want;
-                const uint64_t other = ~__ballot(same);
-                const int count = other == 0 ? 64 : __builtin_ctzll(other);
-                constexpr int AT_ONCE = 4;
-                for (int j = sub; j < count; j += AT_ONCE * RPI) {
-                    u32x4 x[AT_ONCE];
+        if (end > R) {
 #pragma unroll
-                    for (int e = 0; e < AT_ONCE; ++e)   // (past the end the last row again)
-                        x[e] = row_of(a.K, t + min(j + e * RPI, count - 1));
-#pragma unroll
-                    for (int e = 0; e < AT_ONCE; ++e) b.add(Piece<T>::of(x[e]));
+            for (int i = 0; i < NX; ++i) b.add(Piece<T>::of(x[i]));
+            // what is left of a long page
+            for (int done = min(behind, NX * RPI), known = behind;;) {
+                if (done == known) {
+                    // how many of the next 64 rows are the run's
+                    if (R + known < 64) break;
+                    const int t = t0 + R + done, want = s + (t - t0 - from) + lane;
+                    const bool same = want >> a.shift == s >> a.shift && slot_of(t + lane) == want;
+                    const uint64_t other = ~__ballot(same);
+                    const int more = other == 0 ? 64 : __builtin_ctzll(other);
+                    if (more == 0) break;
+                    known += more;
                 }
-                if (count < 64) break;
-            }
+                constexpr int AT_ONCE = 8;
+                u32x4 y[AT_ONCE];
 #pragma unroll
-        for (int m = RL; m < 64; m *= 2) {
-            Piece<T> l, u;
+                for (int e = 0; e < AT_ONCE; ++e)   // (past the end the last row again)
+                    y[e] = *row_at(a.K, t0 + R + min(done + e * RPI + sub, known - 1));
 #pragma unroll
-            for (int e = 0; e < Piece<T>::kN; ++e) {
-                l.x[e] = xor_lanes(b.lo.x[e], m);
-                u.x[e] = xor_lanes(b.hi.x[e], m);
+                for (int e = 0; e < AT_ONCE; ++e) b.add(Piece<T>::of(y[e]));
+                done = min(done + AT_ONCE * RPI, known);
             }
-            b.join(l, u);
         }
+        b.template join_lanes<RL>();
         if (sub == 0) b.write(bounds_of(s), RB, (s & (page - 1)) != 0);
     }
 }
@@ -194,13 +225,14 @@ hipError_t append(const PagedAppend &p, AppendArgs a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Few rows: one read a wave, so that all compute units have some; many: as many as
-// keep their loads together.
+// Few rows: one read a wave, so that all compute units have some; many: 16 rows a
+// wave (with 32, whose registers leave room for fewer waves, pages of 16 take 43 us
+// instead of 39).
 template <typename T, int D>
 hipError_t append(const PagedAppend &p, const AppendArgs &a, hipStream_t s) {
     constexpr int RPI = 64 / (D * (int)sizeof(T) / 16);
     if ((int64_t)p.T * p.H <= 16384) return append<T, D, 1>(p, a, s);
-    return append<T, D, (32 / RPI > 8 ? 8 : 32 / RPI)>(p, a, s);
+    return append<T, D, (16 / RPI > 4 ? 4 : 16 / RPI > 1 ? 16 / RPI : 2)>(p, a, s);
 }
 
 }  // namespace
