@@ -108,7 +108,7 @@ struct Bounds {
     }
 };
 
-template <typename T, int D, int NI>
+template <typename T, int D, int NI, bool PAST>
 __global__ __launch_bounds__(kThreads)
 void paged_append(AppendArgs a) {
     constexpr int RB = D * (int)sizeof(T), RL = RB / 16;   // lanes a row
@@ -141,7 +141,8 @@ void paged_append(AppendArgs a) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
         const int t = min(t0 + i * RPI + sub, a.T - 1);
-        k[i] = a.shift < 6 ? __builtin_nontemporal_load(row_at(a.K, t)) : *row_at(a.K, t);
+        if constexpr (PAST) k[i] = __builtin_nontemporal_load(row_at(a.K, t));
+        else k[i] = *row_at(a.K, t);
         v[i] = __builtin_nontemporal_load(row_at(a.V, t));
     }
     const bool on = good && (slot & (page - 1)) != 0 && before == slot - 1;
@@ -217,11 +218,11 @@ void paged_append(AppendArgs a) {
     }
 }
 
-template <typename T, int D, int NI>
+template <typename T, int D, int NI, bool PAST>
 hipError_t append(const PagedAppend &p, AppendArgs a, hipStream_t s) {
     constexpr int R = 64 / (D * (int)sizeof(T) / 16) * NI;
     a.waves = (int64_t)((p.T + R - 1) / R) * p.H;
-    paged_append<T, D, NI><<<(unsigned)((a.waves + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
+    paged_append<T, D, NI, PAST><<<(unsigned)((a.waves + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -231,8 +232,10 @@ hipError_t append(const PagedAppend &p, AppendArgs a, hipStream_t s) {
 template <typename T, int D>
 hipError_t append(const PagedAppend &p, const AppendArgs &a, hipStream_t s) {
     constexpr int RPI = 64 / (D * (int)sizeof(T) / 16);
-    if ((int64_t)p.T * p.H <= 16384) return append<T, D, 1>(p, a, s);
-    return append<T, D, (16 / RPI > 4 ? 4 : 16 / RPI > 1 ? 16 / RPI : 2)>(p, a, s);
+    if ((int64_t)p.T * p.H <= 16384) return append<T, D, 1, false>(p, a, s);
+    constexpr int NI = 16 / RPI > 4 ? 4 : 16 / RPI > 1 ? 16 / RPI : 2;
+    return p.shift < 6 || a.bounds == nullptr ? append<T, D, NI, true>(p, a, s)
+                                              : append<T, D, NI, false>(p, a, s);
 }
 
 }  // namespace
