@@ -43,7 +43,7 @@ struct AttnArgs {
     int2 *info;   // nullptr: every sequence (sparse: row) is one unit, nothing to join
     const int32_t *table, *index, *key_len, *q_len;
     int B, H, G, Lq, P, N, shift, causal, keep;
-    float scale_log2;
+    float scale_log2, scale_rest;   // scale log2 e as two numbers
     int splits, chunk, share, round, groups;
 };
 
@@ -371,15 +371,15 @@ void paged_attn(AttnArgs a) {
             float top = -INFINITY;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                s[r][t] *= a.scale_log2;
+                const f32x4 x = s[r][t] * a.scale_log2;
                 if (partly) {
                     const int left = limit[r] - now[t].token - 4 * g;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (e >= left) s[r][t][e] = -INFINITY;
-                }
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, e < left ? x[e] : -INFINITY);
+                } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) top = fmaxf(top, s[r][t][e]);
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, x[e]);
+                }
             }
             top = fmaxf(m[r], max_over_groups(top));
             if (__any(top > m[r])) {
@@ -391,12 +391,23 @@ void paged_attn(AttnArgs a) {
             }
             const float from = m[r] == -INFINITY ? 0.f : m[r];
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int t = 0; t < NT; ++t) {
+                // (rounded as a difference, not as the larger product; f32: what the factor's
+                // rounding leaves of scores counts too, 4e-7 of p at a score of 20)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    s[r][t][e] = exp2_fast(s[r][t][e] - from);
-                    l[r] += s[r][t][e];
+                    float x = fmaf(s[r][t][e], a.scale_log2, -from);
+                    if constexpr (!S::kHalf) x = fmaf(s[r][t][e], a.scale_rest, x);
+                    s[r][t][e] = exp2_fast(x);
                 }
+                if (partly) {
+                    const int left = limit[r] - now[t].token - 4 * g;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[r][t][e] = e < left ? s[r][t][e] : 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) l[r] += s[r][t][e];
+            }
             operand[r].set(s[r]);
         }
 
@@ -650,10 +661,12 @@ void paged_join(JoinArgs a) {
 template <typename T, int D>
 hipError_t attn(const PagedAttn &p, const PagedPlan &plan, const void *Q, const void *Kp,
                 const void *Vp, void *O, float *LSE, char *ws, hipStream_t s) {
+    const double factor = p.scale * 1.4426950408889634;
     const AttnArgs a = {Q, Kp, Vp, O, LSE, (float *)(ws + plan.part), (float2 *)(ws + plan.stat),
                         plan.most > 1 ? (int2 *)(ws + plan.info) : nullptr, p.table, p.index, p.key_len, p.q_len,
                         p.B, p.H, p.G, p.Lq, p.P, p.N, p.shift, p.causal, p.keep,
-                        p.scale * kLog2e, plan.splits, plan.chunk, plan.share, plan.round, plan.groups};
+                        (float)factor,
+                        (float)(factor - (float)factor), plan.splits, plan.chunk, plan.share, plan.round, plan.groups};
     const unsigned grid = (unsigned)((int64_t)plan.units * p.H * plan.groups);
     const auto run = [&](auto SPARSE, auto RT, auto TW, auto CACHE) {
         paged_attn<T, D, decltype(SPARSE)::value, decltype(RT)::value, decltype(TW)::value,
