@@ -442,6 +442,9 @@ SELECT = [
     (1, 2, 1, 1, 64, 256, 20, [5000], None, True, 5, 3, 2),      # nothing left to choose
     (2, 4, 2, 2, 64, 16, 20, [320, 17], None, True, 40, 1, 1),   # room for more than there are
     (40, 2, 2, 1, 32, 16, 64, [25 * b for b in range(40)], None, True, 16, 1, 1),
+    (1, 16, 1, 2, 64, 16, 1024, [16384], None, True, 300, 1, 1),
+    (2, 12, 2, 5, 128, 32, 1100, [35200, 9000], [5, 3], True, 77, 2, 2),
+    (1, 3, 1, 3, 32, 16, 1500, [24000], None, True, 800, 0, 1),
 ]
 
 
