@@ -25,6 +25,7 @@ constexpr int64_t kCached = 64 << 20;   // bytes that caches may hold from call 
 constexpr int kLongest = 1 << 13; // blocks of a unit (2^18 tokens)
 
 void paged_workspace(PagedPlan &plan, const PagedAttn &p, int64_t rows) {
+    plan.join_waves = plan.most <= 16 ? 1 : 4;
     if (plan.most <= 1) return;
     const size_t slots = (size_t)plan.units * p.H * rows;
     plan.part = plan.bytes;
@@ -183,7 +184,9 @@ mg_status_t check_attn(const mg::PagedAttn &p, int Hq, int page, bool sparse,
     if (!std::isfinite(p.scale * kLog2e))
         return fail(MG_ERR_INVALID_ARGUMENT, "scale log2 e is not finite (scale %g)", p.scale);
     *plan = mg::paged_plan(p, sparse);
-    if ((int64_t)plan->units * p.H * plan->groups > kMaxGroups)
+    const int64_t joins = (int64_t)p.B * Hq * p.Lq * plan->join_waves / 4;
+    if ((int64_t)plan->units * p.H * plan->groups > kMaxGroups ||
+        (plan->most > 1 && joins >= kMaxGroups))
         return fail(MG_ERR_INVALID_ARGUMENT, "too much work for one call (B=%d H=%d Lq=%d P=%d)",
                     p.B, p.H, p.Lq, p.P);
     return MG_OK;

@@ -397,7 +397,11 @@ void paged_attn(AttnArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float x = fmaf(s[r][t][e], a.scale_log2, -from);
-                    if constexpr (!S::kHalf) x = fmaf(s[r][t][e], a.scale_rest, x);
+                    if constexpr (!S::kHalf) {   // (an infinite score is x already)
+                        const float finite =
+                            __builtin_amdgcn_fmed3f(s[r][t][e], -0x1.fffffep127f, 0x1.fffffep127f);
+                        x = fmaf(finite, a.scale_rest, x);
+                    }
                     s[r][t][e] = exp2_fast(x);
                 }
                 if (partly) {
@@ -697,7 +701,7 @@ hipError_t join(const PagedAttn &p, const PagedPlan &plan, void *O, float *LSE, 
     const JoinArgs a = {O, LSE, (const float *)(ws + plan.part), (const float2 *)(ws + plan.stat),
                         sparse ? nullptr : (const int2 *)(ws + plan.info), p.H, p.G, p.Lq, rows,
                         plan.splits, (int)total};
-    if (plan.most <= 16)
+    if (plan.join_waves == 1)
         paged_join<T, D, 1><<<(unsigned)((total + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
     else
         paged_join<T, D, kWaves><<<(unsigned)total, kThreads, 0, s>>>(a);

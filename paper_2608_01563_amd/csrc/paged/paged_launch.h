@@ -56,6 +56,7 @@ struct PagedPlan {
     int groups;    // workgroups of a unit and cache head
     bool once;     // K and V are read past the caches
     int most;      // units a sequence has at most
+    int join_waves;   // that join a row: 1 or 4
     size_t part, stat, info, bytes;   // workspace: offsets of the parts, size
 };
 PagedPlan paged_plan(const PagedAttn &p, bool sparse);

@@ -231,6 +231,8 @@ ATTN = [
     (2, 8, 8, 1, 64, 16, 130, [2000, 77], None, True),
     (1, 8, 2, 2, 128, 16, 400, [4999], None, True),        # many units of one sequence
     (5, 4, 2, 1, 128, 16, 70, [1100, 3, 0, 640, 64], None, True),
+    (1, 8, 2, 40, 64, 16, 40, [610], [37], True),          # 160 rows a cache head
+    (2, 80, 1, 1, 32, 64, 12, [700, 90], None, True),
     (70, 8, 4, 1, 64, 16, 40, [(37 * b) % 600 for b in range(70)], None, True),   # by lengths
     (3, 4, 4, 2, 32, 64, 900, [50000, 57600, 1], None, True),
     (2, 16, 1, 1, 128, 64, 2000, [90000, 128000], None, True),
@@ -304,6 +306,49 @@ def test_attention(gpu_lib, B, Hq, H, Lq, d, page, P, key_len, q_len, causal, co
     Kp, Vp = pooled(rng, N, H, page, d, contract)
     Q = rows(rng, (B, Hq, Lq, d), contract)
     check_attention(gpu_lib, Q, Kp, Vp, table, key_len, q_len, causal, d ** -0.5, contract)
+
+
+@pytest.mark.parametrize("contract", ["fast_bf16", "strict_f32"])
+@pytest.mark.parametrize("sparse", [False, True])
+def test_long_units(gpu_lib, contract, sparse):
+    """Units of several thousand tokens in pages of 16 (two sequences are checked)."""
+    say("paged attention long units %s sparse %s" % (contract, sparse))
+    rng = np.random.default_rng(12)
+    B, H, d, page, N = 12, 16, 128, 16, 60
+    P = 1400 if sparse else 2600
+    key_len = [P * page - 5 - (b % 3) for b in range(B)]
+    table = rng.integers(0, N, (B, P))
+    Kp, Vp = pooled(rng, N, H, page, d, contract)
+    Q = rows(rng, (B, H, 1, d), contract)
+    index = None
+    if sparse:
+        B = 64
+        table, key_len = np.tile(table, (6, 1))[:B], (key_len * 6)[:B]
+        Q = np.tile(Q, (6, 1, 1, 1))[:B]
+        index = np.sort(rng.permuted(np.tile(np.arange(P), (B, H, 1, 1)), axis=3)[..., :301], 3)
+    check_attention(gpu_lib, Q, Kp, Vp, table, key_len, None, True, d ** -0.5, contract, index,
+                    sequences=[0, 11])
+
+
+@pytest.mark.parametrize("contract", ["fast_bf16", "strict_f32"])
+def test_infinite_scores(gpu_lib, contract):
+    """Tokens whose score is -inf count as ones with no weight."""
+    say("paged attention infinite scores %s" % contract)
+    rng = np.random.default_rng(13)
+    N, table = table_of(rng, 1, 6, 16, [90])
+    Kp, Vp = pooled(rng, N, 1, 16, 64, contract)
+    Q = np.abs(rows(rng, (1, 3, 1, 64), contract))
+    whole = Kp.copy()
+    for j in (0, 17, 50, 89):
+        Kp[table[0, j // 16], 0, j % 16, 5] = -np.inf
+        whole[table[0, j // 16], 0, j % 16] = -60 / Q.min((0, 1, 2))   # as good as nothing
+    for scale in (0.125, 0.1):
+        out = [gpu_lib.attention_forward_paged(dev(Q, dtype_of(contract)), dev(k, dtype_of(contract)),
+                                               dev(Vp, dtype_of(contract)), ints(table), ints([90]),
+                                               causal=True, scale=scale) for k in (Kp, whole)]
+        # (exp(-60 * 64 / 10) is 0 in f32: the same sums)
+        for a, b in zip(*out):
+            assert np.array_equal(host(a), host(b))
 
 
 def test_accelerated_gives_the_strict_results(gpu_lib):

@@ -109,6 +109,8 @@ def test_queries_refuse_bad_sizes(lib, call, kwargs, status):
     (attn, dict(scale=float("inf")), 1), (attn, dict(scale=float("nan")), 1),
     (attn, dict(scale=3e38), 1), (attn, dict(P=1 << 12, ws=0), 4),
     (attn, dict(P=1 << 12, nbytes=64), 4), (attn, dict(B=1 << 14, H=32, Hq=32, P=1 << 16), 1),
+    (attn, dict(B=1 << 10, H=1 << 9, Hq=1 << 16, d=32, P=1 << 9), 1),   # rows to join
+    (sparse, dict(B=1 << 10, H=1 << 9, Hq=1 << 16, d=32, keep=512), 1),
     (sparse, dict(keep=0), 1), (sparse, dict(keep=1 << 21), 1),
     (sparse, dict(scale=float("nan")), 1), (sparse, dict(keep=999, ws=0), 4),
     (select, dict(keep=0), 1), (select, dict(first=-1), 1), (select, dict(recent=-1), 1),
