@@ -108,7 +108,7 @@ struct Bounds {
     }
 };
 
-template <typename T, int D, int NI, bool PAST>
+template <typename T, int D, int NI, bool OWN, bool PAST>
 __global__ __launch_bounds__(kThreads)
 void paged_append(AppendArgs a) {
     constexpr int RB = D * (int)sizeof(T), RL = RB / 16;   // lanes a row
@@ -132,110 +132,138 @@ void paged_append(AppendArgs a) {
     const int first = t0 > 0 ? a.slot[t0 - 1] : -1;
     const int shifted = __shfl_up(slot, 1, 64), before = lane == 0 ? first : shifted;
     const bool good = (uint32_t)slot < slots;
-    // few rows do not wait for their slots; of many, those without one are not read.
-    // Rows are read past the caches (30 us instead of 36 for 168 MB, without bounds), but
-    // K of long pages, where a run's owner reads most rows a second time (pages of 64: 40
-    // us instead of 45 with bounds; of 16: 39 instead of 37).
-    if (NI > 1 && (__ballot(good) & mine) == 0) return;
-    u32x4 k[NI], v[NI];
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-        const int t = min(t0 + i * RPI + sub, a.T - 1);
-        if constexpr (PAST) k[i] = __builtin_nontemporal_load(row_at(a.K, t));
-        else k[i] = *row_at(a.K, t);
-        v[i] = __builtin_nontemporal_load(row_at(a.V, t));
-    }
     const bool on = good && (slot & (page - 1)) != 0 && before == slot - 1;
-    const uint64_t ons = __ballot(on), starts = __ballot(good && !on) & mine;
+    const uint64_t goods = __ballot(good), ons = __ballot(on), starts = goods & ~ons & mine;
     const uint64_t singles = starts & ~(ons >> 1);
-    // the rows of the last run behind the wave's own, as far as slots are known: the
-    // first of them come with the own rows
-    const bool owner = a.bounds != nullptr && starts != 0;
-    const int behind = owner ? __builtin_ctzll(~(ons >> R)) : 0;
-    constexpr int NX = 4;
-    u32x4 x[NX];
-    if (behind > 0)
-#pragma unroll
-        for (int i = 0; i < NX; ++i) x[i] = *row_at(a.K, t0 + R + min(i * RPI + sub, behind - 1));
+    const auto end_of = [&](int from) {   // of the run that begins there, as far as is known
+        const uint64_t rest = ~ons >> from >> 1;
+        return from + 1 + (rest == 0 ? 64 : __builtin_ctzll(rest));
+    };
     // a head's rows in the pools, and its bounds
     const auto head_of = [&](int s) { return (size_t)(s >> a.shift) * a.H + h; };
     const auto bounds_of = [&](int s) { return a.bounds + head_of(s) * 2 * RB + piece; };
 
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-        const int j = i * RPI + sub, s = __shfl(slot, j, 64);
-        if ((uint32_t)s >= slots) continue;
-        const size_t to = ((head_of(s) << a.shift) + (s & (page - 1))) * RB + piece;
-        *reinterpret_cast<u32x4 *>(a.Kp + to) = k[i];
-        *reinterpret_cast<u32x4 *>(a.Vp + to) = v[i];
-        if (a.bounds != nullptr && (singles >> j & 1)) {
-            Bounds<T> b;
-            b.add(Piece<T>::of(k[i]));
-            b.write(bounds_of(s), RB, (s & (page - 1)) != 0);
-        }
+    // The rows that the wave moves.  Of many rows, those without a slot are not read (few
+    // do not wait for their slots).  Where pages have at most R rows, a wave moves the
+    // runs that begin among its rows, whole: no row is read twice.  In two parts where
+    // they are more than R, the last of them by itself.
+    int base = 0, count = R, second = -1;
+    if constexpr (OWN) {
+        if (starts == 0) return;
+        base = __builtin_ctzll(starts);
+        second = 63 - __builtin_clzll(starts);
+        count = end_of(second) - base;
+        if (count <= R) second = -1;
+        else count = second - base;
+    } else if (NI > 1 && (goods & mine) == 0) {
+        return;
     }
-    if (a.bounds == nullptr) return;
-    for (uint64_t left = starts & ~singles; left != 0; left &= left - 1) {
-        const int from = __builtin_ctzll(left);
-        const int s = __builtin_amdgcn_readlane(slot, from);
-        // rows from .. end - 1 of the wave's, and those behind them
-        const uint64_t rest = ~ons >> (from + 1);
-        const int end = from + 1 + (rest == 0 ? 64 : __builtin_ctzll(rest));
-        Bounds<T> b;
+    for (;;) {
+        u32x4 k[NI], v[NI];
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            if (i * RPI >= end || (i + 1) * RPI <= from) continue;   // (so for all lanes)
-            const int j = i * RPI + sub;
-            if (j >= from && j < end) b.add(Piece<T>::of(k[i]));
+            const int t = min(t0 + base + min(i * RPI + sub, count - 1), a.T - 1);
+            if constexpr (PAST) k[i] = __builtin_nontemporal_load(row_at(a.K, t));
+            else k[i] = *row_at(a.K, t);
+            v[i] = __builtin_nontemporal_load(row_at(a.V, t));
         }
-        if (end > R) {
+        // the rows of the last run behind the wave's own, as far as slots are known: the
+        // first of them come with the own rows
+        const int behind =
+            !OWN && a.bounds != nullptr && starts != 0 ? __builtin_ctzll(~(ons >> R)) : 0;
+        constexpr int NX = OWN ? 1 : 4;
+        u32x4 x[NX];
+        if (behind > 0)
 #pragma unroll
-            for (int i = 0; i < NX; ++i) b.add(Piece<T>::of(x[i]));
-            // what is left of a long page
-            for (int done = min(behind, NX * RPI), known = behind;;) {
-                if (done == known) {
-                    // how many of the next 64 rows are the run's
-                    if (R + known < 64) break;
-                    const int t = t0 + R + done, want = s + (t - t0 - from) + lane;
-                    const bool same = want >> a.shift == s >> a.shift && slot_of(t + lane) == want;
-                    const uint64_t other = ~__ballot(same);
-                    const int more = other == 0 ? 64 : __builtin_ctzll(other);
-                    if (more == 0) break;
-                    known += more;
-                }
-                constexpr int AT_ONCE = 8;
-                u32x4 y[AT_ONCE];
+            for (int i = 0; i < NX; ++i)
+                x[i] = *row_at(a.K, t0 + R + min(i * RPI + sub, behind - 1));
+
 #pragma unroll
-                for (int e = 0; e < AT_ONCE; ++e)   // (past the end the last row again)
-                    y[e] = *row_at(a.K, t0 + R + min(done + e * RPI + sub, known - 1));
-#pragma unroll
-                for (int e = 0; e < AT_ONCE; ++e) b.add(Piece<T>::of(y[e]));
-                done = min(done + AT_ONCE * RPI, known);
+        for (int i = 0; i < NI; ++i) {
+            const int j = base + i * RPI + sub, s = __shfl(slot, j, 64);
+            if (j >= base + count || (uint32_t)s >= slots) continue;
+            const size_t to = ((head_of(s) << a.shift) + (s & (page - 1))) * RB + piece;
+            *reinterpret_cast<u32x4 *>(a.Kp + to) = k[i];
+            *reinterpret_cast<u32x4 *>(a.Vp + to) = v[i];
+            if (a.bounds != nullptr && (singles >> j & 1)) {
+                Bounds<T> b;
+                b.add(Piece<T>::of(k[i]));
+                b.write(bounds_of(s), RB, (s & (page - 1)) != 0);
             }
         }
-        b.template join_lanes<RL>();
-        if (sub == 0) b.write(bounds_of(s), RB, (s & (page - 1)) != 0);
+        if (a.bounds == nullptr) return;
+        const uint64_t here = (count == 64 ? ~0ull : (1ull << count) - 1) << base;
+        for (uint64_t left = starts & ~singles & here; left != 0; left &= left - 1) {
+            const int from = __builtin_ctzll(left), end = end_of(from);
+            const int s = __builtin_amdgcn_readlane(slot, from);
+            Bounds<T> b;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                if (base + i * RPI >= end || base + (i + 1) * RPI <= from) continue;   // (uniform)
+                const int j = base + i * RPI + sub;
+                if (j >= from && j < end) b.add(Piece<T>::of(k[i]));
+            }
+            if (!OWN && end > R) {
+#pragma unroll
+                for (int i = 0; i < NX; ++i) b.add(Piece<T>::of(x[i]));
+                // what is left of a long page
+                for (int done = min(behind, NX * RPI), known = behind;;) {
+                    if (done == known) {
+                        // how many of the next 64 rows are the run's
+                        if (R + known < 64) break;
+                        const int t = t0 + R + done, want = s + (t - t0 - from) + lane;
+                        const bool same =
+                            want >> a.shift == s >> a.shift && slot_of(t + lane) == want;
+                        const uint64_t other = ~__ballot(same);
+                        const int more = other == 0 ? 64 : __builtin_ctzll(other);
+                        if (more == 0) break;
+                        known += more;
+                    }
+                    constexpr int AT_ONCE = 8;
+                    u32x4 y[AT_ONCE];
+#pragma unroll
+                    for (int e = 0; e < AT_ONCE; ++e)   // (past the end the last row again)
+                        y[e] = *row_at(a.K, t0 + R + min(done + e * RPI + sub, known - 1));
+#pragma unroll
+                    for (int e = 0; e < AT_ONCE; ++e) b.add(Piece<T>::of(y[e]));
+                    done = min(done + AT_ONCE * RPI, known);
+                }
+            }
+            b.template join_lanes<RL>();
+            if (sub == 0) b.write(bounds_of(s), RB, (s & (page - 1)) != 0);
+        }
+        if (!OWN || second < 0) return;
+        base = second;
+        count = end_of(second) - second;
+        second = -1;
     }
 }
 
-template <typename T, int D, int NI, bool PAST>
+template <typename T, int D, int NI, bool OWN, bool PAST>
 hipError_t append(const PagedAppend &p, AppendArgs a, hipStream_t s) {
     constexpr int R = 64 / (D * (int)sizeof(T) / 16) * NI;
     a.waves = (int64_t)((p.T + R - 1) / R) * p.H;
-    paged_append<T, D, NI, PAST><<<(unsigned)((a.waves + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
+    paged_append<T, D, NI, OWN, PAST>
+        <<<(unsigned)((a.waves + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 
-// Few rows: one read a wave, so that all compute units have some; many: 16 rows a
-// wave (with 32, whose registers leave room for fewer waves, pages of 16 take 43 us
-// instead of 39).
+// Few rows: one read a wave, so that all compute units have some.  Many: pages of 16
+// and 32 by waves of as many rows, which move whole runs (20,480 rows of 8 heads of 128
+// bf16 channels into pages of 16: 33 us; 37 where a run's owner reads on behind its
+// rows); longer ones by waves of 16 rows (40 us for pages of 64; a wave of 32 has
+// registers for fewer waves: 43).  Rows are read past the caches (30 us instead of 36
+// without bounds), but K of long pages, of which most rows are read a second time (40
+// instead of 45).
 template <typename T, int D>
 hipError_t append(const PagedAppend &p, const AppendArgs &a, hipStream_t s) {
     constexpr int RPI = 64 / (D * (int)sizeof(T) / 16);
-    if ((int64_t)p.T * p.H <= 16384) return append<T, D, 1, false>(p, a, s);
     constexpr int NI = 16 / RPI > 4 ? 4 : 16 / RPI > 1 ? 16 / RPI : 2;
-    return p.shift < 6 || a.bounds == nullptr ? append<T, D, NI, true>(p, a, s)
-                                              : append<T, D, NI, false>(p, a, s);
+    if ((int64_t)p.T * p.H <= 16384) return append<T, D, 1, false, false>(p, a, s);
+    if (a.bounds == nullptr) return append<T, D, NI, false, true>(p, a, s);
+    if (p.shift == 4) return append<T, D, 16 / RPI, true, true>(p, a, s);
+    if (p.shift == 5) return append<T, D, 32 / RPI, true, true>(p, a, s);
+    return append<T, D, NI, false, false>(p, a, s);
 }
 
 }  // namespace

@@ -64,13 +64,25 @@ __device__ __forceinline__ void pages_and_slots(const PagedResize &p, const Reco
         const int at = available - 1 - k;
         return at < count ? p.free_pages[at] : given(at - count);
     };
+    // pages given back: the first M are on their way while slots are found
+    const int pushed = min(back, p.N - count);
+    int x[M], b[M], id[M];
+    const auto read = [&](int k) {
+#pragma unroll
+        for (int e = 0; e < M; ++e) x[e] = min(k + e * step, pushed - 1);
+        find(r.back_end, p.B, x, b);
+#pragma unroll
+        for (int e = 0; e < M; ++e) id[e] = p.table[entry_of(b[e], x[e])];
+    };
+    if (first < pushed) read(first);
+
     const int rows = r.row_end[p.B - 1], page = 1 << p.shift;
     for (int t = first; t < p.T; t += step) {
         int slot = -1;
         if (t < rows) {
-            const int x[1] = {t};
+            const int at_row[1] = {t};
             int found[1];
-            find(r.row_end, p.B, x, found);
+            find(r.row_end, p.B, at_row, found);
             const int b = found[0], base = r.base[b];
             if (base >= 0) {
                 const int len = r.len[b], have = (len + page - 1) >> p.shift;
@@ -84,14 +96,8 @@ __device__ __forceinline__ void pages_and_slots(const PagedResize &p, const Reco
         }
         p.slot[t] = slot;
     }
-    const int pushed = min(back, p.N - count);
     for (int k = first; k < pushed; k += M * step) {
-        int x[M], b[M], id[M];
-#pragma unroll
-        for (int e = 0; e < M; ++e) x[e] = min(k + e * step, pushed - 1);
-        find(r.back_end, p.B, x, b);
-#pragma unroll
-        for (int e = 0; e < M; ++e) id[e] = p.table[entry_of(b[e], x[e])];
+        if (k > first) read(k);
 #pragma unroll
         for (int e = 0; e < M; ++e)
             if (k + e * step < pushed) p.free_pages[count + k + e * step] = id[e];
