@@ -331,19 +331,21 @@ void paged_attn(AttnArgs a) {
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                s[r][t] = zero4();
+                // (two sums for f32, whose roundings are what a score is off by)
+                f32x4 sum[2] = {zero4(), zero4()};
 #pragma unroll
                 for (int y = 0; y < S::kPieces; ++y) {
                     if constexpr (S::kHalf) {
-                        s[r][t] = mfma16x16x32bf16(__builtin_bit_cast(bf16x8, x.k[t][y]),
-                                                   __builtin_bit_cast(bf16x8, q[r][y]), s[r][t]);
+                        sum[0] = mfma16x16x32bf16(__builtin_bit_cast(bf16x8, x.k[t][y]),
+                                                  __builtin_bit_cast(bf16x8, q[r][y]), sum[0]);
                     } else {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            s[r][t] = mfma16x16x4(__uint_as_float(x.k[t][y][e]),
-                                                  __uint_as_float(q[r][y][e]), s[r][t]);
+                            sum[e % 2] = mfma16x16x4(__uint_as_float(x.k[t][y][e]),
+                                                     __uint_as_float(q[r][y][e]), sum[e % 2]);
                     }
                 }
+                s[r][t] = S::kHalf ? sum[0] : sum[0] + sum[1];
             }
         // the next block's K comes while this one's scores are worked on (behind
         // the last block: descriptors of no bytes)
