@@ -43,15 +43,22 @@ PagedPlan paged_plan(const PagedAttn &p, bool sparse) {
     const int64_t groups = (int64_t)p.H * plan.groups;   // workgroups of a unit
     const int64_t cut = std::max<int64_t>(1, (plan.rows == 16 ? kWant : kWantMore) / groups);
     const int64_t round = std::max<int64_t>(1, kRound / groups);
-    const int64_t pages = std::min<int64_t>(p.N, (int64_t)p.B * (sparse ? p.Lq * p.keep : p.P));
+    const int64_t pages = std::min<int64_t>(
+        p.N, (int64_t)p.B * (sparse ? (int64_t)p.Lq * p.keep : p.P));
     plan.once = (pages << p.shift) * p.H * p.d * (p.half ? 4 : 8) > kCached;
+    // what is no more than two (f32) or four blocks a wave is one unit, which needs no
+    // joining (500 tokens: 8.8 us instead of 10.7; f32 16.4 instead of 10.8)
+    const int64_t held = (int64_t)(sparse ? p.keep : p.P) << p.shift;
+    const int tokens = p.half ? 512 : p.d == 128 ? 128 : 256;
+    const int blocks = (int)((held + 31) / 32);
+    const int least = held <= tokens ? tokens / 32 : kLeast;
     if (sparse) {
         // lists are short of their `keep` pages only where sequences are: units are all
         // alike, and one round of them will do.
         // A unit has at most 64 pages, whose entries a wave holds.
-        const int blocks = (int)(((int64_t)p.keep << p.shift) + 31) / 32;
         const int64_t seqs = (int64_t)p.B * p.Lq;
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>(round / seqs, blocks / (2 * kLeast)));
+        const int64_t want = std::max<int64_t>(
+            1, std::min<int64_t>(round / seqs, cdiv(blocks, least)));
         plan.chunk = (cdiv(blocks, (int)want) + 3) / 4 * 4;
         plan.chunk = std::min(plan.chunk, 2 << p.shift);
         plan.splits = cdiv(blocks, plan.chunk);
@@ -60,11 +67,7 @@ PagedPlan paged_plan(const PagedAttn &p, bool sparse) {
         paged_workspace(plan, p, rows);
         return plan;
     }
-    const int blocks = (int)((((int64_t)p.P << p.shift) + 31) / 32);
-    // tables of no more than two (f32) or four blocks a wave are one unit, which needs no
-    // joining (500 tokens: 8.8 us instead of 10.7; f32 16.4 instead of 10.8)
-    const int tokens = p.half ? 512 : p.d == 128 ? 128 : 256;
-    plan.chunk = blocks * 32 <= tokens ? tokens / 32 : kLeast;
+    plan.chunk = least;
     const int full = cdiv(blocks, plan.chunk);
     if ((int64_t)p.B * full <= round) {
         plan.splits = full;
