@@ -76,6 +76,7 @@ PagedPlan paged_plan(const PagedAttn &p, bool sparse) {
     } else {
         plan.share = (int)cut;
         plan.round = (int)round;
+        plan.round_most = (int)(plan.rows == 16 ? round + round / 2 : round);
         plan.units = (int)std::max<int64_t>(cut + p.B, (int64_t)p.B * cdiv(blocks, kLongest));
         plan.most = std::max(std::min(full, (int)cut), cdiv(blocks, kLongest));
     }

@@ -44,7 +44,7 @@ struct AttnArgs {
     const int32_t *table, *index, *key_len, *q_len;
     int B, H, G, Lq, P, N, shift, causal, keep;
     float scale_log2, scale_rest;   // scale log2 e as two numbers
-    int splits, chunk, share, round, groups;
+    int splits, chunk, share, round, round_most, groups;
 };
 
 // One unit: blocks [first, first + count) of sequence b (sparse: of row i's list);
@@ -54,17 +54,19 @@ struct Unit {
 };
 
 // Which sequence unit u belongs to where lengths decide: every sequence is cut
-// into units of `chunk` blocks (at least one unit each).  Of 8 cache heads, in us:
+// into units of `chunk` blocks at most, at least one unit each and all of a sequence
+// alike.  Of 8 cache heads, in us, by the workgroups that the lengths are cut into:
 //
-//                                       workgroups:  512   768  1024  1536
-//   8 sequences of 16,384 to 65,536 tokens, 1 row    230   190   194   186
-//   32 of 1,024 to 4,096, 1 row                       72    67    63    63
-//   4 of 32,768, 1 row                                85    87    86    93
-//   8 of 1,000 to 4,001, 28 rows                      27          35    35
+//                                                    384   512   768  1536
+//   8 sequences of 16,384 to 65,536 tokens, 1 row    219   180   179   190
+//   32 of 1,024 to 4,096, 1 row                             63    60    63
+//   4 of 32,768, 1 row                               101    86    87    92
+//   8 of 1,000 to 4,001, 28 rows                      31    27    35    35
 //
-// So: about `round` units (two workgroups a compute unit, all at once) where that
-// fills them to 15 in 16, or where they are so short that a second round costs more
-// than it evens out; `share` (more rounds) otherwise.
+// So: one round, two workgroups a compute unit or (where three fit) three, if units of
+// some length, at most a third longer than would do without remainders, make no more
+// of them and fill them to 13 in 16, or if they are short; `share` units, several
+// rounds, otherwise.
 __device__ __forceinline__ Unit unit_by_length(const AttnArgs &a, int u, int lane) {
     const int capacity = a.P << a.shift;
     const auto blocks_of = [&](int b) {
@@ -75,21 +77,28 @@ __device__ __forceinline__ Unit unit_by_length(const AttnArgs &a, int u, int lan
     for (int b = 64 + lane; b < a.B + lane; b += 64) total += blocks_of(b);
     total = wave_sum(total);
     const auto parts_of = [](uint32_t n, uint32_t chunk) { return max((n + chunk - 1) / chunk, 1u); };
-    const auto whole = [&](uint32_t chunk) {   // of streams, within the bounds
-        return min(max((chunk + kWaves - 1) / kWaves * kWaves, (uint32_t)a.chunk), 1u << 13);
-    };
+    const auto whole = [&](uint32_t chunk) { return min(max(chunk, (uint32_t)a.chunk), 1u << 13); };
     const uint32_t once = whole((total + a.round - 1) / a.round);
-    uint32_t chunk = once <= kShort ? once : 0;
-    for (int turn = 0; chunk == 0 && turn < 2 && a.B <= a.round; ++turn) {
-        const uint32_t longer = whole(turn == 0 ? once : once + once / 16);
-        uint32_t parts = lane < a.B ? parts_of(mine, longer) : 0u;
-        for (int b = 64 + lane; b < a.B + lane; b += 64)
-            parts += b < a.B ? parts_of(blocks_of(b), longer) : 0u;
-        if (wave_sum(parts) <= (uint32_t)a.round && 16u * (total / longer) >= 15u * a.round)
-            chunk = longer;
+    uint32_t chunk = 0;
+    for (int round = a.round; round <= a.round_most && a.B <= round; round += a.round / 2) {
+        const uint32_t least = whole((total + round - 1) / round);
+        for (uint32_t turn = 0; chunk == 0 && turn < 6; ++turn) {
+            const uint32_t longer = whole(least + least * turn / 16);
+            if (once > kShort && (uint64_t)16 * total < (uint64_t)13 * round * longer) break;
+            // (a quotient that rounds to one more or less changes the cut, not its sense)
+            const float inverse = __builtin_amdgcn_rcpf((float)longer);
+            const auto about = [&](uint32_t n) {
+                return max((uint32_t)ceilf((float)n * inverse), 1u);
+            };
+            uint32_t parts = lane < a.B ? about(mine) : 0u;
+            for (int b = 64 + lane; b < a.B + lane; b += 64)
+                parts += b < a.B ? about(blocks_of(b)) : 0u;
+            if (wave_sum(parts) <= (uint32_t)round) chunk = longer;
+        }
+        if (chunk != 0 || a.round < 2) break;
     }
-    if (chunk == 0) chunk = whole((total + a.share - 1) / a.share);
-    Unit r = {-1, 0, 0, (int)chunk, 0, 0, 0};
+    if (chunk == 0) chunk = once <= kShort ? once : whole((total + a.share - 1) / a.share);
+    Unit r = {-1, 0, 0, 0, 0, 0, 0};
     uint32_t carry = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
         const uint32_t n = b0 == 0 ? mine : blocks_of(b0 + lane);
@@ -102,7 +111,9 @@ __device__ __forceinline__ Unit unit_by_length(const AttnArgs &a, int u, int lan
             r.splits = __builtin_amdgcn_readlane(parts, at);
             r.base = carry + __builtin_amdgcn_readlane(end, at) - r.splits;
             r.split = u - r.base;
-            r.first = r.split * (int)chunk;
+            // (its units are all alike, so that none is left with a few blocks)
+            r.count = (__builtin_amdgcn_readlane(n, at) + r.splits - 1) / r.splits;
+            r.first = r.split * r.count;
             return r;
         }
         carry += __builtin_amdgcn_readlane(end, 63);
@@ -672,7 +683,8 @@ hipError_t attn(const PagedAttn &p, const PagedPlan &plan, const void *Q, const 
                         plan.most > 1 ? (int2 *)(ws + plan.info) : nullptr, p.table, p.index, p.key_len, p.q_len,
                         p.B, p.H, p.G, p.Lq, p.P, p.N, p.shift, p.causal, p.keep,
                         (float)factor,
-                        (float)(factor - (float)factor), plan.splits, plan.chunk, plan.share, plan.round, plan.groups};
+                        (float)(factor - (float)factor), plan.splits, plan.chunk, plan.share, plan.round,
+                        plan.round_most, plan.groups};
     const unsigned grid = (unsigned)((int64_t)plan.units * p.H * plan.groups);
     const auto run = [&](auto SPARSE, auto RT, auto TW, auto CACHE) {
         paged_attn<T, D, decltype(SPARSE)::value, decltype(RT)::value, decltype(TW)::value,

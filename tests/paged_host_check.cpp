@@ -101,14 +101,13 @@ int main() {
                                 } else {
                                     // as the kernel cuts them, whatever the lengths
                                     EXPECT(!sparse && q.share >= 1 && q.round >= 1 &&
-                                           q.round <= q.share);
+                                           q.round <= q.round_most && q.round_most <= q.share);
                                     for (int64_t n : {(int64_t)0, (int64_t)1, blocks / 3, blocks}) {
                                         const int64_t total = n * B;
                                         for (int64_t share : {q.share, q.round}) {
                                             int64_t chunk = (total + share - 1) / share;
                                             chunk = std::min<int64_t>(
-                                                std::max<int64_t>((chunk + 3) / 4 * 4, q.chunk),
-                                                1 << 13);
+                                                std::max<int64_t>(chunk, q.chunk), 1 << 13);
                                             const int64_t parts =
                                                 std::max<int64_t>((n + chunk - 1) / chunk, 1);
                                             EXPECT(parts * B <= q.units && parts <= q.most);
