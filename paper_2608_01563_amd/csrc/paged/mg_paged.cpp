@@ -67,21 +67,31 @@ PagedPlan paged_plan(const PagedAttn &p, bool sparse) {
         paged_workspace(plan, p, rows);
         return plan;
     }
+    const int full = cdiv(blocks, least), longest = cdiv(blocks, kLongest);
     plan.chunk = least;
-    const int full = cdiv(blocks, plan.chunk);
-    if ((int64_t)p.B * full <= round) {
-        plan.splits = full;
+    plan.most = std::max(std::min(full, (int)cut), longest);   // a cut sequence's units
+    if (plan.most == 1) {
+        plan.splits = 1;
+        plan.chunk = std::max(blocks, least);
+        plan.units = p.B;
+    } else if ((int64_t)p.B * full <= round) {
+        plan.splits = plan.most = full;
         plan.units = p.B * full;
-        plan.most = full;
     } else {
         plan.share = (int)cut;
         plan.round = (int)round;
         plan.round_most = (int)(plan.rows == 16 ? round + round / 2 : round);
-        plan.units = (int)std::max<int64_t>(cut + p.B, (int64_t)p.B * cdiv(blocks, kLongest));
-        plan.most = std::max(std::min(full, (int)cut), cdiv(blocks, kLongest));
+        plan.units = (int)std::max<int64_t>(cut + p.B, (int64_t)p.B * longest);
+        plan.lengths = p.B > kPagedScanned;
     }
-    plan.info = plan.bytes;
-    plan.bytes += plan.most > 1 ? host::round256((size_t)p.B * 8) : 0;
+    if (plan.most > 1) {
+        plan.info = plan.bytes;
+        plan.bytes += host::round256((size_t)p.B * 8);
+    }
+    if (plan.lengths) {
+        plan.map = plan.bytes;
+        plan.bytes += host::round256((size_t)plan.units * 4);
+    }
     paged_workspace(plan, p, rows);
     return plan;
 }
@@ -219,6 +229,10 @@ mg_status_t attn_call(const mg::PagedAttn &p, int Hq, int page, bool sparse, con
                       {{p.table, "table"}, {p.key_len, "key_len"}},
                       {{p.q_len, "q_len"}, {sparse ? p.index : nullptr, "index"},
                        {ws, "workspace"}}, 4));
+    if (plan.lengths)
+        MG_TRY(run_kernel("paged_cut", stream, [&] {
+            return mg::launch_paged_cut(p, plan, workspace, stream);
+        }));
     MG_TRY(run_kernel("paged_attn", stream, [&] {
         return mg::launch_paged_attn(p, plan, Q, Kp, Vp, O, LSE, workspace, stream);
     }));

@@ -35,27 +35,9 @@ constexpr int kOnce = 2;   // cache policy: non-temporal
 constexpr uint32_t kShort = 24;   // blocks of a unit
 constexpr int kFar = 1 << 30;   // a token that no row sees
 
-struct AttnArgs {
-    const void *Q, *Kp, *Vp;
-    void *O;
-    float *LSE, *part;
-    float2 *stat;
-    int2 *info;   // nullptr: every sequence (sparse: row) is one unit, nothing to join
-    const int32_t *table, *index, *key_len, *q_len;
-    int B, H, G, Lq, P, N, shift, causal, keep;
-    float scale_log2, scale_rest;   // scale log2 e as two numbers
-    int splits, chunk, share, round, round_most, groups;
-};
-
-// One unit: blocks [first, first + count) of sequence b (sparse: of row i's list);
-// its sequence has `splits` units, the first of them number `base`.
-struct Unit {
-    int b, i, first, count, splits, base, split;
-};
-
-// Which sequence unit u belongs to where lengths decide: every sequence is cut
-// into units of `chunk` blocks at most, at least one unit each and all of a sequence
-// alike.  Of 8 cache heads, in us, by the workgroups that the lengths are cut into:
+// Where lengths decide, every sequence is cut into units of `chunk` blocks at most, at
+// least one unit each and all of a sequence alike (so that none is left with a few
+// blocks).  Of 8 cache heads, in us, by the workgroups that the lengths are cut into:
 //
 //                                                    384   512   768  1536
 //   8 sequences of 16,384 to 65,536 tokens, 1 row    219   180   179   190
@@ -67,58 +49,134 @@ struct Unit {
 // some length, at most a third longer than would do without remainders, make no more
 // of them and fill them to 13 in 16, or if they are short; `share` units, several
 // rounds, otherwise.
-__device__ __forceinline__ Unit unit_by_length(const AttnArgs &a, int u, int lane) {
-    const int capacity = a.P << a.shift;
-    const auto blocks_of = [&](int b) {
-        return b < a.B ? (uint32_t)(key_limit(a.key_len, b, capacity) + 31) / 32 : 0u;
-    };
-    const uint32_t mine = blocks_of(lane);
-    uint32_t total = mine;
-    for (int b = 64 + lane; b < a.B + lane; b += 64) total += blocks_of(b);
-    total = wave_sum(total);
-    const auto parts_of = [](uint32_t n, uint32_t chunk) { return max((n + chunk - 1) / chunk, 1u); };
-    const auto whole = [&](uint32_t chunk) { return min(max(chunk, (uint32_t)a.chunk), 1u << 13); };
-    const uint32_t once = whole((total + a.round - 1) / a.round);
+__device__ __forceinline__ uint32_t parts_of(uint32_t blocks, uint32_t chunk) {
+    return max((blocks + chunk - 1) / chunk, 1u);
+}
+struct Cut {
+    int least, share, round, round_most;   // as PagedPlan's chunk, share, round, round_most
+
+    __device__ __forceinline__ uint32_t within(uint32_t chunk) const {
+        return min(max(chunk, (uint32_t)least), 1u << 13);
+    }
+    __device__ __forceinline__ uint32_t once(uint32_t total) const {
+        return within((total + round - 1) / round);
+    }
+    __device__ __forceinline__ uint32_t rounds(uint32_t total) const {
+        return once(total) <= kShort ? once(total) : within((total + share - 1) / share);
+    }
+};
+
+struct AttnArgs {
+    const void *Q, *Kp, *Vp;
+    void *O;
+    float *LSE, *part;
+    float2 *stat;
+    int2 *info;   // nullptr: every sequence (sparse: row) is one unit, nothing to join
+    const int32_t *table, *index, *key_len, *q_len;
+    int B, H, G, Lq, P, N, shift, causal, keep;
+    float scale_log2, scale_rest;   // scale log2 e as two numbers
+    const int32_t *unit_of;   // many sequences: each unit's
+    int splits, chunk, groups;
+    Cut cut;
+};
+
+// One unit: blocks [first, first + count) of sequence b (sparse: of row i's list);
+// its sequence has `splits` units, the first of them number `base`.
+struct Unit {
+    int b, i, first, count, splits, base, split;
+};
+
+// Which sequence unit u belongs to; at most 64 M sequences, M a lane.
+template <int M>
+__device__ __forceinline__ Unit unit_by_length(const AttnArgs &a, const Cut &cut, int u, int lane) {
+    uint32_t n[M], mine = 0;
+#pragma unroll
+    for (int e = 0; e < M; ++e) {
+        const int b = M * lane + e;
+        n[e] = b < a.B ? (uint32_t)(key_limit(a.key_len, b, a.P << a.shift) + 31) / 32 : 0u;
+        mine += n[e];
+    }
+    const uint32_t total = wave_sum(mine), once = cut.once(total);
     uint32_t chunk = 0;
-    for (int round = a.round; round <= a.round_most && a.B <= round; round += a.round / 2) {
-        const uint32_t least = whole((total + round - 1) / round);
+    for (int round = cut.round; round <= cut.round_most && a.B <= round; round += cut.round / 2) {
+        const uint32_t least = cut.within((total + round - 1) / round);
         for (uint32_t turn = 0; chunk == 0 && turn < 6; ++turn) {
-            const uint32_t longer = whole(least + least * turn / 16);
+            const uint32_t longer = cut.within(least + least * turn / 16);
             if (once > kShort && (uint64_t)16 * total < (uint64_t)13 * round * longer) break;
             // (a quotient that rounds to one more or less changes the cut, not its sense)
             const float inverse = __builtin_amdgcn_rcpf((float)longer);
-            const auto about = [&](uint32_t n) {
-                return max((uint32_t)ceilf((float)n * inverse), 1u);
-            };
-            uint32_t parts = lane < a.B ? about(mine) : 0u;
-            for (int b = 64 + lane; b < a.B + lane; b += 64)
-                parts += b < a.B ? about(blocks_of(b)) : 0u;
+            uint32_t parts = 0;
+#pragma unroll
+            for (int e = 0; e < M; ++e)
+                if (M * lane + e < a.B) parts += max((uint32_t)ceilf((float)n[e] * inverse), 1u);
             if (wave_sum(parts) <= (uint32_t)round) chunk = longer;
         }
-        if (chunk != 0 || a.round < 2) break;
+        if (chunk != 0 || cut.round < 2) break;
     }
-    if (chunk == 0) chunk = once <= kShort ? once : whole((total + a.share - 1) / a.share);
-    Unit r = {-1, 0, 0, 0, 0, 0, 0};
-    uint32_t carry = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const uint32_t n = b0 == 0 ? mine : blocks_of(b0 + lane);
-        const uint32_t parts = b0 + lane < a.B ? parts_of(n, chunk) : 0u;
-        const uint32_t end = wave_scan(parts);
-        const uint64_t past = __ballot(carry + end > (uint32_t)u);
-        if (past != 0) {
-            const int at = __builtin_ctzll(past);
-            r.b = b0 + at;
-            r.splits = __builtin_amdgcn_readlane(parts, at);
-            r.base = carry + __builtin_amdgcn_readlane(end, at) - r.splits;
-            r.split = u - r.base;
-            // (its units are all alike, so that none is left with a few blocks)
-            r.count = (__builtin_amdgcn_readlane(n, at) + r.splits - 1) / r.splits;
-            r.first = r.split * r.count;
-            return r;
+    if (chunk == 0) chunk = cut.rounds(total);
+    uint32_t parts[M], sum = 0;
+#pragma unroll
+    for (int e = 0; e < M; ++e) {
+        parts[e] = M * lane + e < a.B ? parts_of(n[e], chunk) : 0u;
+        sum += parts[e];
+    }
+    const uint32_t end = wave_scan(sum);
+    const uint64_t past = __ballot(end > (uint32_t)u);
+    if (past == 0) return {-1, 0, 0, 0, 0, 0, 0};
+    const int l = __builtin_ctzll(past);
+    int base = __builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(sum, l);
+#pragma unroll
+    for (int e = 0; e < M; ++e) {
+        const int splits = __builtin_amdgcn_readlane(parts[e], l);
+        if (e == M - 1 || base + splits > u) {
+            const int count = (__builtin_amdgcn_readlane(n[e], l) + splits - 1) / splits;
+            return {M * l + e, 0, (u - base) * count, count, splits, base, u - base};
         }
-        carry += __builtin_amdgcn_readlane(end, 63);
+        base += splits;
     }
-    return r;
+    return {-1, 0, 0, 0, 0, 0, 0};
+}
+
+// More than kPagedScanned sequences: a workgroup writes for every sequence its first unit and
+// how many it has, and for every unit its sequence (-1 behind the last).  It takes 5 us;
+// with it and with lengths that every unit scans, of up to 1,000 tokens and 2 cache heads:
+// 1,024 sequences 127 and 141 us, 500 73 and 79; of 8 heads, 100: 59 and 57.
+constexpr int kCutThreads = 1024;
+__global__ __launch_bounds__(kCutThreads)
+void paged_cut(const int32_t *key_len, int B, int capacity, int units, Cut cut, int2 *info,
+               int32_t *unit_of) {
+    __shared__ uint32_t sums[2][kCutThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const auto blocks_of = [&](int b) {
+        return b < B ? (uint32_t)(key_limit(key_len, b, capacity) + 31) / 32 : 0u;
+    };
+    const auto all_of = [&](uint32_t v, uint32_t *to) {   // of the waves' sums, those before
+        if (lane == 63) to[w] = v;
+        __syncthreads();
+        uint32_t before = 0, all = 0;
+        for (int k = 0; k < kCutThreads / 64; ++k) {
+            before += k < w ? to[k] : 0u;
+            all += to[k];
+        }
+        return make_uint2(before, all);
+    };
+    uint32_t total = 0;
+    for (int b = tid; b < B; b += kCutThreads) total += blocks_of(b);
+    total = all_of(wave_scan(total), sums[0]).y;
+    const uint32_t chunk = cut.rounds(total);
+    uint32_t carry = 0;
+    for (int b0 = 0, turn = 1; b0 < B; b0 += kCutThreads, ++turn) {
+        const int b = b0 + tid;
+        const uint32_t parts = b < B ? parts_of(blocks_of(b), chunk) : 0u, end = wave_scan(parts);
+        const uint2 others = all_of(end, sums[turn & 1]);
+        const int base = carry + others.x + end - parts;
+        if (b < B) {
+            info[b] = make_int2(base, parts);
+            for (int k = 0; k < (int)parts && base + k < units; ++k) unit_of[base + k] = b;
+        }
+        carry += others.y;
+    }
+    for (int u = carry + tid; u < units; u += kCutThreads) unit_of[u] = -1;
 }
 
 template <typename T, int D>
@@ -231,15 +289,26 @@ void paged_attn(AttnArgs a) {
         un.splits = a.splits;
         un.count = a.chunk;
         un.first = un.split * a.chunk;
+    } else if (a.unit_of != nullptr) {
+        un = {__builtin_amdgcn_readfirstlane(a.unit_of[u]), 0, 0, 0, 0, 0, 0};
+        if (un.b < 0) return;
+        const int2 its = a.info[un.b];
+        un.base = its.x;
+        un.splits = its.y;
+        un.split = u - its.x;
     } else {
-        un = unit_by_length(a, u, lane);
+        un = a.B <= 64 ? unit_by_length<1>(a, a.cut, u, lane) : unit_by_length<4>(a, a.cut, u, lane);
         if (un.b < 0) return;
     }
     const PagedMask mask =
         paged_mask(a.key_len, a.q_len, un.b, a.P << a.shift, a.Lq, a.causal);
     if (a.splits > 0 && !SPARSE)   // units behind the sequence's end are none
         un.splits = max(1, min(a.splits, ((mask.n + 31) / 32 + a.chunk - 1) / a.chunk));
-    if (!SPARSE && a.info != nullptr && h == 0 && group == 0 && un.split == 0 && tid == 0)
+    if (!SPARSE && a.unit_of != nullptr) {
+        un.count = ((mask.n + 31) / 32 + un.splits - 1) / un.splits;
+        un.first = un.split * un.count;
+    }
+    if (!SPARSE && a.unit_of == nullptr && a.info != nullptr && h == 0 && group == 0 && un.split == 0 && tid == 0)
         a.info[un.b] = make_int2(un.base, un.splits);
     if (un.split >= un.splits) return;
 
@@ -675,6 +744,10 @@ void paged_join(JoinArgs a) {
     if (lane == 0) a.LSE[to] = sum != sum ? sum : row_lse(top, sum);
 }
 
+Cut cut_of(const PagedPlan &plan) {
+    return {plan.chunk, plan.share, plan.round, plan.round_most};
+}
+
 template <typename T, int D>
 hipError_t attn(const PagedAttn &p, const PagedPlan &plan, const void *Q, const void *Kp,
                 const void *Vp, void *O, float *LSE, char *ws, hipStream_t s) {
@@ -683,8 +756,9 @@ hipError_t attn(const PagedAttn &p, const PagedPlan &plan, const void *Q, const 
                         plan.most > 1 ? (int2 *)(ws + plan.info) : nullptr, p.table, p.index, p.key_len, p.q_len,
                         p.B, p.H, p.G, p.Lq, p.P, p.N, p.shift, p.causal, p.keep,
                         (float)factor,
-                        (float)(factor - (float)factor), plan.splits, plan.chunk, plan.share, plan.round,
-                        plan.round_most, plan.groups};
+                        (float)(factor - (float)factor), plan.lengths ? (const int32_t *)(ws + plan.map)
+                                                                : nullptr,
+                        plan.splits, plan.chunk, plan.groups, cut_of(plan)};
     const unsigned grid = (unsigned)((int64_t)plan.units * p.H * plan.groups);
     const auto run = [&](auto SPARSE, auto RT, auto TW, auto CACHE) {
         paged_attn<T, D, decltype(SPARSE)::value, decltype(RT)::value, decltype(TW)::value,
@@ -723,6 +797,13 @@ hipError_t join(const PagedAttn &p, const PagedPlan &plan, void *O, float *LSE, 
 }
 
 }  // namespace
+
+hipError_t launch_paged_cut(const PagedAttn &p, const PagedPlan &plan, void *ws, hipStream_t s) {
+    char *w = static_cast<char *>(ws);
+    paged_cut<<<1, kCutThreads, 0, s>>>(p.key_len, p.B, p.P << p.shift, plan.units, cut_of(plan),
+                                        (int2 *)(w + plan.info), (int32_t *)(w + plan.map));
+    return hipGetLastError();
+}
 
 hipError_t launch_paged_attn(const PagedAttn &p, const PagedPlan &plan, const void *Q,
                              const void *Kp, const void *Vp, void *O, float *LSE, void *ws,

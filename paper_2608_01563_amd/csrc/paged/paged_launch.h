@@ -43,6 +43,8 @@ inline int64_t paged_rows(const PagedAttn &p, bool sparse) {
     return sparse ? p.G : (int64_t)p.G * p.Lq;
 }
 
+constexpr int kPagedScanned = 256;   // sequences whose lengths every wave can scan
+
 // How one call runs: every sequence (sparse: every query row) is cut into units
 // of the same number of blocks of 32 tokens, each a workgroup for every cache
 // head and so many of the rows that share it.
@@ -57,10 +59,12 @@ struct PagedPlan {
     bool once;     // K and V are read past the caches
     int most;      // units a sequence has at most
     int join_waves;   // that join a row: 1 or 4
-    size_t part, stat, info, bytes;   // workspace: offsets of the parts, size
+    bool lengths;     // the units are found by a kernel of their own
+    size_t part, stat, info, map, bytes;   // workspace: offsets of the parts, size
 };
 PagedPlan paged_plan(const PagedAttn &p, bool sparse);
 
+hipError_t launch_paged_cut(const PagedAttn &p, const PagedPlan &plan, void *ws, hipStream_t s);
 hipError_t launch_paged_attn(const PagedAttn &p, const PagedPlan &plan, const void *Q,
                              const void *Kp, const void *Vp, void *O, float *LSE, void *ws,
                              hipStream_t s);

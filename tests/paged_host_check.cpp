@@ -35,6 +35,9 @@ hipError_t launch_paged_resize(const PagedResize &, void *, hipStream_t) { retur
 hipError_t launch_paged_slots(const PagedResize &, const void *, hipStream_t) { return reached(); }
 hipError_t launch_paged_append(const PagedAppend &, const void *, const void *, void *, void *, void *,
                                bool, hipStream_t) { return reached(); }
+hipError_t launch_paged_cut(const PagedAttn &, const PagedPlan &, void *, hipStream_t) {
+    return reached();
+}
 hipError_t launch_paged_attn(const PagedAttn &, const PagedPlan &, const void *, const void *,
                              const void *, void *, float *, void *, hipStream_t) { return reached(); }
 hipError_t launch_paged_join(const PagedAttn &, const PagedPlan &, void *, float *, const void *,
@@ -92,7 +95,7 @@ int main() {
                                 const int64_t blocks = (((int64_t)P << shift) + 31) / 32;
                                 EXPECT(q.rows * (int64_t)q.groups >= rows);
                                 EXPECT(q.rows == 16 || q.rows == 32 || q.rows == 64 || q.rows == 128);
-                                EXPECT(q.chunk >= 4 && q.chunk % 4 == 0 && q.chunk <= 1 << 13);
+                                EXPECT(q.chunk >= 4 && q.chunk <= 1 << 13);
                                 const int64_t seqs = (int64_t)B * (sparse ? Lq : 1);
                                 if (q.splits > 0) {
                                     EXPECT((int64_t)q.splits * q.chunk >= blocks);
@@ -120,11 +123,17 @@ int main() {
                                         EXPECT(q.info == 0);
                                         at = (size_t)B * 8;
                                     }
+                                    EXPECT(q.lengths == (q.splits == 0 && B > mg::kPagedScanned));
+                                    EXPECT(q.splits != 0 || q.most > 1);
+                                    if (q.lengths) {
+                                        EXPECT(q.map >= at);
+                                        at = q.map + (size_t)q.units * 4;
+                                    }
                                     const size_t slots = (size_t)q.units * H * rows;
                                     EXPECT(q.part >= at && q.stat >= q.part + slots * 32 * 4 &&
                                            q.bytes >= q.stat + slots * 8);
                                 }
-                                EXPECT(q.most > 1 || q.bytes == 0);
+                                EXPECT(q.most > 1 || (q.bytes == 0 && !q.lengths && q.splits == 1));
                             }
     EXPECT(mg_attn_fwd_paged(p, p, p, p, f, n32, n32, n32, 1, 4, 2, 1, 64, 16, 4, 9, 1, std::nanf(""),
                              fast, nullptr, 0, nullptr) == MG_ERR_INVALID_ARGUMENT);

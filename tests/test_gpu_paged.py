@@ -236,6 +236,11 @@ ATTN = [
     (70, 8, 4, 1, 64, 16, 40, [(37 * b) % 600 for b in range(70)], None, True),   # by lengths
     (3, 4, 4, 2, 32, 64, 900, [50000, 57600, 1], None, True),
     (2, 16, 1, 1, 128, 64, 2000, [90000, 128000], None, True),
+    (700, 2, 1, 1, 32, 16, 700, [(b * 7919) % 90 if b != 333 else 11000 for b in range(700)], None,
+     True),
+    (65, 8, 8, 3, 64, 64, 40, [2560 - 30 * b for b in range(65)], None, True),
+    (256, 2, 1, 1, 32, 16, 130, [(b * 7919) % 2080 for b in range(256)], None, True),
+    (257, 2, 1, 1, 32, 16, 130, [(b * 7919) % 2080 for b in range(257)], None, True),
     (130, 2, 2, 1, 32, 32, 33, [1056 - 8 * b for b in range(130)], None, False),
 ]
 
