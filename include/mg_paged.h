@@ -116,8 +116,8 @@ mg_status_t mg_paged_append(const void *K, const void *V, void *Kp, void *Vp, vo
  * hold), get O = 0 and LSE = -inf.  Tokens that a row does not see have no part
  * in it, whatever their slots hold.
  *
- * Made for one new token or a few: 16 of the rows that share a cache head
- * (Hq/H * Lq) are worked on at once, and the cache is read anew for the next 16.
+ * Made for one new token or a few: up to 128 of the rows that share a cache head
+ * (Hq/H * Lq) are worked on at once, and the cache is read anew for the next 128.
  */
 mg_status_t mg_attn_fwd_paged(const void *Q, const void *Kp, const void *Vp, void *O, float *LSE,
                               const int32_t *table, const int32_t *key_len, const int32_t *q_len,
@@ -146,6 +146,7 @@ size_t mg_attn_fwd_paged_workspace_bytes(int B, int Hq, int H, int Lq, int d, in
  * leaves them: a sum in which 0 meets an infinite one is NaN.  A page without an
  * entry in [0, N) counts as NaN.)
  *   index  int32 [B][H][Lq][keep]: pages j / page, ascending; -1 behind the last
+ * B*H*Lq*P and B*H*Lq*keep at most 2^29.
  */
 mg_status_t mg_paged_select(const void *Q, const void *bounds, const int32_t *table,
                             const int32_t *key_len, const int32_t *q_len, int32_t *index,
@@ -161,6 +162,7 @@ size_t mg_paged_select_workspace_bytes(int B, int Hq, int H, int Lq, int d, int 
  * mg_attn_fwd_paged where row i of cache head h sees, of its tokens, those of
  * the pages index[b][h][i][0..keep) only.  The list ascends: an entry that is not
  * above the one before it (a repeated one) and one outside [0, P) are skipped.
+ * keep*page at most 2^24.
  */
 mg_status_t mg_attn_fwd_paged_sparse(const void *Q, const void *Kp, const void *Vp, void *O,
                                      float *LSE, const int32_t *table, const int32_t *index,

@@ -262,10 +262,10 @@ mg_status_t check_select(const mg::PagedSelect &p, int Hq, int page, mg_contract
         return fail(MG_ERR_INVALID_ARGUMENT,
                     "keep must be >= 1, first and recent >= 0 and together at most keep (keep=%d "
                     "first=%d recent=%d)", p.keep, p.first, p.recent);
-    if ((int64_t)p.B * p.H * p.Lq * p.P > 1 << 29 || (int64_t)p.B * p.H * p.Lq * p.keep > INT32_MAX)
+    if ((int64_t)p.B * p.H * p.Lq * std::max(p.P, p.keep) > 1 << 29)
         return fail(MG_ERR_INVALID_ARGUMENT,
-                    "too many scores (B=%d H=%d Lq=%d P=%d keep=%d): B*H*Lq*P at most 2^29, "
-                    "B*H*Lq*keep below 2^31", p.B, p.H, p.Lq, p.P, p.keep);
+                    "too many scores (B=%d H=%d Lq=%d P=%d keep=%d): B*H*Lq*P and B*H*Lq*keep at "
+                    "most 2^29", p.B, p.H, p.Lq, p.P, p.keep);
     return MG_OK;
 }
 

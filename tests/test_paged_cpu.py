@@ -122,6 +122,14 @@ def test_queries_refuse_bad_arguments(lib, call, kwargs, status):
     assert mg.mg_last_error_detail() != ""
 
 
+def test_lists_that_a_row_could_not_count_are_refused(lib):
+    # (a workgroup's threads go on from keep - 1 by up to 1,024)
+    assert select(lib, Hq=1, H=1, keep=(1 << 31) - 1) == 1
+    assert "too many scores" in mg.mg_last_error_detail()
+    assert select(lib, Hq=1, H=1, keep=1 << 29) == 1   # in range: only the pointers are none
+    assert "too many scores" not in mg.mg_last_error_detail()
+
+
 @pytest.mark.parametrize("call,wide,narrow,optional", [
     (resize, (), range(9), ()), (append, (0, 1, 2, 3), (5,), (4,)),
     (attn, range(5), (5, 6), (7,)), (sparse, range(5), (5, 6, 7), (8,)),
