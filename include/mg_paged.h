@@ -38,7 +38,7 @@
  *
  * Sizes: d in {32, 64, 128}; N*page below 2^31; P*page at most 2^24 and B*P*page
  * at most 2^35; B at most 2^16 and B*H*Lq at most 2^19; H*page*d below 2^28;
- * B*Hq*Lq*d below 2^31.
+ * B*Hq*Lq*d below 2^31.  Attention that would need 2^24 workgroups is refused.
  */
 #ifndef MG_PAGED_H
 #define MG_PAGED_H

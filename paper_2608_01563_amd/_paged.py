@@ -120,7 +120,8 @@ def mg_attn_fwd_paged(Q, Kp, Vp, table, key_len, O, LSE, q_len=None, *, causal, 
     [B,P], into O and LSE [B,Hq,Lq].  `workspace` as for mg_attn_bwd (sized by
     mg_attn_fwd_paged_workspace_bytes; allocated here with torch when None)."""
     c = _contract_id(contract)
-    dev, sizes, (ws, nbytes, _kept) = _attn(Q, Kp, Vp, table, key_len, q_len, None, O, LSE, c, workspace, stream)
+    dev, sizes, (ws, nbytes, _kept) = _attn(Q, Kp, Vp, table, key_len, q_len, None, O, LSE, c,
+                                            workspace, stream)
     _call(dev, stream, load_library().mg_attn_fwd_paged, Q.data_ptr(), Kp.data_ptr(),
           Vp.data_ptr(), O.data_ptr(), LSE.data_ptr(), table.data_ptr(), key_len.data_ptr(),
           _ptr(q_len), *sizes, 1 if causal else 0, scale, c, ws, nbytes)
@@ -131,7 +132,8 @@ def mg_attn_fwd_paged_sparse(Q, Kp, Vp, table, key_len, index, O, LSE, q_len=Non
     """As mg_attn_fwd_paged, where row i of cache head h sees the tokens of pages
     index[b,h,i] ([B,H,Lq,keep], ascending) only."""
     c = _contract_id(contract)
-    dev, sizes, (ws, nbytes, _kept) = _attn(Q, Kp, Vp, table, key_len, q_len, index, O, LSE, c, workspace, stream)
+    dev, sizes, (ws, nbytes, _kept) = _attn(Q, Kp, Vp, table, key_len, q_len, index, O, LSE, c,
+                                            workspace, stream)
     _call(dev, stream, load_library().mg_attn_fwd_paged_sparse, Q.data_ptr(), Kp.data_ptr(),
           Vp.data_ptr(), O.data_ptr(), LSE.data_ptr(), table.data_ptr(), index.data_ptr(),
           key_len.data_ptr(), _ptr(q_len), *sizes, 1 if causal else 0, index.shape[3], scale, c,

@@ -1,10 +1,10 @@
 // paged_attn.hip -- attention of a few query rows over a paged cache.
 //
-// A workgroup takes one cache head, 16 of the rows that share it and one unit: a
-// stretch of a sequence's tokens (or of the pages that a row's list names).  Its
-// four waves take blocks of 32 tokens (f32, d = 128: 16) in turn, each with its
-// own online softmax, and join through LDS; units of one sequence join in
-// paged_join.
+// A workgroup takes one cache head, 16 to 128 of the rows that share it and one unit:
+// a stretch of a sequence's tokens (or of the pages that a row's list names).  Its
+// four waves, or the two or one of them that have the same up to 32 rows, take blocks
+// of 32 tokens (f32, d = 128: 16) in turn, each with its own online softmax, and join
+// through LDS; units of one sequence join in paged_join.
 //
 // No operand passes through LDS.  A score tile is S^T = K Q^T: lane (c, g) = (l %
 // 16, l / 16) holds 16-byte pieces 4 s + g of token c's K row and of row c's Q row,
@@ -308,7 +308,8 @@ void paged_attn(AttnArgs a) {
         un.count = ((mask.n + 31) / 32 + un.splits - 1) / un.splits;
         un.first = un.split * un.count;
     }
-    if (!SPARSE && a.unit_of == nullptr && a.info != nullptr && h == 0 && group == 0 && un.split == 0 && tid == 0)
+    if (!SPARSE && a.unit_of == nullptr && a.info != nullptr && h == 0 && group == 0 &&
+        un.split == 0 && tid == 0)
         a.info[un.b] = make_int2(un.base, un.splits);
     if (un.split >= un.splits) return;
 
@@ -753,12 +754,11 @@ hipError_t attn(const PagedAttn &p, const PagedPlan &plan, const void *Q, const 
                 const void *Vp, void *O, float *LSE, char *ws, hipStream_t s) {
     const double factor = p.scale * 1.4426950408889634;
     const AttnArgs a = {Q, Kp, Vp, O, LSE, (float *)(ws + plan.part), (float2 *)(ws + plan.stat),
-                        plan.most > 1 ? (int2 *)(ws + plan.info) : nullptr, p.table, p.index, p.key_len, p.q_len,
-                        p.B, p.H, p.G, p.Lq, p.P, p.N, p.shift, p.causal, p.keep,
-                        (float)factor,
-                        (float)(factor - (float)factor), plan.lengths ? (const int32_t *)(ws + plan.map)
-                                                                : nullptr,
-                        plan.splits, plan.chunk, plan.groups, cut_of(plan)};
+                        plan.most > 1 ? (int2 *)(ws + plan.info) : nullptr, p.table, p.index,
+                        p.key_len, p.q_len, p.B, p.H, p.G, p.Lq, p.P, p.N, p.shift, p.causal,
+                        p.keep, (float)factor, (float)(factor - (float)factor),
+                        plan.lengths ? (const int32_t *)(ws + plan.map) : nullptr, plan.splits,
+                        plan.chunk, plan.groups, cut_of(plan)};
     const unsigned grid = (unsigned)((int64_t)plan.units * p.H * plan.groups);
     const auto run = [&](auto SPARSE, auto RT, auto TW, auto CACHE) {
         paged_attn<T, D, decltype(SPARSE)::value, decltype(RT)::value, decltype(TW)::value,

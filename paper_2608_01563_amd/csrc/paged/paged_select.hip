@@ -40,7 +40,8 @@ void paged_scores(ScoreArgs a) {
     const int c = lane & 3, block = lane >> 2 & 3, k = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     // (turned, so that the first parts, which all sequences have, are not on the same XCDs)
-    const int at = blockIdx.x / a.parts, part = (blockIdx.x % a.parts + 3 * (at % a.parts)) % a.parts;
+    const int at = blockIdx.x / a.parts;
+    const int part = (blockIdx.x % a.parts + 3 * (at % a.parts)) % a.parts;
     const int tile = at % a.tiles, bh = at / a.tiles;
     const int b = bh / a.H, h = bh - b * a.H;
     const int p0 = (part * kWaves + w) * 16;
@@ -107,7 +108,7 @@ void paged_scores(ScoreArgs a) {
     }
     const int il = a.G > 4 ? 0 : c / a.G;
     // the largest over a row's heads, which are c of the same k and block
-    if (a.G == 2 || a.G > 2) best = fmaxf(best, other_lane<0>(best));
+    if (a.G > 1) best = fmaxf(best, other_lane<0>(best));
     if (a.G > 2) best = fmaxf(best, other_lane<1>(best));
     const int p = p0 + 4 * block + k;
     const bool page_known = __shfl((int)known, 4 * block + k, 64);

@@ -89,7 +89,8 @@ class Session:
 SESSIONS = [dict(seed=1), dict(seed=2, Lq=5, d=128, contract="strict_f32", page=32),
             dict(seed=3, B=2, Hq=12, H=1, n=3000, room=9000, d=128, page=64, keep=20),
             dict(seed=4, B=70, Hq=4, H=2, n=60, room=200, d=32, Lq=2),
-            dict(seed=5, B=1, Hq=16, H=1, n=9000, room=20000, Lq=3, page=256, keep=9)]
+            dict(seed=5, B=1, Hq=16, H=1, n=9000, room=20000, Lq=3, page=256, keep=9),
+            dict(seed=8, B=300, Hq=4, H=2, n=700, room=1000, d=32)]
 
 
 def expected(s):
@@ -150,6 +151,43 @@ def test_sessions_captured_in_a_graph(gpu_lib):
         torch.cuda.synchronize()
         for k, (s, w) in enumerate(zip(sessions, want)):
             assert same(s.outputs(), w), (rep, k)
+
+
+@pytest.mark.parametrize("B", [100, 300])
+def test_captured_attention_follows_the_lengths_of_many_sequences(gpu_lib, B):
+    """Units that every wave finds, and that a kernel writes down, are the replay's."""
+    import torch
+    mg = gpu_lib
+    say("paged: captured attention of %d sequences" % B)
+    rng = np.random.default_rng(22)
+    Hq, H, d, page, P = 2, 1, 32, 16, 300
+    N = B * P // 8
+    Kp, Vp = (randn(rng, N, H, page, d) for _ in range(2))
+    Q = randn(rng, B, Hq, 1, d)
+    table = ints(*rng.integers(0, N, B * P)).view(B, P)
+    length, O, LSE = ints(*[0] * B), torch.empty_like(Q), torch.empty(B, Hq, 1, device="cuda")
+    ws = torch.empty(mg.mg_attn_fwd_paged_workspace_bytes(B, Hq, H, 1, d, page, P),
+                     dtype=torch.uint8, device="cuda")
+    call = lambda O, LSE, ws: mg.mg_attn_fwd_paged(Q, Kp, Vp, table, length, O, LSE, causal=True,
+                                                   scale=0.2, workspace=ws)
+    call(O, LSE, ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, capture_error_mode="relaxed"):
+        call(O, LSE, ws)
+    for most in (4800, 1, 900, 0, 4800):
+        n = rng.integers(0, most + 1, B)
+        n[rng.integers(B)] = most
+        length.copy_(ints(*n))
+        O.fill_(math.nan)
+        LSE.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [O.clone(), LSE.clone()]
+        call(O, LSE, None)
+        torch.cuda.synchronize()
+        assert same(got, [O, LSE]), most
+        assert bool((torch.isinf(LSE[:, 0, 0]) == (length == 0)).all())
+        assert bool(torch.isfinite(O).all())
 
 
 def test_a_captured_step_follows_the_lengths(gpu_lib):
