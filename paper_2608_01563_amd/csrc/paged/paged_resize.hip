@@ -199,10 +199,11 @@ void paged_resize(PagedResize p, Records r) {
         back_before += backs;
         need_before += all;
     }
-    // pages taken: up to the last granted sequence's
+    // pages taken: up to the last granted sequence's (part[0] was read before the last
+    // scan's barrier; part[1] and part[2] are read behind it)
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) took_before = max(took_before, __shfl_xor(took_before, m, 64));
-    if ((tid & 63) == 0) part[2][tid >> 6] = took_before;
+    if ((tid & 63) == 0) part[0][tid >> 6] = took_before;
     const int available = (int)min((int64_t)count + back_total, (int64_t)p.N);
     if (tid == 0) {
         r.sums[kCount] = count;
@@ -212,7 +213,7 @@ void paged_resize(PagedResize p, Records r) {
     __syncthreads();
     if (tid == 0) {
         int took = 0;
-        for (int k = 0; k < W; ++k) took = max(took, part[2][k]);
+        for (int k = 0; k < W; ++k) took = max(took, part[0][k]);
         p.new_count[0] = available - took;
     }
     if constexpr (ALONE) pages_and_slots<4>(p, r, tid, THREADS);
