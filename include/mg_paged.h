@@ -94,8 +94,10 @@ size_t mg_paged_resize_workspace_bytes(int B, int T);
  * out, infinities count as the type's largest value.
  *
  * A slot must not occur twice in a call, and the rows of one page must follow
- * each other in `slot` with rising slots, as mg_paged_resize gives them:
- * otherwise which row a slot holds is not defined, nor what bounds its page has.
+ * each other in `slot`, without a row of another page or one without a slot
+ * between them, with rising slots, as mg_paged_resize gives them (slots may be
+ * left out): otherwise which row a slot holds is not defined, nor what bounds its
+ * page has.
  * T*H at most 2^28.
  */
 mg_status_t mg_paged_append(const void *K, const void *V, void *Kp, void *Vp, void *bounds,

@@ -1,8 +1,8 @@
 // paged_append.hip -- rows of K and V into their slots, and the bounds of the
 // pages they go to.
 //
-// A wave takes R rows of one head, 16 bytes a lane, and keeps their K.  Rows whose
-// slots follow each other inside a page are a run; the wave in whose rows a run
+// A wave takes R rows of one head, 16 bytes a lane, and keeps their K.  Rows, one behind
+// the other, whose slots rise inside a page are a run; the wave in whose rows a run
 // begins owns it, reads on to the run's end where that lies behind its rows, and
 // writes its bounds: every page has one writer, and no order of waves matters.  A
 // run of one row (a decode step) needs no reduction over lanes and costs nothing
@@ -132,7 +132,7 @@ void paged_append(AppendArgs a) {
     const int first = t0 > 0 ? a.slot[t0 - 1] : -1;
     const int shifted = __shfl_up(slot, 1, 64), before = lane == 0 ? first : shifted;
     const bool good = (uint32_t)slot < slots;
-    const bool on = good && (slot & (page - 1)) != 0 && before == slot - 1;
+    const bool on = good && before < slot && before >> a.shift == slot >> a.shift;
     const uint64_t goods = __ballot(good), ons = __ballot(on), starts = goods & ~ons & mine;
     const uint64_t singles = starts & ~(ons >> 1);
     const auto end_of = [&](int from) {   // of the run that begins there, as far as is known
@@ -211,9 +211,8 @@ void paged_append(AppendArgs a) {
                     if (done == known) {
                         // how many of the next 64 rows are the run's
                         if (R + known < 64) break;
-                        const int t = t0 + R + done, want = s + (t - t0 - from) + lane;
-                        const bool same =
-                            want >> a.shift == s >> a.shift && slot_of(t + lane) == want;
+                        const int t = t0 + R + done + lane, next = slot_of(t);
+                        const bool same = next >> a.shift == s >> a.shift && slot_of(t - 1) < next;
                         const uint64_t other = ~__ballot(same);
                         const int more = other == 0 ? 64 : __builtin_ctzll(other);
                         if (more == 0) break;
