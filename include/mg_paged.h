@@ -91,7 +91,9 @@ size_t mg_paged_resize_workspace_bytes(int B, int T);
  * whose first row is written holds the bounds of what this call writes to it,
  * others gone on with those and what they were.  (So they cover every token that
  * a page holds, and may cover ones that a sequence has since lost.)  NaN is left
- * out, infinities count as the type's largest value.
+ * out (of a channel that is NaN in all rows nothing is left: lo is the type's
+ * largest value, hi the lowest, which the next rows go on from), infinities count
+ * as the type's largest value.
  *
  * A slot must not occur twice in a call, and the rows of one page must follow
  * each other in `slot`, without a row of another page or one without a slot
@@ -142,11 +144,13 @@ size_t mg_attn_fwd_paged_workspace_bytes(int B, int Hq, int H, int Lq, int d, in
  * A page's score is the largest that its bounds allow a row of the group to give
  * one of its tokens (scale > 0):
  *
- *   max over the group's heads g of  sum_c max(Q[g][c] lo[c], Q[g][c] hi[c])
+ *   max over the group's heads g of  sum_c (max(Q[g][c], 0) hi[c] + min(Q[g][c], 0) lo[c])
  *
- * each sum in 64 bits, rounded to f32.  (Bounds are finite, as mg_paged_append
- * leaves them: a sum in which 0 meets an infinite one is NaN.  A page without an
- * entry in [0, N) counts as NaN.)
+ * each sum in 64 bits, rounded to f32.  (A channel that is NaN in all of a page's
+ * tokens, whose lo is the type's largest value and hi the lowest, takes the page
+ * behind the others where Q[g][c] is not 0: its tokens' scores are NaN.  Bounds are
+ * finite, as mg_paged_append leaves them: a sum in which 0 meets an infinite one is
+ * NaN.  A page without an entry in [0, N) counts as NaN.)
  *   index  int32 [B][H][Lq][keep]: pages j / page, ascending; -1 behind the last
  * B*H*Lq*P and B*H*Lq*keep at most 2^29.
  */

@@ -1,8 +1,9 @@
 // paged_select.hip -- the pages that each query row reads: scores from the pages'
 // bounds, and the largest of them.
 //
-// sum_c max(q_c lo_c, q_c hi_c) is sum_c max(q_c, 0) hi_c + min(q_c, 0) lo_c: a
-// matrix product of pages and rows over 2 d channels.  It runs on the f64 matrix
+// sum_c max(q_c, 0) hi_c + min(q_c, 0) lo_c (where lo <= hi: max(q_c lo_c, q_c hi_c)) is
+// a matrix product of pages and rows over 2 d channels.  A channel of NaN alone, whose
+// bounds are reversed, makes the sum as low as it goes.  It runs on the f64 matrix
 // units, as the choice must not hang on a sum's order: products of bf16 values are
 // exact, and so are nearly all of their sums.  (f32 sums would let pages next to
 // the border change places with the tile they are computed in.)
