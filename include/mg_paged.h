@@ -27,6 +27,9 @@
  * and O is rounded once.  LSE and the workspace are f32.  Sums are in chains of
  * at most 2^18 tokens.
  *
+ * In range are sums of |Q K| below 2^127, with any scale (one whose product with
+ * log2 e is infinite is refused).  Beyond that results may be infinite or NaN.
+ *
  * Ownership, asynchrony, errors: as for mg_attn.h.  The caller owns every
  * buffer; nothing is allocated; calls enqueue on `stream` and return; arguments
  * are checked on the host before anything is enqueued.  Rows, pools and

@@ -20,6 +20,9 @@
 //
 // bf16 probabilities enter as two bf16 parts each, which the matrix units have room
 // for.
+#include <algorithm>
+#include <cfloat>
+#include <cmath>
 #include <type_traits>
 
 #include "paged_device.h"
@@ -66,6 +69,41 @@ struct Cut {
     }
 };
 
+// What scores stand for: 2^(factor s) with factor = |scale| log2 e, as two numbers (of a
+// negative scale, Q's signs are turned).  Weights go by s less the row's largest, which
+// is exact where they matter: a product with the factor less a rounded maximum is off by
+// half a step of that maximum, which from 2^31 on is more than an exponent holds.
+struct Scale {
+    float factor, rest;
+    float lowest;   // times rest it is finite
+
+    // 2^(factor d), d <= 0 (-inf: 0; NaN stays).  f32: what the factor's rounding leaves
+    // counts too, 4e-7 at d = -20.
+    template <bool EXACT>
+    __device__ __forceinline__ float weight(float d) const {
+        if constexpr (EXACT) return exp2_fast(fmaf(d, factor, fmaxf(d, lowest) * rest));
+        return exp2_fast(d * factor);
+    }
+    // (sums of a part without a score above -inf are 0, or NaN where a score is)
+    template <bool EXACT>
+    __device__ __forceinline__ float of_part(float its_top, float top) const {
+        return its_top == -INFINITY ? 1.f : weight<EXACT>(its_top - top);
+    }
+    // log sum exp of a row with largest score m and sum l of weights: as row_lse, with the
+    // part of factor m that its f32 value leaves
+    __device__ __forceinline__ float lse(float m, float l) const {
+        if (l != l) return l;
+        if (!(l > 0.f)) return -INFINITY;
+        const float top = m * factor;
+        if (!(fabsf(top) < INFINITY)) return top;
+        const float e = (float)__builtin_amdgcn_frexp_expf(l);
+        const float n = top + e, a = n - top;
+        const float low = (top - (n - a)) + (e - a) + (fmaf(m, factor, -top) + m * rest);
+        return fmaf(n, kLn2, fmaf(n, kLn2Low, (__builtin_amdgcn_logf(
+                                                   __builtin_amdgcn_frexp_mantf(l)) + low) * kLn2));
+    }
+};
+
 struct AttnArgs {
     const void *Q, *Kp, *Vp;
     void *O;
@@ -74,7 +112,8 @@ struct AttnArgs {
     int2 *info;   // nullptr: every sequence (sparse: row) is one unit, nothing to join
     const int32_t *table, *index, *key_len, *q_len;
     int B, H, G, Lq, P, N, shift, causal, keep;
-    float scale_log2, scale_rest;   // scale log2 e as two numbers
+    Scale scale;
+    uint32_t turn;   // Q's sign bits where the scale is negative
     const int32_t *unit_of;   // many sequences: each unit's
     int splits, chunk, groups;
     Cut cut;
@@ -392,7 +431,7 @@ void paged_attn(AttnArgs a) {
         for (int s = 0; s < S::kPieces; ++s)
             q[r][s] = limit[r] > 0 ? *reinterpret_cast<const u32x4 *>(
                                          static_cast<const char *>(a.Q) + row_at[r] * RB + 64 * s +
-                                         16 * g)
+                                         16 * g) ^ a.turn
                                    : u32x4{0, 0, 0, 0};
 
     float m[RT], l[RT];
@@ -454,7 +493,7 @@ void paged_attn(AttnArgs a) {
             float top = -INFINITY;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const f32x4 x = s[r][t] * a.scale_log2;
+                const f32x4 x = s[r][t];
                 if (partly) {
                     const int left = limit[r] - now[t].token - 4 * g;
 #pragma unroll
@@ -466,7 +505,8 @@ void paged_attn(AttnArgs a) {
             }
             top = fmaxf(m[r], max_over_groups(top));
             if (__any(top > m[r])) {
-                const float alpha = m[r] == -INFINITY ? 0.f : exp2_fast(m[r] - top);
+                const float alpha =
+                    m[r] == -INFINITY ? 0.f : a.scale.template weight<!S::kHalf>(m[r] - top);
                 l[r] *= alpha;
 #pragma unroll
                 for (int j = 0; j < N; ++j) o[r][j] *= alpha;
@@ -475,18 +515,9 @@ void paged_attn(AttnArgs a) {
             const float from = m[r] == -INFINITY ? 0.f : m[r];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                // (rounded as a difference, not as the larger product; f32: what the factor's
-                // rounding leaves of scores counts too, 4e-7 of p at a score of 20)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float x = fmaf(s[r][t][e], a.scale_log2, -from);
-                    if constexpr (!S::kHalf) {   // (an infinite score is x already)
-                        const float finite =
-                            __builtin_amdgcn_fmed3f(s[r][t][e], -0x1.fffffep127f, 0x1.fffffep127f);
-                        x = fmaf(finite, a.scale_rest, x);
-                    }
-                    s[r][t][e] = exp2_fast(x);
-                }
+                for (int e = 0; e < 4; ++e)
+                    s[r][t][e] = a.scale.template weight<!S::kHalf>(s[r][t][e] - from);
                 if (partly) {
                     const int left = limit[r] - now[t].token - 4 * g;
 #pragma unroll
@@ -589,8 +620,7 @@ void paged_attn(AttnArgs a) {
         for (int k = 0; k < N; ++k) y[k] = 0.f;
 #pragma unroll
         for (int k = part; k < kWaves; k += TW) {
-            // without a score above -inf the sums are 0, or NaN where a score is
-            const float f = top == -INFINITY ? 1.f : exp2_fast(Ms[k][row] - top);
+            const float f = a.scale.template of_part<!S::kHalf>(Ms[k][row], top);
             sum = fmaf(f, Ls[k][row], sum);
 #pragma unroll
             for (int e = 0; e < N; ++e) y[e] = fmaf(f, Os[k][row][d0 + e], y[e]);
@@ -638,7 +668,7 @@ void paged_attn(AttnArgs a) {
         } else {
             *reinterpret_cast<f32x2 *>(out) = f32x2{y[0], y[1]};
         }
-        if (d0 == 0) a.LSE[to] = sum != sum ? sum : row_lse(top, sum);
+        if (d0 == 0) a.LSE[to] = a.scale.lse(top, sum);
     }
 }
 
@@ -650,6 +680,7 @@ struct JoinArgs {
     const float2 *stat;
     const int2 *info;   // nullptr: every sequence (row) has `splits` units
     int H, G, Lq, rows, splits, total;
+    Scale scale;
 };
 
 // WAVES waves join a row.  Lanes in teams of D / 4, four channels each, take the
@@ -702,7 +733,7 @@ void paged_join(JoinArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (k + e * STEP >= in.y) continue;
-            const float f = top == -INFINITY ? 1.f : exp2_fast(st[e].x - top);
+            const float f = a.scale.template of_part<sizeof(T) == 4>(st[e].x, top);
             sum = fmaf(f, st[e].y, sum);
             x += f * y[e];
         }
@@ -742,21 +773,28 @@ void paged_join(JoinArgs a) {
         for (int e = 0; e < 4; ++e) y[e] = sum == 0.f ? 0.f : x[e] * inv;
         store_row(static_cast<T *>(a.O) + to * D + d0, y);
     }
-    if (lane == 0) a.LSE[to] = sum != sum ? sum : row_lse(top, sum);
+    if (lane == 0) a.LSE[to] = a.scale.lse(top, sum);
 }
 
 Cut cut_of(const PagedPlan &plan) {
     return {plan.chunk, plan.share, plan.round, plan.round_most};
 }
 
+Scale scale_of(const PagedAttn &p) {
+    const double whole = std::fabs(p.scale * 1.4426950408889634);
+    const float factor = (float)whole, rest = (float)(whole - factor);
+    return {factor, rest, rest == 0.f ? -FLT_MAX : -(float)std::min<double>(
+                                                       FLT_MAX, 0x1p126 / std::fabs(rest))};
+}
+
 template <typename T, int D>
 hipError_t attn(const PagedAttn &p, const PagedPlan &plan, const void *Q, const void *Kp,
                 const void *Vp, void *O, float *LSE, char *ws, hipStream_t s) {
-    const double factor = p.scale * 1.4426950408889634;
     const AttnArgs a = {Q, Kp, Vp, O, LSE, (float *)(ws + plan.part), (float2 *)(ws + plan.stat),
                         plan.most > 1 ? (int2 *)(ws + plan.info) : nullptr, p.table, p.index,
                         p.key_len, p.q_len, p.B, p.H, p.G, p.Lq, p.P, p.N, p.shift, p.causal,
-                        p.keep, (float)factor, (float)(factor - (float)factor),
+                        p.keep, scale_of(p),
+                        p.scale < 0.f ? p.half ? 0x80008000u : 0x80000000u : 0u,
                         plan.lengths ? (const int32_t *)(ws + plan.map) : nullptr, plan.splits,
                         plan.chunk, plan.groups, cut_of(plan)};
     const unsigned grid = (unsigned)((int64_t)plan.units * p.H * plan.groups);
@@ -788,7 +826,7 @@ hipError_t join(const PagedAttn &p, const PagedPlan &plan, void *O, float *LSE, 
     const int64_t total = (int64_t)p.B * (sparse ? p.Lq : 1) * p.H * rows;
     const JoinArgs a = {O, LSE, (const float *)(ws + plan.part), (const float2 *)(ws + plan.stat),
                         sparse ? nullptr : (const int2 *)(ws + plan.info), p.H, p.G, p.Lq, rows,
-                        plan.splits, (int)total};
+                        plan.splits, (int)total, scale_of(p)};
     if (plan.join_waves == 1)
         paged_join<T, D, 1><<<(unsigned)((total + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
     else

@@ -1,0 +1,45 @@
+"""Scores of any size that the type's products have (mg_paged.h: "In range"): the
+tokens of the largest score, all others without weight."""
+import numpy as np
+import pytest
+
+import paged_ref as ref
+import paged_tight as tight
+from gpu_util import say
+from test_gpu_paged import kind_of
+from test_gpu_paged_tight import attention
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("contract", ["fast_bf16", "strict_f32"])
+@pytest.mark.parametrize("scale", [0.3, -1.7, 2.0 ** -30 / 3])
+@pytest.mark.parametrize("B,Hq,H,Lq,d,page,key_len,listed", [
+    (2, 4, 2, 3, 32, 16, [40, 9], False), (2, 8, 1, 5, 64, 64, [250, 700], False),
+    (1, 8, 2, 1, 128, 16, [9000], False), (2, 8, 2, 2, 64, 32, [3000, 129], True)])
+def test_scores_of_any_size(gpu_lib, B, Hq, H, Lq, d, page, key_len, listed, scale, contract):
+    """Products are whole numbers times a power of two, so scores are exact; from 2^7 on
+    one that is not the largest has no weight in f32."""
+    say("paged range B%d Hq%d d%d %s scale %g %s" % (B, Hq, d, key_len, scale, contract))
+    rng = np.random.default_rng(d + B)
+    P, G, N = ref.pages(max(key_len), page), Hq // H, 30
+    table = rng.integers(0, N, (B, P))
+    K = rng.integers(-3, 4, (N, H, page, d)).astype(np.float32)
+    K[..., 3:] = rng.integers(-200, 201, (N, H, page, d - 3))
+    V = rng.integers(-1, 2, (N, H, page, d)).astype(np.float32)
+    index = np.tile(np.arange(P), (B, H, Lq, 1)) if listed else None
+    whole = rng.integers(1, 4, (B, Hq, Lq, 3)) * rng.choice([-1, 1], (B, Hq, Lq, 3))
+    down = 2.0 ** np.ceil(np.log2(1 / abs(scale)))   # scores from 1 on, whatever the scale
+    for power in (7, 20, 31, 40, 75, 90):
+        Q = np.zeros((B, Hq, Lq, d), np.float32)
+        Q[..., :3] = whole * 2.0 ** power * down
+        O, LSE = attention(gpu_lib, Q, K, V, table, key_len, None, scale, contract, index)
+        for b, hq, i in np.ndindex(B, Hq, Lq):
+            j = np.arange(ref.limit(key_len[b], Lq, i, True))
+            at = (table[b, j // page], hq // G, j % page)
+            s = K[at].astype(np.float64) @ Q[b, hq, i].astype(np.float64) * np.float64(np.float32(scale))
+            most = s == s.max()
+            want = V[at][most].astype(np.float64).mean(0), s.max() + np.log(most.sum())
+            off = tight.marked_off(O[b, hq, i][None], LSE[b, hq, i][None], want[0][None],
+                                   np.array([want[1]]), kind_of(contract))
+            assert not off.any(), (power, b, hq, i, O[b, hq, i][:4], LSE[b, hq, i], want[1])
