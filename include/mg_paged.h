@@ -28,7 +28,9 @@
  * at most 2^18 tokens.
  *
  * In range are sums of |Q K| below 2^127, with any scale (one whose product with
- * log2 e is infinite is refused).  Beyond that results may be infinite or NaN.
+ * log2 e is infinite is refused), and n tokens of |V| below 2^127 / n (2^103 at any
+ * length), as a row's weights, of which the largest is 1, are added before they are
+ * divided.  Beyond that results may be infinite or NaN.
  *
  * Ownership, asynchrony, errors: as for mg_attn.h.  The caller owns every
  * buffer; nothing is allocated; calls enqueue on `stream` and return; arguments

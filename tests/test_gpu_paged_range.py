@@ -1,5 +1,4 @@
-"""Scores of any size that the type's products have (mg_paged.h: "In range"): the
-tokens of the largest score, all others without weight."""
+"""Scores and values of any size in range (mg_paged.h: "In range")."""
 import numpy as np
 import pytest
 
@@ -43,3 +42,28 @@ def test_scores_of_any_size(gpu_lib, B, Hq, H, Lq, d, page, key_len, listed, sca
             off = tight.marked_off(O[b, hq, i][None], LSE[b, hq, i][None], want[0][None],
                                    np.array([want[1]]), kind_of(contract))
             assert not off.any(), (power, b, hq, i, O[b, hq, i][:4], LSE[b, hq, i], want[1])
+
+
+@pytest.mark.parametrize("contract", ["fast_bf16", "strict_f32"])
+@pytest.mark.parametrize("power", [-100, 103])
+@pytest.mark.parametrize("B,Hq,H,Lq,d,page,P,key_len,listed", [
+    (2, 8, 2, 3, 64, 16, 30, 477, False), (1, 16, 1, 1, 128, 64, 2000, 128000, False),
+    (2, 8, 2, 1, 32, 128, 300, 38000, True)])
+def test_values_of_any_size(gpu_lib, B, Hq, H, Lq, d, page, P, key_len, listed, power, contract):
+    """Whole numbers times a power of two, added exactly (paged_tight.py)."""
+    say("paged range of V 2^%d d%d %d tokens %s" % (power, d, key_len, contract))
+    rng = np.random.default_rng(P)
+    N, G, unit = 60, Hq // H, 2.0 ** power
+    K, V = tight.marked_inputs(rng, N, H, page, d)
+    V[:, :, 0] = 1   # sums grow with the length
+    Q, channel = tight.marked_rows(rng, B, Hq, Lq, d)
+    table = rng.integers(0, N, (B, P))
+    index = np.tile(np.arange(P), (B, H, Lq, 1)) if listed else None
+    O, LSE = attention(gpu_lib, Q, K, (V * unit).astype(np.float32), table, [key_len] * B, None, 1.0,
+                       contract, index)
+    for b, h, i in np.ndindex(B, H, Lq):
+        j = np.arange(ref.limit(key_len, Lq, i, True))
+        hq = slice(h * G, (h + 1) * G)
+        want = tight.marked(K, V, table[b, j // page], j % page, h, channel[b, hq, i])
+        off = tight.marked_off(O[b, hq, i] / unit, LSE[b, hq, i], *want, kind_of(contract))
+        assert not off.any(), (b, h, i, O[b, hq, i] / unit - want[0])
