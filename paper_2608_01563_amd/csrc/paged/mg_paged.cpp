@@ -14,18 +14,24 @@
 namespace mg {
 
 namespace {
+// (Measured at d = 128, where a compute unit runs three workgroups of 16 rows or two of 32.
+// Smaller heads fit more, d = 32 bf16 six and five, d = 64 four and three, and are cut
+// alike: 4.8 to 4.9 TB/s over 8 long caches, 5.3 with d = 128.)
 constexpr int kWant = 1536;       // workgroups of 16 rows that a call is cut into: six a
-                                  // compute unit, of which three run at once
-constexpr int kWantMore = 1024;   // of more rows: four, of which two run at once
+                                  // compute unit
+constexpr int kWantMore = 1024;   // of more rows: four
 constexpr int kRound = 512;       // of a short call
 constexpr int kLeast = 4;         // blocks of a unit: one a wave (2 sequences of 1,020 tokens, 8
                                   // heads: 10.6 us with 4, 12.1 with 8, 13.6 with 32, f32 11.5,
                                   // 15.0, 30.8)
-constexpr int64_t kCached = 64 << 20;   // bytes that caches may hold from call to call
+// Bytes that caches may hold from call to call; by the room in tables, not the lengths.
+// (4 to 130 MB held in roomy tables: 0 to 5 % slower past the caches.  Shared pages: 16
+// sequences over the same 8,192 tokens 57 us, 47 through the caches.)
+constexpr int64_t kCached = 64 << 20;
 constexpr int kLongest = 1 << 13; // blocks of a unit (2^18 tokens)
 
 void paged_workspace(PagedPlan &plan, const PagedAttn &p, int64_t rows) {
-    plan.join_waves = plan.most <= 16 ? 1 : 4;
+    plan.join_waves = plan.most <= 16 ? 1 : 4;   // (by the room in tables, not the lengths)
     if (plan.most <= 1) return;
     const size_t slots = (size_t)plan.units * p.H * rows;
     plan.part = plan.bytes;

@@ -40,7 +40,8 @@ constexpr int kFar = 1 << 30;   // a token that no row sees
 
 // Where lengths decide, every sequence is cut into units of `chunk` blocks at most, at
 // least one unit each and all of a sequence alike (so that none is left with a few
-// blocks).  Of 8 cache heads, in us, by the workgroups that the lengths are cut into:
+// blocks).  Of 8 cache heads, bf16, d = 128, in us, by the workgroups that the lengths are
+// cut into:
 //
 //                                                    384   512   768  1536
 //   8 sequences of 16,384 to 65,536 tokens, 1 row    219   180   179   190
@@ -48,7 +49,7 @@ constexpr int kFar = 1 << 30;   // a token that no row sees
 //   4 of 32,768, 1 row                               101    86    87    92
 //   8 of 1,000 to 4,001, 28 rows                      31    27    35    35
 //
-// So: one round, two workgroups a compute unit or (where three fit) three, if units of
+// So: one round, two workgroups a compute unit or (of 16 rows) three, if units of
 // some length, at most a third longer than would do without remainders, make no more
 // of them and fill them to 13 in 16, or if they are short; `share` units, several
 // rounds, otherwise.

@@ -53,7 +53,7 @@ struct PagedPlan {
     int splits;    // units of every sequence; 0: as many as its length asks for
     int chunk;     // blocks of a unit (splits 0: at least)
     int share;     // splits 0: units that all lengths together are cut into
-    int round, round_most;   // splits 0: units that run at once, surely and if all goes well
+    int round, round_most;   // splits 0: units of one round, two or three a compute unit
     int rows;      // of a workgroup: 16, 32, 64 or 128
     int groups;    // workgroups of a unit and cache head
     bool once;     // K and V are read past the caches

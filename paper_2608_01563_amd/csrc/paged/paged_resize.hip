@@ -242,6 +242,8 @@ Records records_of(const PagedResize &p, void *ws) {
 
 }  // namespace
 
+// (Pages given back do not count here: some 10,000 cost nothing, 65,536 take 25 us where
+// the grid needs 8.)
 bool paged_resize_alone(int B, int T) { return B <= 1024 && T <= 2048; }
 
 size_t paged_resize_bytes(int B, int T) {
